@@ -285,6 +285,116 @@ reqat_status reqat_fakequant_kv4(const void *x, int64_t rows, int64_t cols, int6
                                  void *stream);
 
 /*
+ * Paged KV4 cache: the 4-bit KV cache of the W4A4KV4 setting (Sec. 4.3) as a
+ * serving loop keeps it.  The caller allocates it, page by page of every KV
+ * head, and says in a page table which pages hold a sequence's tokens; a slot is
+ * page * page_size + the token's place in the page.  Per page and head (D =
+ * head_dim, P = page_size; the elements, block scales and rounding of
+ * reqat_quantize_kv4 with blocks of 16 channels of a head):
+ *   k_codes  [pages][heads][P][D/2]           element 2i in bits 3:0 of byte i
+ *   k_scales [pages][heads][P][D/16]
+ *   v_codes  [pages][heads][P/4][D/8][4][4]   at (g, w, t): channels 8w .. 8w+7 of token 4g+t
+ *   v_scales [pages][heads][P/4][D/16][4]
+ * (the values four tokens together, as the product with them wants them).
+ * Keys are held less the shift: k - m.  A page that has not been written may
+ * hold any bytes: only the tokens that a call names are read.
+ *   k_tensor_scale, v_tensor_scale: device floats, g of reqat_quantize_kv4
+ *     (REQAT_TS_GIVEN: finite, > 0), the same for every call on the cache;
+ *   k_shift: NULL or heads * D floats on the device (16-byte aligned);
+ *   page_size: a power of two from 16 to 2^20; head_dim: 64 or 128.
+ * The four arrays are 16-byte aligned.  The struct itself is host memory, read
+ * during the call.
+ * Errors of every call below: REQAT_E_NULL (a pointer), REQAT_E_SHAPE (a size,
+ * page_size), REQAT_E_ALIGN, REQAT_E_UNSUPPORTED (head_dim, others as stated).
+ */
+typedef struct reqat_kv4_cache_s {
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    const float *k_tensor_scale, *v_tensor_scale;
+    const float *k_shift;
+    int64_t num_pages;
+    int64_t page_size, kv_heads, head_dim;
+} reqat_kv4_cache;
+
+/*
+ * Write T tokens into the cache (the KV4 cache write, with the rotary position
+ * and the post-RoPE shift in the same pass, Sec. 4.3, K~ = R(K_pre) - m).
+ *   slots [T] int64: where each token goes; a slot outside the cache (say -1)
+ *     marks padding, whose keys and values go nowhere.  Two tokens of a call
+ *     must not share a slot.
+ *   k, v [T][ld] bfloat16: heads * D columns (slices of the fused QKV output).
+ *   rope_cos, rope_sin [rope_len][D/2] FP32 and positions [T] int32: row
+ *     positions[t] rotates the token's keys and queries, channel c of a head
+ *     with c + D/2, in FP32, every operation rounded:
+ *       lo' = RN(RN(lo cos) - RN(hi sin)),  hi' = RN(RN(hi cos) + RN(lo sin)).
+ *     A position outside the tables gives NaN.  All NULL: no rotation.
+ *   Keys: RN_fp32(lo' - m), without a rounding to bfloat16 in between, then the
+ *     block quantization of reqat_quantize_kv4 under the cache's scale; values
+ *     likewise without rotation and shift.
+ *   q [T][ldq] bfloat16, q_heads * D columns: the queries, rotated into q_out
+ *     [T][ldq_out] bfloat16, RN_bf16 (padding tokens too).  q_out == q with the
+ *     same stride is allowed, any other overlap is not (REQAT_E_UNSUPPORTED).
+ *     q_heads == 0: none (q, q_out NULL).  Queries need the tables.
+ * Strides are multiples of 8 elements and at least the columns; k, v, q, q_out
+ * and the tables 16-byte aligned.  T == 0 is a no-op.
+ */
+reqat_status reqat_kv4_append(const reqat_kv4_cache *cache, int64_t T, const int64_t *slots, const void *k, int64_t ldk,
+                              const void *v, int64_t ldv, const void *q, int64_t ldq, int64_t q_heads, void *q_out,
+                              int64_t ldq_out, const float *rope_cos, const float *rope_sin, const int32_t *positions,
+                              int64_t rope_len, void *stream);
+
+/*
+ * Read T slots back: k_out, v_out [T][ld] bfloat16 (either may be NULL),
+ * RN_bf16(E1M2(code) * s * g), in the shifted domain, or with add_shift != 0
+ * RN_bf16(RN_fp32(RN_fp32(E1M2(code) * s * g) + m)) for the keys.  NaN (0x7FC0)
+ * where the scale byte is NaN; zeros for a slot outside the cache.
+ * Strides and alignment as reqat_kv4_append.
+ */
+reqat_status reqat_kv4_gather(const reqat_kv4_cache *cache, int64_t T, const int64_t *slots, void *k_out, int64_t ldk,
+                              void *v_out, int64_t ldv, int add_shift, void *stream);
+
+/*
+ * Attention of the queries of B sequences over their cached tokens (the KV4
+ * attention of W4A4KV4 serving): for query i of the nq queries of sequence b,
+ * head h, and the cached values k^, v^ of KV head h / (q_heads / kv_heads),
+ *     out = sum_j softmax_j(sm_scale q . k^_j) v^_j
+ * over the tokens j < kv_len[b], when causal those with j <= kv_len[b] - nq + i
+ * (the queries are the last nq tokens).  k^ is in the shifted domain: a shift
+ * moves all scores of a row alike and leaves the softmax as it is.
+ *   q [T][ldq] bfloat16, q_heads * D columns; sequence b's queries are the rows
+ *     q_start[b] .. q_start[b+1] - 1 (int32 [B+1], not decreasing, within
+ *     0 .. T), or row b when q_start is NULL (then T == B).
+ *   kv_len [B] int32: cached tokens, the new ones included.
+ *   block_table [B][ld_table] int32: the page of tokens p * page_size ..,
+ *     table_cols entries of a row are used (ld_table >= table_cols).
+ *   max_q, max_kv: bounds on every nq and kv_len (they size the launch).
+ *   out [T][ldo] bfloat16; lse NULL or [T][q_heads] FP32, the natural logarithm
+ *     of sum_j exp(sm_scale q . k^_j) (of the shifted keys).
+ *   workspace: reqat_kv4_attention_workspace_bytes(...) bytes, 16-byte aligned
+ *     (may be NULL when that is 0): partial results of long sequences.
+ * A row without a visible token gets zeros and lse -Inf.  What a row does not
+ * see does not reach it, NaN included; a NaN or Inf in its query or a NaN among
+ * its visible keys or values does.  A visible token whose page entry lies outside the
+ * cache is not read and gives NaN, and so do rows of a sequence with kv_len
+ * beyond max_kv or beyond the table.  Queries beyond max_q and rows of no
+ * sequence are left as they are.
+ * Computed in FP32; the products run on FP16 matrix cores: the queries under a
+ * power-of-two factor per row, keys and values exact, the weights p rounded to
+ * FP16.  sm_scale is finite and > 0 (REQAT_E_UNSUPPORTED), q_heads a multiple of
+ * kv_heads.  Strides and alignment as reqat_kv4_append.  The result is
+ * deterministic: kernel and splits follow from the host's sizes, and partial
+ * results are joined in a fixed order.
+ */
+reqat_status reqat_kv4_attention(const reqat_kv4_cache *cache, int64_t B, int64_t T, const void *q, int64_t ldq,
+                                 int64_t q_heads, const int32_t *q_start, const int32_t *kv_len,
+                                 const int32_t *block_table, int64_t ld_table, int64_t table_cols, int64_t max_q,
+                                 int64_t max_kv, int causal, float sm_scale, void *out, int64_t ldo, float *lse,
+                                 void *workspace, void *stream);
+
+/* Bytes of workspace reqat_kv4_attention needs (0: none; 0 on bad arguments). */
+size_t reqat_kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int64_t q_heads,
+                                           int64_t kv_heads, int64_t head_dim);
+
+/*
  * SEM loss, the training objective of ReQAT's TAQ stage (Sec. 4.2):
  *     L = (1/T) sum_t NLL_t + lambda (1/T) sum_t w_t H_t,
  *     w_t = max(0, 1 - (H_t - H_min) / (tau - H_min + eps)),

@@ -165,6 +165,124 @@ reqat_status reqat_fakequant_kv4(const void *x, int64_t rows, int64_t cols, int6
     return run_kv4(x, rows, cols, ldx, shift, nullptr, nullptr, y, ldy, tensor_scale, ts, workspace, stream, true);
 }
 
+// The cache's own arguments; *view is filled when they hold.
+static reqat_status check_kv4_cache(const reqat_kv4_cache *c, Kv4View *view) {
+    if (!c) return REQAT_E_NULL;
+    if (c->num_pages < 0 || c->kv_heads <= 0 || c->kv_heads > 65535) return REQAT_E_SHAPE;
+    if (c->page_size < 16 || c->page_size > (1 << 20) || (c->page_size & (c->page_size - 1))) return REQAT_E_SHAPE;
+    if (c->head_dim != 64 && c->head_dim != 128) return REQAT_E_UNSUPPORTED;
+    // every byte offset has to fit 63 bits
+    if (c->num_pages > INT64_MAX / 128 / c->page_size / c->kv_heads) return REQAT_E_SHAPE;
+    if (!c->k_tensor_scale || !c->v_tensor_scale) return REQAT_E_NULL;
+    if (c->num_pages > 0 && (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales)) return REQAT_E_NULL;
+    if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales) ||
+        !aligned16(c->k_shift))
+        return REQAT_E_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(c->k_tensor_scale) | reinterpret_cast<uintptr_t>(c->v_tensor_scale)) & 3u)
+        return REQAT_E_ALIGN;
+    *view = {c->k_codes, c->k_scales, c->v_codes, c->v_scales, c->k_tensor_scale, c->v_tensor_scale, c->k_shift,
+             c->num_pages, __builtin_ctzll((unsigned long long)c->page_size), (int)c->kv_heads, (int)c->head_dim};
+    return REQAT_OK;
+}
+
+// A bfloat16 matrix of `cols` columns: stride and alignment.
+static reqat_status check_rows(const void *p, int64_t ld, int64_t cols) {
+    if (ld < cols) return REQAT_E_SHAPE;
+    if (!aligned16(p) || ld % 8) return REQAT_E_ALIGN;
+    return REQAT_OK;
+}
+
+reqat_status reqat_kv4_append(const reqat_kv4_cache *cache, int64_t T, const int64_t *slots, const void *k, int64_t ldk,
+                              const void *v, int64_t ldv, const void *q, int64_t ldq, int64_t q_heads, void *q_out,
+                              int64_t ldq_out, const float *rope_cos, const float *rope_sin, const int32_t *positions,
+                              int64_t rope_len, void *stream) {
+    Kv4View view;
+    reqat_status st = check_kv4_cache(cache, &view);
+    if (st != REQAT_OK) return st;
+    if (T < 0 || T > 0x7FFFFFFF || q_heads < 0 || q_heads > 65535) return REQAT_E_SHAPE;
+    const bool rope = rope_cos || rope_sin || positions;
+    if (rope && rope_len < 0) return REQAT_E_SHAPE;
+    if (rope && (!rope_cos || !rope_sin || (T > 0 && !positions))) return REQAT_E_NULL;
+    if (q_heads > 0 && !rope) return REQAT_E_NULL;
+    if (T == 0) return REQAT_OK;
+    if (!slots || !k || !v || (q_heads > 0 && (!q || !q_out))) return REQAT_E_NULL;
+    const int64_t cols = cache->kv_heads * cache->head_dim, qcols = q_heads * cache->head_dim;
+    if ((st = check_rows(k, ldk, cols)) != REQAT_OK || (st = check_rows(v, ldv, cols)) != REQAT_OK) return st;
+    if (q_heads > 0 && ((st = check_rows(q, ldq, qcols)) != REQAT_OK || (st = check_rows(q_out, ldq_out, qcols)) != REQAT_OK))
+        return st;
+    if (rope && (!aligned16(rope_cos) || !aligned16(rope_sin))) return REQAT_E_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(slots) & 7u) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return REQAT_E_ALIGN;
+    if (q_heads > 0 && overlaps(q, span_bf16(T, qcols, ldq), q_out, span_bf16(T, qcols, ldq_out)) &&
+        (q != q_out || ldq != ldq_out))
+        return REQAT_E_UNSUPPORTED;
+    hipError_t e = launch_kv4_append(view, T, slots, reinterpret_cast<const uint16_t *>(k), ldk,
+                                     reinterpret_cast<const uint16_t *>(v), ldv, reinterpret_cast<const uint16_t *>(q),
+                                     ldq, (int)q_heads, reinterpret_cast<uint16_t *>(q_out), ldq_out, rope_cos, rope_sin,
+                                     positions, rope_len, reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? REQAT_OK : REQAT_E_HIP;
+}
+
+reqat_status reqat_kv4_gather(const reqat_kv4_cache *cache, int64_t T, const int64_t *slots, void *k_out, int64_t ldk,
+                              void *v_out, int64_t ldv, int add_shift, void *stream) {
+    Kv4View view;
+    reqat_status st = check_kv4_cache(cache, &view);
+    if (st != REQAT_OK) return st;
+    if (T < 0 || T > 0x7FFFFFFF) return REQAT_E_SHAPE;
+    if (T == 0 || (!k_out && !v_out)) return REQAT_OK;
+    if (!slots) return REQAT_E_NULL;
+    const int64_t cols = cache->kv_heads * cache->head_dim;
+    if (k_out && (st = check_rows(k_out, ldk, cols)) != REQAT_OK) return st;
+    if (v_out && (st = check_rows(v_out, ldv, cols)) != REQAT_OK) return st;
+    if (reinterpret_cast<uintptr_t>(slots) & 7u) return REQAT_E_ALIGN;
+    hipError_t e = launch_kv4_gather(view, T, slots, reinterpret_cast<uint16_t *>(k_out), ldk,
+                                     reinterpret_cast<uint16_t *>(v_out), ldv, add_shift != 0,
+                                     reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? REQAT_OK : REQAT_E_HIP;
+}
+
+static bool kv4_attention_sizes_ok(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int64_t q_heads,
+                                   int64_t kv_heads) {
+    return B >= 0 && B <= 65535 && T >= 0 && T <= 0x7FFFFFFF && max_q >= 0 && max_q <= 0x7FFFFFFF && max_kv >= 0 &&
+           max_kv <= 0x7FFFFFFF && kv_heads > 0 && kv_heads <= 65535 && q_heads > 0 && q_heads <= 65535 &&
+           q_heads % kv_heads == 0;
+}
+
+size_t reqat_kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int64_t q_heads,
+                                           int64_t kv_heads, int64_t head_dim) {
+    if (!kv4_attention_sizes_ok(B, T, max_q, max_kv, q_heads, kv_heads) || (head_dim != 64 && head_dim != 128)) return 0;
+    return kv4_attention_workspace_bytes(B, T, max_q < T ? max_q : T, max_kv, (int)q_heads, (int)kv_heads, (int)head_dim);
+}
+
+reqat_status reqat_kv4_attention(const reqat_kv4_cache *cache, int64_t B, int64_t T, const void *q, int64_t ldq,
+                                 int64_t q_heads, const int32_t *q_start, const int32_t *kv_len,
+                                 const int32_t *block_table, int64_t ld_table, int64_t table_cols, int64_t max_q,
+                                 int64_t max_kv, int causal, float sm_scale, void *out, int64_t ldo, float *lse,
+                                 void *workspace, void *stream) {
+    Kv4View view;
+    reqat_status st = check_kv4_cache(cache, &view);
+    if (st != REQAT_OK) return st;
+    if (!kv4_attention_sizes_ok(B, T, max_q, max_kv, q_heads, cache->kv_heads)) return REQAT_E_SHAPE;
+    if (table_cols < 0 || table_cols > 0x7FFFFFFF || ld_table < table_cols || (!q_start && T != B)) return REQAT_E_SHAPE;
+    if (!(sm_scale > 0.0f) || sm_scale > 3.4028234e38f) return REQAT_E_UNSUPPORTED;
+    if (B == 0 || T == 0 || max_q == 0) return REQAT_OK;
+    if (!q || !out || !kv_len || (table_cols > 0 && !block_table)) return REQAT_E_NULL;
+    const int64_t cols = q_heads * cache->head_dim;
+    if ((st = check_rows(q, ldq, cols)) != REQAT_OK || (st = check_rows(out, ldo, cols)) != REQAT_OK) return st;
+    if ((reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(kv_len) |
+         reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(lse)) & 3u)
+        return REQAT_E_ALIGN;
+    if (max_q > T) max_q = T;
+    const size_t need = kv4_attention_workspace_bytes(B, T, max_q, max_kv, (int)q_heads, view.heads, view.D);
+    if (need > 0 && !workspace) return REQAT_E_NULL;
+    if (!aligned16(workspace)) return REQAT_E_ALIGN;
+    if (overlaps(q, span_bf16(T, cols, ldq), out, span_bf16(T, cols, ldo))) return REQAT_E_UNSUPPORTED;
+    const Kv4AttnArgs a = {view, reinterpret_cast<const uint16_t *>(q), reinterpret_cast<uint16_t *>(out), lse, q_start,
+                           kv_len, block_table, B, T, ldq, ldo, ld_table, table_cols, max_q, max_kv, (int)q_heads,
+                           causal != 0, sm_scale, workspace};
+    hipError_t e = launch_kv4_attention(a, reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? REQAT_OK : REQAT_E_HIP;
+}
+
 static reqat_status run_rht(const void *x, int64_t rows, int64_t cols, int64_t ldx, uint32_t signs,
                             uint8_t *codes, uint8_t *scales, void *y, int64_t ldy, void *stream, bool fake) {
     reqat_status st = check_quant(REQAT_FMT_MXFP4, x, rows, cols, ldx, fake ? y : codes, scales, ldy,

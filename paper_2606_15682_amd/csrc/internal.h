@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "dispatch.h"
+#include "kv4_cache.h"
 
 namespace reqat {
 
@@ -66,6 +67,32 @@ hipError_t launch_w4a16_pack(const uint8_t *codes, const uint8_t *scales, int64_
 hipError_t launch_kv4(QuantOut out, const uint16_t *x, int64_t rows, int64_t cols, int64_t ldx, const float *shift,
                       uint8_t *codes, uint8_t *scales, uint16_t *y, int64_t ldy, float *gptr, bool computed,
                       uint32_t *partials, uint16_t *seg_table, hipStream_t stream);
+
+// Paged KV4 cache (kv4_cache.hip): D is 64 or 128.  q may be null (q_heads 0); cos null: no rotation.
+hipError_t launch_kv4_append(const Kv4View &c, int64_t T, const int64_t *slots, const uint16_t *k, int64_t ldk,
+                             const uint16_t *v, int64_t ldv, const uint16_t *q, int64_t ldq, int q_heads,
+                             uint16_t *q_out, int64_t ldq_out, const float *cos, const float *sin,
+                             const int32_t *positions, int64_t rope_len, hipStream_t stream);
+// k or v may be null.
+hipError_t launch_kv4_gather(const Kv4View &c, int64_t T, const int64_t *slots, uint16_t *k, int64_t ldk, uint16_t *v,
+                             int64_t ldv, bool add_shift, hipStream_t stream);
+
+// Attention over the cache (kv4_attention.hip).
+struct Kv4AttnArgs {
+    Kv4View c;
+    const uint16_t *q;
+    uint16_t *out;
+    float *lse;                            // [T][q_heads] or null
+    const int32_t *q_start, *kv_len, *table;
+    int64_t B, T, ldq, ldo, ld_table, table_cols, max_q, max_kv;
+    int q_heads;
+    bool causal;
+    float scale;
+    void *workspace;
+};
+size_t kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads,
+                                     int D);
+hipError_t launch_kv4_attention(const Kv4AttnArgs &a, hipStream_t stream);
 
 // SEM loss: per-row statistics ([T][4]: H, NLL, lse, 0), weights [T], loss[4]
 // (L, L_SFT, L_ent, tau); backward writes dL/dlogits.  V % 8 == 0.

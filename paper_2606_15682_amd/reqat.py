@@ -58,6 +58,12 @@ SIGNATURES = {
                                        _VP, _INT, _I64, _VP]),
     "reqat_quantize_kv4": (_INT, [_VP, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _INT, _VP, _VP]),
     "reqat_fakequant_kv4": (_INT, [_VP, _I64, _I64, _I64, _VP, _VP, _I64, _VP, _INT, _VP, _VP]),
+    "reqat_kv4_append": (_INT, [_VP, _I64, _VP, _VP, _I64, _VP, _I64, _VP, _I64, _I64, _VP, _I64, _VP, _VP, _VP, _I64,
+                                _VP]),
+    "reqat_kv4_gather": (_INT, [_VP, _I64, _VP, _VP, _I64, _VP, _I64, _INT, _VP]),
+    "reqat_kv4_attention": (_INT, [_VP, _I64, _I64, _VP, _I64, _I64, _VP, _VP, _VP, _I64, _I64, _I64, _I64, _INT,
+                                   ctypes.c_float, _VP, _I64, _VP, _VP, _VP]),
+    "reqat_kv4_attention_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _I64, _I64, _I64, _I64, _I64]),
     "reqat_gemm_w4a16": (_INT, [_I64, _I64, _I64, _VP, _I64, _VP, _VP, _VP, _INT, _I64, _VP, _VP]),
     "reqat_w4a16_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _I64]),
     "reqat_w4a16_packed_bytes": (ctypes.c_size_t, [_I64, _I64]),
@@ -142,6 +148,37 @@ def reqat_quantize_kv4(x, rows, cols, ldx, shift, codes, scales, tensor_scale, t
 
 def reqat_fakequant_kv4(x, rows, cols, ldx, shift, y, ldy, tensor_scale, ts, workspace, stream):
     return load().reqat_fakequant_kv4(x, rows, cols, ldx, shift, y, ldy, tensor_scale, ts, workspace, stream)
+
+
+class Kv4CacheStruct(ctypes.Structure):
+    """reqat_kv4_cache of the C ABI; the calls below take it by reference."""
+    _fields_ = [("k_codes", _VP), ("k_scales", _VP), ("v_codes", _VP), ("v_scales", _VP),
+                ("k_tensor_scale", _VP), ("v_tensor_scale", _VP), ("k_shift", _VP),
+                ("num_pages", _I64), ("page_size", _I64), ("kv_heads", _I64), ("head_dim", _I64)]
+
+
+def _cache_ref(cache):
+    return None if cache is None else ctypes.addressof(cache)
+
+
+def reqat_kv4_append(cache, T, slots, k, ldk, v, ldv, q, ldq, q_heads, q_out, ldq_out, rope_cos, rope_sin, positions,
+                     rope_len, stream):
+    return load().reqat_kv4_append(_cache_ref(cache), T, slots, k, ldk, v, ldv, q, ldq, q_heads, q_out, ldq_out,
+                                   rope_cos, rope_sin, positions, rope_len, stream)
+
+
+def reqat_kv4_gather(cache, T, slots, k_out, ldk, v_out, ldv, add_shift, stream):
+    return load().reqat_kv4_gather(_cache_ref(cache), T, slots, k_out, ldk, v_out, ldv, add_shift, stream)
+
+
+def reqat_kv4_attention(cache, B, T, q, ldq, q_heads, q_start, kv_len, block_table, ld_table, table_cols, max_q,
+                        max_kv, causal, sm_scale, out, ldo, lse, workspace, stream):
+    return load().reqat_kv4_attention(_cache_ref(cache), B, T, q, ldq, q_heads, q_start, kv_len, block_table, ld_table,
+                                      table_cols, max_q, max_kv, causal, sm_scale, out, ldo, lse, workspace, stream)
+
+
+def reqat_kv4_attention_workspace_bytes(B, T, max_q, max_kv, q_heads, kv_heads, head_dim) -> int:
+    return load().reqat_kv4_attention_workspace_bytes(B, T, max_q, max_kv, q_heads, kv_heads, head_dim)
 
 
 def reqat_gemm_w4a16(M, N, K, x, ldx, w_codes, w_scales, y, y_dtype, ldy, workspace, stream):
@@ -501,6 +538,197 @@ def fakequant_kv4(x: torch.Tensor, shift=None, tensor_scale=None, out=None, g_ou
                              workspace(x.device).data_ptr(), _stream(x.device))
     _check(st, "reqat_fakequant_kv4")
     return y, g
+
+
+class Kv4Cache:
+    """A paged KV4 cache: ``num_pages`` pages of ``page_size`` tokens (a power of two, 16 or more) of ``kv_heads``
+    heads of ``head_dim`` (64 or 128) channels, with the calibrated tensor scales of keys and values and, optionally,
+    the post-RoPE shift of the keys (float32 [kv_heads * head_dim]).
+
+    A scale is a number, or a float32 tensor of one element on the device.  The codes and scales (``k_codes``,
+    ``k_scales``, ``v_codes``, ``v_scales``) have the layout that include/reqat.h states.  Which pages belong to which
+    sequence is the caller's: a slot is page * page_size + the token's place in the page."""
+
+    def __init__(self, num_pages, page_size, kv_heads, head_dim=128, k_scale=1.0, v_scale=1.0, k_shift=None,
+                 device="cuda"):
+        if num_pages < 0 or kv_heads < 1:
+            raise ValueError("num_pages must be >= 0 and kv_heads >= 1")
+        if page_size < 16 or page_size > 1 << 20 or page_size & (page_size - 1):
+            raise ValueError("page_size must be a power of two from 16 to 2^20")
+        if head_dim not in (64, 128):
+            raise ValueError("head_dim must be 64 or 128")
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.num_pages, self.page_size, self.kv_heads, self.head_dim = num_pages, page_size, kv_heads, head_dim
+
+        def scale(g, name):
+            if isinstance(g, torch.Tensor):
+                return _scale_arg(g, NVFP4, self.device, name)
+            if not 0.0 < float(g) < float("inf"):
+                raise ValueError("%s must be positive and finite" % name)
+            return torch.tensor([float(g)], dtype=torch.float32, device=self.device)
+
+        self.k_scale, self.v_scale = scale(k_scale, "k_scale"), scale(v_scale, "v_scale")
+        self.k_shift, _ = _shift_ptr(k_shift, kv_heads * head_dim, self.device)
+        run = num_pages * kv_heads * page_size
+        u8 = dict(dtype=torch.uint8, device=self.device)
+        self.k_codes = torch.zeros(run * head_dim // 2, **u8)
+        self.k_scales = torch.zeros(run * head_dim // 16, **u8)
+        self.v_codes = torch.zeros(run * head_dim // 2, **u8)
+        self.v_scales = torch.zeros(run * head_dim // 16, **u8)
+
+    @property
+    def width(self) -> int:
+        """Channels of a token's keys (or values): kv_heads * head_dim."""
+        return self.kv_heads * self.head_dim
+
+    def struct(self) -> Kv4CacheStruct:
+        return Kv4CacheStruct(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
+                              self.v_scales.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                              _ptr(self.k_shift), self.num_pages, self.page_size, self.kv_heads, self.head_dim)
+
+
+def _cache_arg(cache):
+    if not isinstance(cache, Kv4Cache):
+        raise TypeError("cache must be a Kv4Cache")
+    return cache
+
+
+def _index_arg(t, shape, dtype, device, name):
+    """A contiguous integer tensor that the kernels read on the device."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise TypeError("%s must be a %s tensor" % (name, dtype))
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, shape, tuple(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    _same_device(t, device, name)
+    return t
+
+
+def _rows_arg(x, rows, cols, device, name):
+    """A bfloat16 [rows, cols] input; returns its row stride."""
+    if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16 or x.dim() != 2:
+        raise TypeError("%s must be a 2-D bfloat16 tensor" % name)
+    return _out2d(x, rows, cols, torch.bfloat16, device, name)
+
+
+def kv4_append(cache, k, v, slots, q=None, rope=None, positions=None, q_out=None):
+    """Write T tokens into a Kv4Cache in one pass: keys k and values v (bfloat16 [T, kv_heads * head_dim], rows may
+    be strided) go to ``slots`` (int64 [T]; a slot outside the cache, such as -1, marks padding), keys rotated when
+    ``rope`` = (cos, sin), float32 [P, head_dim / 2], and ``positions`` (int32 [T]) are given, then less the cache's
+    shift.  Queries q [T, q_heads * head_dim] are rotated too; returns them (into q_out when given; q itself is
+    allowed), or None without q."""
+    _cache_arg(cache)
+    dev, D = cache.device, cache.head_dim
+    T = k.shape[0] if isinstance(k, torch.Tensor) and k.dim() == 2 else 0
+    ldk, ldv = _rows_arg(k, T, cache.width, dev, "k"), _rows_arg(v, T, cache.width, dev, "v")
+    _index_arg(slots, (T,), torch.int64, dev, "slots")
+    cos = sin = None
+    rope_len = 0
+    if rope is not None:
+        cos, sin = rope
+        if not isinstance(cos, torch.Tensor) or cos.dim() != 2:
+            raise TypeError("rope must be two float32 tensors [P, head_dim / 2]")
+        rope_len = cos.shape[0]
+        _index_arg(cos, (rope_len, D // 2), torch.float32, dev, "rope cos")
+        _index_arg(sin, (rope_len, D // 2), torch.float32, dev, "rope sin")
+        _index_arg(positions, (T,), torch.int32, dev, "positions")
+    elif positions is not None:
+        raise ValueError("positions without rope")
+    ldq = ldqo = q_heads = 0
+    if q is not None:
+        if rope is None:
+            raise ValueError("queries are rotated: q needs rope and positions")
+        if not isinstance(q, torch.Tensor) or q.dim() != 2 or q.shape[1] == 0 or q.shape[1] % D:
+            raise ValueError("q must be [T, q_heads * head_dim]")
+        q_heads = q.shape[1] // D
+        ldq = _rows_arg(q, T, q.shape[1], dev, "q")
+        if q_out is None:
+            q_out = torch.empty((T, q.shape[1]), dtype=torch.bfloat16, device=dev)
+        ldqo = _out2d(q_out, T, q.shape[1], torch.bfloat16, dev, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _require_cuda(k, "k")
+    cs = cache.struct()
+    st = reqat_kv4_append(cs, T, slots.data_ptr(), k.data_ptr(), ldk, v.data_ptr(), ldv, _ptr(q), ldq, q_heads,
+                          _ptr(q_out), ldqo, _ptr(cos), _ptr(sin), _ptr(positions), rope_len, _stream(dev))
+    _check(st, "reqat_kv4_append")
+    return q_out
+
+
+def kv4_gather(cache, slots, add_shift=False, out=None):
+    """The keys and values that ``slots`` (int64 [T]) of a Kv4Cache hold, as bfloat16 [T, kv_heads * head_dim] each
+    (zeros for a slot outside the cache); keys in the shifted domain, or with the shift added.  out: (k, v)
+    preallocated, rows may be strided."""
+    _cache_arg(cache)
+    if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
+        raise TypeError("slots must be a 1-D int64 tensor")
+    T, dev = slots.shape[0], cache.device
+    _index_arg(slots, (T,), torch.int64, dev, "slots")
+    k, v = out if out is not None else (torch.empty((T, cache.width), dtype=torch.bfloat16, device=dev)
+                                        for _ in range(2))
+    ldk = _out2d(k, T, cache.width, torch.bfloat16, dev, "out[0]")
+    ldv = _out2d(v, T, cache.width, torch.bfloat16, dev, "out[1]")
+    _require_cuda(slots, "slots")
+    cs = cache.struct()
+    st = reqat_kv4_gather(cs, T, slots.data_ptr(), k.data_ptr(), ldk, v.data_ptr(), ldv, 1 if add_shift else 0,
+                          _stream(dev))
+    _check(st, "reqat_kv4_gather")
+    return k, v
+
+
+def kv4_attention(q, cache, block_table, kv_len, q_start=None, max_q=None, max_kv=None, causal=True, sm_scale=None,
+                  out=None, return_lse=False, ws=None):
+    """Attention of the queries of B sequences over their tokens in a Kv4Cache.
+
+    q: bfloat16 [T, q_heads * head_dim] (rows may be strided); block_table: int32 [B, pages of a sequence];
+    kv_len: int32 [B], cached tokens, the new ones included; q_start: int32 [B + 1], the first query row of each
+    sequence, or None: one query each.  max_q and max_kv bound the queries and tokens of every sequence on the host
+    (by default T, 1 without q_start, and what the table can hold); closer bounds launch less.  causal: the queries
+    are the last tokens of their sequence.  sm_scale: default head_dim ** -0.5.  ws: uint8 tensor of
+    reqat_kv4_attention_workspace_bytes(B, T, max_q, max_kv, q_heads, kv_heads, head_dim) bytes.
+    Returns out, bfloat16 like q, or (out, lse) with lse float32 [T, q_heads]."""
+    _cache_arg(cache)
+    dev, D = cache.device, cache.head_dim
+    if not isinstance(q, torch.Tensor) or q.dim() != 2 or q.shape[1] == 0 or q.shape[1] % cache.width:
+        raise ValueError("q must be [T, q_heads * head_dim], q_heads a multiple of kv_heads")
+    T, q_heads = q.shape[0], q.shape[1] // D
+    ldq = _rows_arg(q, T, q.shape[1], dev, "q")
+    if not isinstance(block_table, torch.Tensor) or block_table.dtype != torch.int32 or block_table.dim() != 2:
+        raise TypeError("block_table must be a 2-D int32 tensor")
+    B, cols = block_table.shape
+    if cols > 1 and block_table.stride(1) != 1 or B > 1 and block_table.stride(0) < cols:
+        raise ValueError("block_table rows must be contiguous")
+    ld_table = block_table.stride(0) if B > 1 else cols
+    _same_device(block_table, dev, "block_table")
+    _index_arg(kv_len, (B,), torch.int32, dev, "kv_len")
+    if q_start is not None:
+        _index_arg(q_start, (B + 1,), torch.int32, dev, "q_start")
+    elif T != B:
+        raise ValueError("without q_start there is one query per sequence")
+    if max_q is None:
+        max_q = T if q_start is not None else 1
+    if max_kv is None:
+        max_kv = min(cols * cache.page_size, 0x7FFFFFFF)
+    if sm_scale is None:
+        sm_scale = D ** -0.5
+    y = out if out is not None else torch.empty((T, q.shape[1]), dtype=torch.bfloat16, device=dev)
+    ldo = _out2d(y, T, q.shape[1], torch.bfloat16, dev, "out")
+    lse = torch.empty((T, q_heads), dtype=torch.float32, device=dev) if return_lse else None
+    need = reqat_kv4_attention_workspace_bytes(B, T, max_q, max_kv, q_heads, cache.kv_heads, D)
+    if ws is not None:
+        _workspace_arg(ws, need, dev)
+    _require_cuda(q, "q")
+    if ws is None and need > 0:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    cs = cache.struct()
+    st = reqat_kv4_attention(cs, B, T, q.data_ptr(), ldq, q_heads, _ptr(q_start), kv_len.data_ptr(),
+                             block_table.data_ptr(), ld_table, cols, max_q, max_kv, 1 if causal else 0, sm_scale,
+                             y.data_ptr(), ldo, _ptr(lse), _ptr(ws) if need > 0 else None, _stream(dev))
+    _check(st, "reqat_kv4_attention")
+    return (y, lse) if return_lse else y
 
 
 def gemm_w4a16(x: torch.Tensor, w_codes, w_scales, out_dtype=torch.float32, out=None, ws=None):
