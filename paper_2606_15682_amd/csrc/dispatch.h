@@ -258,4 +258,28 @@ inline int pick_w4a16(int64_t M, int64_t N, int64_t K, int64_t ldx) {
     return tile < 0 && w4a16_decode_pays(M, N, K) ? kW16Decode : tile;
 }
 
+// ---------------------------------------------------------------- attention over the KV4 cache
+
+// How a call is cut: rows (queries x heads of a group) into qtiles of 16 x tiles, tokens into splits of `chunk`.
+struct Kv4Plan {
+    int tiles, qtiles, splits, chunk;
+};
+
+inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads) {
+    Kv4Plan p;
+    const int64_t rows = max_q * (q_heads / kv_heads);
+    p.tiles = rows > 16 ? 2 : 1;
+    p.qtiles = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
+    const int64_t groups = B * kv_heads * p.qtiles;
+    int64_t splits = groups > 0 ? (1024 + groups - 1) / groups : 1;
+    const int64_t most = (max_kv + 255) / 256;
+    splits = splits > most ? most : splits;
+    splits = splits < 1 ? 1 : splits;
+    const int64_t chunk = ((max_kv + splits - 1) / splits + 127) / 128 * 128;
+    p.chunk = (int)(chunk < 128 ? 128 : chunk > 0x7FFFFF80 ? 0x7FFFFF80 : chunk);
+    p.splits = (int)((max_kv + p.chunk - 1) / p.chunk);
+    if (p.splits < 1) p.splits = 1;
+    return p;
+}
+
 }  // namespace reqat

@@ -1,105 +1,495 @@
 // Attention over the paged 4-bit cache (W4A4KV4 serving, Sec. 4.3; layout in kv4_cache.h):
-//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i . k_j - max),  j over the row's visible tokens.
+//   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i . k_j - m_i),  j over the row's visible tokens.
 // The shift of the keys is left out of the scores: q . m is the same for every key of a row,
 // and a softmax does not change when its scores all move by as much.
 //
-// The simple kernel: one wave per query and head; 64 tokens a step, one lane each for the scores,
-// then D / 64 channels a lane for the values.
-#include "internal.h"
+// Arithmetic.  A code times its block scale has at most 7 significant bits, so keys and values are exact
+// in FP16: a code's half word, sign at bit 15 and magnitude n at bits 6:4, is n 2^-20; the E4M3 scale
+// enters as s 2^7 (<= 57344), and the product n s 2^-13 is a multiple of 2^-22.  A query row takes a
+// power-of-two factor that puts its largest value into [2^14, 2^15), so that its bfloat16 values are FP16
+// numbers (those below 2^-28 of the largest are rounded, to 2^-39 of it).  The scores sum in FP32.  Weights p =
+// 2^(s - r) are rounded to FP16 (11 bits, 3 more than the output has): r trails the running maximum,
+// at least 7 and at most 15 below it, so p is at most 2^15 and the FP16 range reaches 2^-31 of the largest
+// weight or below; the sum of weights is taken in FP32 before that rounding.
 #include "fp4_device.h"
+#include "internal.h"
 
 namespace reqat {
 
 namespace {
 
-__device__ __forceinline__ float code_value(uint32_t c) {
-    const float m = 0.5f * (float)(c & 7u);
-    return (c & 8u) ? -m : m;
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr uint32_t kCodeMask = 0x80708070u;    // sign and magnitude of a code in either half word
+constexpr float kScaleUp = 128.0f;             // FP16 scales are s 2^7
+constexpr float kBelow = 7.0f, kSlack = 8.0f;  // r = maximum - kBelow, renewed when the maximum has grown by kSlack
+constexpr float kLowest = -3.4028234663852886e38f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ uint32_t scaled(uint32_t code_bits, h2 s) {
+    return __builtin_bit_cast(uint32_t, (h2)(__builtin_bit_cast(h2, code_bits) * s));
 }
 
-template <int D>
-__global__ __launch_bounds__(64) void kv4_attention_simple_kernel(const Kv4AttnArgs a) {
-    const int i = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, lane = threadIdx.x;
+__device__ __forceinline__ h8 frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_bit_cast(h8, make_uint4(a, b, c, d));
+}
+
+// Maximum (sum) over the four lanes that share lane % 16.
+__device__ __forceinline__ float max16(float x) {
+    x = __builtin_fmaxf(x, __shfl_xor(x, 16, 64));
+    return __builtin_fmaxf(x, __shfl_xor(x, 32, 64));
+}
+__device__ __forceinline__ float sum16(float x) {
+    x += __shfl_xor(x, 16, 64);
+    return x + __shfl_xor(x, 32, 64);
+}
+
+// The queries and tokens of sequence b.
+struct Seq {
+    int64_t q0;          // first query row
+    int nq;              // queries
+    int len;             // cached tokens
+    bool lost;           // more tokens than the caller's bounds or the table hold: NaN
+};
+
+__device__ __forceinline__ Seq sequence(const Kv4AttnArgs &a, int b) {
+    Seq s;
     int64_t q0 = b, q1 = b + 1;
     if (a.q_start) {
-        q0 = a.q_start[b] < 0 ? 0 : a.q_start[b];
-        q1 = a.q_start[b + 1] > a.T ? a.T : a.q_start[b + 1];
+        q0 = a.q_start[b];
+        q1 = a.q_start[b + 1];
+        q0 = q0 < 0 ? 0 : q0;
+        q1 = q1 > a.T ? a.T : q1;
     }
-    if (q0 + i >= q1) return;
-    const int64_t row = q0 + i, nq = q1 - q0;
-    const int64_t len = a.kv_len[b] < 0 ? 0 : a.kv_len[b];
-    const bool lost = len > a.max_kv || len > (a.table_cols << a.c.page_log2);
-    int64_t n = a.causal ? len - nq + i + 1 : len;
-    if (n < 0) n = 0;
-    const int h = hq / (a.q_heads / a.c.heads);
-    __shared__ float q[D], p[64];
-    for (int d = lane; d < D; d += 64) q[d] = f32_from_bits((uint32_t)a.q[row * a.ldq + hq * D + d] << 16);
-    __syncthreads();
-    float top = -__builtin_inff(), total = 0.0f, o[D / 64] = {};
-    for (int64_t j0 = 0; j0 < n && !lost; j0 += 64) {
-        const int64_t j = j0 + lane;
-        float s = -__builtin_inff();
-        if (j < n) {
-            const int64_t page = a.table[b * a.ld_table + (j >> a.c.page_log2)];
-            s = __builtin_nanf("");
-            if (page >= 0 && page < a.c.pages) {
-                const int tok = (int)(j & ((1 << a.c.page_log2) - 1));
-                const int64_t run = a.c.run(page, h);
-                s = 0.0f;
-                for (int g = 0; g < D / 16; ++g) {
-                    float t = 0.0f;
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t w = a.c.kc[kv4_k_codes(run, tok, D) + 8 * g + e];
-                        t += q[16 * g + 2 * e] * code_value(w & 15u) + q[16 * g + 2 * e + 1] * code_value(w >> 4);
-                    }
-                    s += t * e4m3_value(a.c.ks[kv4_k_scales(run, tok, D) + g]);
+    s.q0 = q0;
+    s.nq = (int)(q1 > q0 ? q1 - q0 : 0);
+    s.len = a.kv_len[b] < 0 ? 0 : a.kv_len[b];
+    s.lost = s.len > a.max_kv || s.len > (a.table_cols << a.c.page_log2) || (s.len > 0 && a.c.pages == 0);
+    return s;
+}
+
+// Tokens that query i of the sequence sees: 0 .. visible - 1.
+__device__ __forceinline__ int visible(const Kv4AttnArgs &a, const Seq &s, int i) {
+    const int n = a.causal ? s.len - s.nq + i + 1 : s.len;
+    return n < 0 ? 0 : n;
+}
+
+// ------------------------------------------------------------------ few queries
+
+// A wave takes 32 tokens a step against 16 NT rows (query, head of the KV head's group), alone: codes go
+// from memory to registers in the matrix cores' operand layout, and nothing is shared until the end.
+//   S^T = K Q^T  (16 tokens x 16 rows, K = 32 channels): lane (r, g) = (lane % 16, lane / 16) holds token r, channels
+//     D/4 g ..; it gets the scores of row r and tokens 4 g .. 4 g + 3, twice.
+//   O^T = V^T P^T (16 channels x 16 rows, K = 32 tokens): those eight tokens are its share of the K axis, so the weights
+//     are the operand as they stand, and the cache holds the values of four tokens together.  Tile c has channels
+//     8 w + c of the dwords w.
+template <int D> struct Step {
+    uint32_t k[2][D / 32], ks[2];
+    uint32_t v[2][4], vs[2];
+};
+
+template <int D, int NT, int W>
+__global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a, int qtiles, int splits, int chunk) {
+    constexpr int KW = D / 32, VT = D / 16;
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int id = blockIdx.x;
+    const int qt = id % qtiles;
+    id /= qtiles;
+    const int split = id % splits;
+    id /= splits;
+    const int h = id % a.c.heads, b = id / a.c.heads;
+    const int group = a.q_heads / a.c.heads;
+
+    const Seq sq = sequence(a, b);
+    const int nq = sq.nq < a.max_q ? sq.nq : (int)a.max_q;
+    const int rows = nq * group, row0 = qt * 16 * NT;
+    if (row0 >= rows) return;
+    const int row_last = row0 + 16 * NT < rows ? row0 + 16 * NT - 1 : rows - 1;
+    const int see_least = visible(a, sq, row0 / group), see_most = visible(a, sq, row_last / group);
+    const int t0 = split * chunk;
+    const int t1 = sq.lost ? 0 : see_most < t0 + chunk ? see_most : t0 + chunk;   // this workgroup's tokens
+    if (split > 0 && t0 >= t1) return;                                            // the join does not read it
+
+    // queries, the factor from scores to exponents, and what each row sees
+    h8 qf[NT][KW];
+    float c[NT], ref[NT], sum[NT];
+    int see[NT];
+    const float gk = *a.c.gk;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = row0 + 16 * n + r;
+        const bool there = row < rows;
+        const int i = there ? row / group : 0;
+        see[n] = there ? visible(a, sq, i) : 0;
+        uint32_t w[4 * KW];
+        const uint16_t *src = a.q + (sq.q0 + i) * a.ldq + (int64_t)(h * group + (there ? row - i * group : 0)) * D + (D / 4) * g;
+#pragma unroll
+        for (int j = 0; j < KW; ++j) {
+            const uint4 x = there ? reinterpret_cast<const uint4 *>(src)[j] : make_uint4(0, 0, 0, 0);
+            w[4 * j] = x.x;
+            w[4 * j + 1] = x.y;
+            w[4 * j + 2] = x.z;
+            w[4 * j + 3] = x.w;
+        }
+        float top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4 * KW; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t m = (e ? w[j] & 0x7FFF0000u : (w[j] << 16) & 0x7FFF0000u);
+                top = m < 0x7F800000u ? __builtin_fmaxf(top, f32_from_bits(m)) : top;
+            }
+        top = max16(top);
+        const int up = top > 0.0f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
+        // channels of a dword of codes in the order that kcodes() unpacks them: 0 2 1 3 4 6 5 7
+#pragma unroll
+        for (int j = 0; j < KW; ++j) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[2 * e] = __builtin_ldexpf(f32_from_bits(w[4 * j + e] << 16), up);
+                x[2 * e + 1] = __builtin_ldexpf(f32_from_bits(w[4 * j + e] & 0xFFFF0000u), up);
+            }
+            const h8 y = {(_Float16)x[0], (_Float16)x[2], (_Float16)x[1], (_Float16)x[3],
+                          (_Float16)x[4], (_Float16)x[6], (_Float16)x[5], (_Float16)x[7]};
+            qf[n][j] = y;
+        }
+        // a code is half its integer: 2^-13 n s = 2^-12 (n / 2) s
+        c[n] = __builtin_fmaxf(__builtin_ldexpf(a.scale * kLog2e * gk * 4096.0f, -up), 0x1p-126f);
+        ref[n] = kLowest;
+        sum[n] = 0.0f;
+    }
+
+    f32x4 o[VT][NT];
+#pragma unroll
+    for (int x = 0; x < VT; ++x)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[x][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const int *table = a.table + (int64_t)b * a.ld_table;
+    const int plog = a.c.page_log2, pmask = (1 << plog) - 1;
+    const uint32_t w_at = D == 128 ? r : r & 7;                        // the lane's dword of value codes
+    const uint32_t k_at = r * (D / 2) + g * (D / 8), ks_at = r * (D / 16) + g * (D / 64);
+    const uint32_t v_at = g * (2 * D) + w_at * 16, vs_at = g * (D / 4) + (w_at >> 1) * 4;
+    // D = 64: sixteen rows of a tile are eight dwords times two: lanes 8 .. 15 take the dword's upper channels
+    const uint32_t half = D == 128 ? 0u : (uint32_t)(r >> 3) * 0x02020202u;
+
+    auto pages = [&](int t, int (&p)[2]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) p[u] = t + 16 * u < t1 ? __builtin_amdgcn_readfirstlane(table[(t + 16 * u) >> plog]) : 0;
+    };
+    auto load = [&](int t, const int (&p)[2], Step<D> &st) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const bool in = p[u] >= 0 && p[u] < a.c.pages;             // uniform
+            const int tok = (t + 16 * u) & pmask;
+            const int64_t run = a.c.run(in ? p[u] : 0, h) + tok;      // tokens (values: a multiple of 4 of them)
+            const uint8_t *kp = a.c.kc + run * (D / 2) + k_at, *vp = a.c.vc + run * (D / 2) + v_at;
+            if constexpr (D == 128) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(kp);
+                st.k[u][0] = x.x;
+                st.k[u][1] = x.y;
+                st.k[u][2] = x.z;
+                st.k[u][3] = x.w;
+                st.ks[u] = *reinterpret_cast<const uint16_t *>(a.c.ks + run * (D / 16) + ks_at);
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(kp);
+                st.k[u][0] = x.x;
+                st.k[u][1] = x.y;
+                st.ks[u] = a.c.ks[run * (D / 16) + ks_at];
+            }
+            const uint4 y = *reinterpret_cast<const uint4 *>(vp);
+            st.v[u][0] = y.x;
+            st.v[u][1] = y.y;
+            st.v[u][2] = y.z;
+            st.v[u][3] = y.w;
+            st.vs[u] = *reinterpret_cast<const uint32_t *>(a.c.vs + run * (D / 16) + vs_at);
+            if (!in) {                                                 // nothing of it is used
+                st.ks[u] = 0x7F7Fu;
+                st.vs[u] = 0u;
+            }
+        }
+    };
+
+    auto compute = [&](int t, Step<D> &st) {
+        f32x4 s[2][NT];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const h2 sc = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(st.ks[u], kScaleUp, false);
+            const h2 sc0 = {sc[0], sc[0]}, sc1 = {sc[1], sc[1]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[u][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < KW; ++j) {
+                const h2 sj = j < 2 ? sc0 : sc1;
+                const uint32_t x = __builtin_amdgcn_perm(st.k[u][j], st.k[u][j], 0x01010000u);
+                const uint32_t y = __builtin_amdgcn_perm(st.k[u][j], st.k[u][j], 0x03030202u);
+                const h8 kf = frag(scaled((x << 4) & kCodeMask, sj), scaled(x & kCodeMask, sj),
+                                   scaled((y << 4) & kCodeMask, sj), scaled(y & kCodeMask, sj));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][j], s[u][n], 0, 0, 0);
+            }
+        }
+        int bad_at = 0x7FFFFFFF;                                       // first NaN value of the lane's block that some row does not see
+        const bool edge = t + 32 > see_least;                          // uniform
+        if (edge) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (t + 16 * u + 4 * g + i >= see[n]) s[u][n][i] = -__builtin_inff();
+            // a hidden value must not reach a row: 0 NaN is NaN.  Beyond every row a scale becomes 0, and so does a
+            // NaN scale, whose NaN is put back below into the rows that see it.
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = t + 16 * u + 4 * g + i;
+                    const bool nan = ((st.vs[u] >> (8 * i)) & 0x7Fu) == 0x7Fu;
+                    if (at >= t1 || nan) st.vs[u] &= ~(0xFFu << (8 * i));
+                    if (at < t1 && nan) bad_at = bad_at < at ? bad_at : at;
                 }
-                s *= a.scale * *a.c.gk;
+        }
+        uint32_t p[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float top = s[0][n][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = __builtin_fmaxf(top, s[i >> 2][n][i & 3]);
+            if (__any(__builtin_fmaf(top, c[n], -ref[n]) > kBelow + kSlack)) {
+                const float m = max16(top) * c[n] - kBelow;
+                const float next = __builtin_fmaxf(m, ref[n]);
+                const float f = __builtin_amdgcn_exp2f(ref[n] - next);
+                ref[n] = next;
+                sum[n] *= f;
+#pragma unroll
+                for (int x = 0; x < VT; ++x)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[x][n][i] *= f;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float e[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][n][i], c[n], -ref[n]));
+                sum[n] += (e[0] + e[1]) + (e[2] + e[3]);
+                const h2 lo = {(_Float16)e[0], (_Float16)e[1]}, hi = {(_Float16)e[2], (_Float16)e[3]};
+                p[n][2 * u] = __builtin_bit_cast(uint32_t, lo);
+                p[n][2 * u + 1] = __builtin_bit_cast(uint32_t, hi);
             }
         }
-        float m = s;
-        for (int off = 32; off > 0; off >>= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, off, 64));
-        const float next = __builtin_elementwise_maximum(m, top);
-        const float keep = top == -__builtin_inff() ? 0.0f : __expf(top - next);
-        const float w = j < n ? __expf(s - next) : 0.0f;
-        float sum = w;
-        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-        total = total * keep + sum;
-        top = next;
-        __syncthreads();
-        p[lane] = w;
-        __syncthreads();
-        for (int e = 0; e < D / 64; ++e) {
-            const int d = lane * (D / 64) + e;
-            float acc = 0.0f;
-            for (int u = 0; u < 64 && j0 + u < n; ++u) {
-                const int64_t page = a.table[b * a.ld_table + ((j0 + u) >> a.c.page_log2)];
-                if (page < 0 || page >= a.c.pages) continue;
-                const int tok = (int)((j0 + u) & ((1 << a.c.page_log2) - 1));
-                const int64_t run = a.c.run(page, h);
-                const uint32_t byte = a.c.vc[kv4_v_codes(run, tok, d / 16, D) + (d % 16 / 8) * 16 + d % 8 / 2];
-                acc += p[u] * (code_value((d & 1) ? byte >> 4 : byte & 15u) * e4m3_value(a.c.vs[kv4_v_scales(run, tok, d / 16, D)]));
+        h2 sv[2][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            sv[u][0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(st.vs[u], kScaleUp, false);
+            sv[u][1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(st.vs[u], kScaleUp, true);
+        }
+#pragma unroll
+        for (int j = 0; j < VT / 2; ++j) {
+            uint32_t x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                x[i] = __builtin_amdgcn_perm(st.v[i >> 1][2 * (i & 1) + 1], st.v[i >> 1][2 * (i & 1)],
+                                             0x04040000u + 0x01010101u * j + half);
+            const h8 even = frag(scaled((x[0] << 4) & kCodeMask, sv[0][0]), scaled((x[1] << 4) & kCodeMask, sv[0][1]),
+                                 scaled((x[2] << 4) & kCodeMask, sv[1][0]), scaled((x[3] << 4) & kCodeMask, sv[1][1]));
+            const h8 odd = frag(scaled(x[0] & kCodeMask, sv[0][0]), scaled(x[1] & kCodeMask, sv[0][1]),
+                                scaled(x[2] & kCodeMask, sv[1][0]), scaled(x[3] & kCodeMask, sv[1][1]));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const h8 pf = frag(p[n][0], p[n][1], p[n][2], p[n][3]);
+                o[2 * j][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, pf, o[2 * j][n], 0, 0, 0);
+                o[2 * j + 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, pf, o[2 * j + 1][n], 0, 0, 0);
             }
-            o[e] = o[e] * keep + acc;
+        }
+        if (edge && __any(bad_at != 0x7FFFFFFF)) {
+            // the block's first NaN over its tokens; lane (r, g) holds channels of the dwords 4 g .. 4 g + 3
+            int x = __shfl_xor(bad_at, 16, 64);
+            bad_at = bad_at < x ? bad_at : x;
+            x = __shfl_xor(bad_at, 32, 64);
+            bad_at = bad_at < x ? bad_at : x;
+            const int first = __shfl(bad_at, 4 * g, 64), second = __shfl(bad_at, 4 * g + 2, 64);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int x = 0; x < VT; ++x)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if ((i < 2 ? first : second) < see[n]) o[x][n][i] = __builtin_nanf("");
+        }
+    };
+
+    constexpr int kStride = 32 * W;
+    int t = t0 + 32 * wave;
+    if (t < t1) {
+        Step<D> A, B;
+        int p[2];
+        pages(t, p);
+        load(t, p, A);
+        pages(t + kStride, p);
+        while (true) {
+            if (t + kStride < t1) load(t + kStride, p, B);
+            pages(t + 2 * kStride, p);
+            compute(t, A);
+            t += kStride;
+            if (t >= t1) break;
+            if (t + kStride < t1) load(t + kStride, p, A);
+            pages(t + 2 * kStride, p);
+            compute(t, B);
+            t += kStride;
+            if (t >= t1) break;
         }
     }
-    const float inv = n == 0 && !lost ? 0.0f : *a.c.gv / total;
-    for (int e = 0; e < D / 64; ++e) {
-        const float y = lost ? __builtin_nanf("") : n == 0 ? 0.0f : o[e] * inv;
-        a.out[row * a.ldo + hq * D + lane * (D / 64) + e] = (uint16_t)bf16_rne_from_float(y);
+
+    // join the waves: references and sums first, then the rows through LDS
+    constexpr int kLd = D + 4;
+    __shared__ float part[W][16][kLd];
+    __shared__ float refs[W][16 * NT], sums[W][16 * NT];
+    const float gv = *a.c.gv * 4096.0f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        sum[n] = sum16(sum[n]);
+        if (g == 0) {
+            refs[wave][16 * n + r] = ref[n];
+            sums[wave][16 * n + r] = sum[n];
+        }
     }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float m = kLowest;
+        for (int w = 0; w < W; ++w) m = __builtin_fmaxf(m, refs[w][16 * n + r]);
+        const float f = __builtin_amdgcn_exp2f(ref[n] - m);
+        if (n > 0) __syncthreads();
+#pragma unroll
+        for (int x = 0; x < VT; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int rho = 4 * g + i;
+                const int ch = D == 128 ? 8 * rho + x : 8 * (rho & 7) + 4 * (rho >> 3) + x;
+                part[wave][r][ch] = o[x][n][i] * f;
+            }
+        __syncthreads();
+        const int have = rows - row0 - 16 * n;
+        for (int x = threadIdx.x; x < (have < 16 ? have : 16) * D; x += 64 * W) {
+            const int rr = x / D, ch = x % D;
+            float top = kLowest;
+            for (int w = 0; w < W; ++w) top = __builtin_fmaxf(top, refs[w][16 * n + rr]);
+            float total = 0.0f, y = 0.0f;
+            for (int w = 0; w < W; ++w) {
+                total = __builtin_fmaf(sums[w][16 * n + rr], __builtin_amdgcn_exp2f(refs[w][16 * n + rr] - top), total);
+                y += part[w][rr][ch];
+            }
+            const int row = row0 + 16 * n + rr, i = row / group;
+            const int64_t at = (sq.q0 + i) * a.q_heads + h * group + (row - i * group);
+            if (splits > 1) {
+                float *po = reinterpret_cast<float *>(a.workspace);
+                float *pm = po + (int64_t)splits * a.T * a.q_heads * D;
+                const int64_t slot = (int64_t)split * a.T * a.q_heads + at;
+                po[slot * D + ch] = y;
+                if (ch == 0) {
+                    pm[2 * slot] = top;
+                    pm[2 * slot + 1] = total;
+                }
+            } else {
+                const bool none = visible(a, sq, i) == 0 && !sq.lost;
+                const float out = sq.lost ? __builtin_nanf("") : none ? 0.0f : y * gv / total;
+                a.out[(sq.q0 + i) * a.ldo + (int64_t)(h * group + (row - i * group)) * D + ch] = (uint16_t)bf16_rne_from_float(out);
+                if (a.lse && ch == 0)
+                    a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (top + __builtin_log2f(total)) * kLn2;
+            }
+        }
+    }
+}
+
+// Joins the splits of a row: one workgroup of W waves per query and head, the waves take the splits in turn.
+template <int D, int W>
+__global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, int splits, int chunk) {
+    constexpr int C = D / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int hq = blockIdx.x % a.q_heads;
+    const int64_t bi = blockIdx.x / a.q_heads;
+    const int i = (int)(bi % a.max_q), b = (int)(bi / a.max_q);
+    const Seq sq = sequence(a, b);
+    if (i >= sq.nq) return;
+    const int n = visible(a, sq, i);
+    // the splits that a workgroup of the row's tile has written: those before the last token that the row sees
+    const int have = sq.lost ? 0 : (n + chunk - 1) / chunk;
+    const int64_t at = (sq.q0 + i) * a.q_heads + hq, all = a.T * a.q_heads;
+    const float *po = reinterpret_cast<const float *>(a.workspace);
+    const float *pm = po + (int64_t)splits * all * D;
+    float m = kLowest;
+    for (int s = lane; s < have; s += 64) m = __builtin_fmaxf(m, pm[2 * (s * all + at)]);
+    for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off, 64));
+    float total = 0.0f, y[C] = {};
+#pragma unroll 8
+    for (int s = wave; s < have; s += W) {
+        const int64_t slot = s * all + at;
+        const float f = __builtin_amdgcn_exp2f(pm[2 * slot] - m);
+        total = __builtin_fmaf(pm[2 * slot + 1], f, total);
+#pragma unroll
+        for (int e = 0; e < C; ++e) y[e] = __builtin_fmaf(po[slot * D + lane * C + e], f, y[e]);
+    }
+    if constexpr (W > 1) {
+        __shared__ float part[W][C + 1][64];
+#pragma unroll
+        for (int e = 0; e < C; ++e) part[wave][e][lane] = y[e];
+        part[wave][C][lane] = total;
+        __syncthreads();
+        if (wave > 0) return;
+        for (int w = 1; w < W; ++w) {
+#pragma unroll
+            for (int e = 0; e < C; ++e) y[e] += part[w][e][lane];
+            total += part[w][C][lane];
+        }
+    }
+    const float gv = *a.c.gv * 4096.0f;
+    const bool none = n == 0 && !sq.lost;
+    uint32_t bits[C];
+#pragma unroll
+    for (int e = 0; e < C; ++e)
+        bits[e] = bf16_rne_from_float(sq.lost ? __builtin_nanf("") : none ? 0.0f : y[e] * gv / total);
+    uint16_t *dst = a.out + (sq.q0 + i) * a.ldo + (int64_t)hq * D + lane * C;
+    if constexpr (C == 2) *reinterpret_cast<uint32_t *>(dst) = bits[0] | (bits[1] << 16);
+    else dst[0] = (uint16_t)bits[0];
     if (a.lse && lane == 0)
-        a.lse[row * a.q_heads + hq] = lost ? __builtin_nanf("") : n == 0 ? -__builtin_inff() : top + __logf(total);
+        a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (m + __builtin_log2f(total)) * kLn2;
+}
+
+template <int D, int NT, int W> void decode(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
+    const int64_t n = a.B * a.c.heads * p.splits * p.qtiles;
+    kv4_decode_kernel<D, NT, W><<<(unsigned)n, 64 * W, 0, stream>>>(a, p.qtiles, p.splits, p.chunk);
+}
+
+template <int D> void join(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
+    const unsigned n = (unsigned)(a.B * a.max_q * a.q_heads);
+    if (p.splits <= 8) kv4_join_kernel<D, 1><<<n, 64, 0, stream>>>(a, p.splits, p.chunk);
+    else if (p.splits <= 32) kv4_join_kernel<D, 4><<<n, 256, 0, stream>>>(a, p.splits, p.chunk);
+    else kv4_join_kernel<D, 8><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
+}
+
+template <int D> void attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
+    if (p.tiles == 1) decode<D, 1, 4>(a, p, stream);
+    else decode<D, 2, 4>(a, p, stream);
+    if (p.splits > 1) join<D>(a, p, stream);
 }
 
 }  // namespace
 
-size_t kv4_attention_workspace_bytes(int64_t, int64_t, int64_t, int64_t, int, int, int) { return 0; }
+size_t kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads, int D) {
+    const Kv4Plan p = kv4_plan(B, max_q, max_kv, q_heads, kv_heads);
+    return p.splits > 1 ? (size_t)p.splits * (size_t)T * (size_t)q_heads * (size_t)(D + 2) * 4 : 0;
+}
 
 hipError_t launch_kv4_attention(const Kv4AttnArgs &a, hipStream_t stream) {
-    const dim3 grid((unsigned)a.max_q, (unsigned)a.q_heads, (unsigned)a.B);
-    if (a.c.D == 128) kv4_attention_simple_kernel<128><<<grid, 64, 0, stream>>>(a);
-    else kv4_attention_simple_kernel<64><<<grid, 64, 0, stream>>>(a);
+    const Kv4Plan p = kv4_plan(a.B, a.max_q, a.max_kv, a.q_heads, a.c.heads);
+    if (a.c.D == 128) attend<128>(a, p, stream);
+    else attend<64>(a, p, stream);
     return hipGetLastError();
 }
 
