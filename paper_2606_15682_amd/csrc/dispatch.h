@@ -268,10 +268,11 @@ struct Kv4Plan {
 inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads) {
     Kv4Plan p;
     const int64_t rows = max_q * (q_heads / kv_heads);
-    p.tiles = rows > 16 ? 2 : 1;
+    p.tiles = rows > 32 ? 16 : rows > 16 ? 2 : 1;
     p.qtiles = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
     const int64_t groups = B * kv_heads * p.qtiles;
-    int64_t splits = groups > 0 ? (1024 + groups - 1) / groups : 1;
+    const int64_t want = p.tiles == 16 ? 256 : 1024;
+    int64_t splits = groups > 0 ? (want + groups - 1) / groups : 1;
     const int64_t most = (max_kv + 255) / 256;
     splits = splits > most ? most : splits;
     splits = splits < 1 ? 1 : splits;

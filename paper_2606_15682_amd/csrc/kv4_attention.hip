@@ -21,10 +21,12 @@ namespace {
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kCodeMask = 0x80708070u;    // sign and magnitude of a code in either half word
 constexpr float kScaleUp = 128.0f;             // FP16 scales are s 2^7
 constexpr float kBelow = 7.0f, kSlack = 8.0f;  // r = maximum - kBelow, renewed when the maximum has grown by kSlack
+constexpr int kNoToken = 0x7FFFFFFF;
 constexpr float kLowest = -3.4028234663852886e38f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -177,6 +179,8 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
     // D = 64: sixteen rows of a tile are eight dwords times two: lanes 8 .. 15 take the dword's upper channels
     const uint32_t half = D == 128 ? 0u : (uint32_t)(r >> 3) * 0x02020202u;
 
+    int bad_at = kNoToken;               // the first token, some rows not seeing it, whose values in the lane's block are NaN
+
     auto pages = [&](int t, int (&p)[2]) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) p[u] = t + 16 * u < t1 ? __builtin_amdgcn_readfirstlane(table[(t + 16 * u) >> plog]) : 0;
@@ -233,7 +237,6 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
                 for (int n = 0; n < NT; ++n) s[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][j], s[u][n], 0, 0, 0);
             }
         }
-        int bad_at = 0x7FFFFFFF;                                       // first NaN value of the lane's block that some row does not see
         const bool edge = t + 32 > see_least;                          // uniform
         if (edge) {
 #pragma unroll
@@ -244,7 +247,7 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
                     for (int i = 0; i < 4; ++i)
                         if (t + 16 * u + 4 * g + i >= see[n]) s[u][n][i] = -__builtin_inff();
             // a hidden value must not reach a row: 0 NaN is NaN.  Beyond every row a scale becomes 0, and so does a
-            // NaN scale, whose NaN is put back below into the rows that see it.
+            // NaN scale, whose NaN is put back at the end into the rows that see it.
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -262,8 +265,8 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
 #pragma unroll
             for (int i = 1; i < 8; ++i) top = __builtin_fmaxf(top, s[i >> 2][n][i & 3]);
             if (__any(__builtin_fmaf(top, c[n], -ref[n]) > kBelow + kSlack)) {
-                const float m = max16(top) * c[n] - kBelow;
-                const float next = __builtin_fmaxf(m, ref[n]);
+                const float m = max16(top);                            // a row moves by its own scores alone
+                const float next = __builtin_fmaf(m, c[n], -ref[n]) > kBelow + kSlack ? m * c[n] - kBelow : ref[n];
                 const float f = __builtin_amdgcn_exp2f(ref[n] - next);
                 ref[n] = next;
                 sum[n] *= f;
@@ -307,21 +310,6 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
                 o[2 * j + 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, pf, o[2 * j + 1][n], 0, 0, 0);
             }
         }
-        if (edge && __any(bad_at != 0x7FFFFFFF)) {
-            // the block's first NaN over its tokens; lane (r, g) holds channels of the dwords 4 g .. 4 g + 3
-            int x = __shfl_xor(bad_at, 16, 64);
-            bad_at = bad_at < x ? bad_at : x;
-            x = __shfl_xor(bad_at, 32, 64);
-            bad_at = bad_at < x ? bad_at : x;
-            const int first = __shfl(bad_at, 4 * g, 64), second = __shfl(bad_at, 4 * g + 2, 64);
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int x = 0; x < VT; ++x)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if ((i < 2 ? first : second) < see[n]) o[x][n][i] = __builtin_nanf("");
-        }
     };
 
     constexpr int kStride = 32 * W;
@@ -344,6 +332,23 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
             t += kStride;
             if (t >= t1) break;
         }
+    }
+
+    if (__any(bad_at != kNoToken)) {
+        // over all tokens of the block; lane (r, g) holds channels of the dwords 4 g .. 4 g + 3.  What a row
+        // sees is a prefix: it sees a NaN if it sees the first.
+        int x = __shfl_xor(bad_at, 16, 64);
+        bad_at = bad_at < x ? bad_at : x;
+        x = __shfl_xor(bad_at, 32, 64);
+        bad_at = bad_at < x ? bad_at : x;
+        const int first = __shfl(bad_at, 4 * g, 64), second = __shfl(bad_at, 4 * g + 2, 64);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int x = 0; x < VT; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if ((i < 2 ? first : second) < see[n]) o[x][n][i] = __builtin_nanf("");
     }
 
     // join the waves: references and sums first, then the rows through LDS
@@ -404,6 +409,338 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
                     a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (top + __builtin_log2f(total)) * kLn2;
             }
         }
+    }
+}
+
+// ------------------------------------------------------------------ prompts
+
+// A workgroup of four waves takes 256 rows, 64 a wave, and 32 tokens a step.  The codes of a step become FP16
+// once, in LDS, in the order of the matrix cores' operands (two waves the keys, two the values, two steps ahead;
+// their codes are loaded three steps ahead), and every wave reads them from there:
+//   S^T = K Q^T  (32 tokens x 32 rows, K = 16 channels): lane (c, u) = (lane % 32, lane / 32) gets the scores of row c
+//     and tokens 8 x + 4 u .. 8 x + 4 u + 3.
+//   O^T = V^T P^T (32 channels x 32 rows, K = 16 tokens): eight of those, two groups of four, are its K share.
+// 64 rows a wave read an operand of 1 KB from LDS for two products of 32 cycles; 32 rows would need all of
+// the LDS bandwidth.  The scores of a step are computed beside the weights of the one before.
+template <int D> struct Tile {
+    static constexpr int KF = D / 16, VF = D / 16;       // operands of keys; of values (D / 32 tiles of channels x 2)
+    static constexpr int kBytes = (KF + VF) * 1024;
+    static constexpr int kRing = 4;
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 1) void kv4_prompt_kernel(const Kv4AttnArgs a, int qtiles, int splits, int chunk) {
+    using C = Tile<D>;
+    constexpr int NC = 2, VT = D / 32, WD = D / 8, CPT = 32 / WD, kRows = 256;
+    __shared__ __attribute__((aligned(16))) uint8_t ring[C::kRing * C::kBytes > 4 * 32 * D * 4 ? C::kRing * C::kBytes : 4 * 32 * D * 4];
+    __shared__ int bad[D / 16];
+    const int lane = threadIdx.x & 63, col = lane & 31, up = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int id = blockIdx.x;
+    const int h = id % a.c.heads;
+    id /= a.c.heads;
+    const int split = id % splits;
+    id /= splits;
+    const int b = id % (int)a.B;
+    const int qt = qtiles - 1 - id / (int)a.B;                          // the longest rows first
+    const int group = a.q_heads / a.c.heads;
+
+    const Seq sq = sequence(a, b);
+    const int nq = sq.nq < a.max_q ? sq.nq : (int)a.max_q;
+    const int rows = nq * group, row0 = qt * kRows;
+    if (row0 >= rows) return;
+    const int row_last = row0 + kRows < rows ? row0 + kRows - 1 : rows - 1;
+    const int see_least = visible(a, sq, row0 / group), see_most = visible(a, sq, row_last / group);
+    const int t0 = split * chunk;
+    const int t1 = sq.lost ? 0 : see_most < t0 + chunk ? see_most : t0 + chunk;
+    if (split > 0 && t0 >= t1) return;
+
+    const int wrow0 = row0 + 64 * wave;                                 // this wave's rows
+    const int wlast = wrow0 + 64 < rows ? wrow0 + 63 : rows - 1;
+    const int wsee_least = wrow0 < rows ? visible(a, sq, wrow0 / group) : 0;
+    const int wsee_most = wrow0 < rows ? visible(a, sq, wlast / group) : 0;
+
+    h8 qf[NC][C::KF];
+    float c[NC], ref[NC], sum[NC];
+    int see[NC];
+    const float gk = *a.c.gk;
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        const int row = wrow0 + 32 * n + col;
+        const bool there = row < rows;
+        const int i = there ? row / group : 0;
+        see[n] = there ? visible(a, sq, i) : 0;
+        const uint16_t *src = a.q + (sq.q0 + i) * a.ldq + (int64_t)(h * group + (there ? row - i * group : 0)) * D + 8 * up;
+        uint4 w[C::KF];
+        float top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < C::KF; ++j) {
+            w[j] = there ? *reinterpret_cast<const uint4 *>(src + 16 * j) : make_uint4(0, 0, 0, 0);
+            const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t m = (e & 1) ? x[e >> 1] & 0x7FFF0000u : (x[e >> 1] << 16) & 0x7FFF0000u;
+                top = m < 0x7F800000u ? __builtin_fmaxf(top, f32_from_bits(m)) : top;
+            }
+        }
+        top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+        const int sh = top > 0.0f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
+#pragma unroll
+        for (int j = 0; j < C::KF; ++j) {
+            const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+            _Float16 y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                y[e] = (_Float16)__builtin_ldexpf(f32_from_bits((e & 1) ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16), sh);
+            qf[n][j] = h8{y[0], y[2], y[1], y[3], y[4], y[6], y[5], y[7]};   // the order of unpacked key codes
+        }
+        c[n] = __builtin_fmaxf(__builtin_ldexpf(a.scale * kLog2e * gk * 4096.0f, -sh), 0x1p-126f);
+        ref[n] = kLowest;
+        sum[n] = 0.0f;
+    }
+    f32x16 o[VT][NC];
+#pragma unroll
+    for (int x = 0; x < VT; ++x)
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[x][n][v] = 0.0f;
+
+    // this thread's part of the codes: keys (waves 0, 1): D / 4 channels of a token; values (2, 3): eight channels of four tokens
+    const bool keys = wave < 2;
+    const int part = threadIdx.x & 127;
+    const int my_tok = keys ? part >> 2 : (part / WD) * 4, my_at = keys ? part & 3 : part % WD;
+    const bool has = keys || part < 8 * WD;
+    const int *table = a.table + (int64_t)b * a.ld_table;
+    const int plog = a.c.page_log2, pmask = (1 << plog) - 1;
+    if (threadIdx.x < D / 16) bad[threadIdx.x] = kNoToken;
+
+    struct Codes {
+        uint32_t w[4], s;
+    };
+    auto fetch = [&](int t, Codes &z) {
+        const int u = wave & 1;                                          // 16 tokens lie in one page
+        const int tt = keys ? t + 16 * u : D == 128 ? t + 16 * u : t + 16 * (part >> 5);
+        int page = tt < t1 ? table[tt >> plog] : 0;
+        const bool in = page >= 0 && page < a.c.pages;
+        const int tok = (t + my_tok) & pmask;
+        const int64_t run = a.c.run(in ? page : 0, h) + tok;
+        if (keys) {
+            const uint8_t *p = a.c.kc + run * (D / 2) + my_at * (D / 8);
+            if constexpr (D == 128) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(p);
+                z.w[0] = x.x; z.w[1] = x.y; z.w[2] = x.z; z.w[3] = x.w;
+                z.s = *reinterpret_cast<const uint16_t *>(a.c.ks + run * (D / 16) + my_at * 2);
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(p);
+                z.w[0] = x.x; z.w[1] = x.y;
+                z.s = a.c.ks[run * (D / 16) + my_at];
+            }
+            if (!in) z.s = 0x7F7Fu;
+        } else if (has) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(a.c.vc + run * (D / 2) + my_at * 16);
+            z.w[0] = x.x; z.w[1] = x.y; z.w[2] = x.z; z.w[3] = x.w;
+            z.s = *reinterpret_cast<const uint32_t *>(a.c.vs + run * (D / 16) + (my_at >> 1) * 4);
+            if (!in) z.s = 0u;
+        }
+    };
+    auto unpack = [&](int t, Codes &z, uint8_t *dst) {
+        if (keys) {
+            const h2 sc = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(z.s, kScaleUp, false);
+            const h2 sc0 = {sc[0], sc[0]}, sc1 = {sc[1], sc[1]};
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                const h2 sj = j < 2 ? sc0 : sc1;
+                const uint32_t x = __builtin_amdgcn_perm(z.w[j], z.w[j], 0x01010000u);
+                const uint32_t y = __builtin_amdgcn_perm(z.w[j], z.w[j], 0x03030202u);
+                const int dw = my_at * (D / 32) + j;
+                *reinterpret_cast<uint4 *>(dst + (dw >> 1) * 1024 + (my_tok + 32 * (dw & 1)) * 16) =
+                    make_uint4(scaled((x << 4) & kCodeMask, sj), scaled(x & kCodeMask, sj), scaled((y << 4) & kCodeMask, sj),
+                               scaled(y & kCodeMask, sj));
+            }
+        } else if (has) {
+            if (t + 32 > see_least) {
+                // hidden values, as in the kernel above
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = t + my_tok + i;
+                    const bool nan = ((z.s >> (8 * i)) & 0x7Fu) == 0x7Fu;
+                    if (at >= t1 || nan) z.s &= ~(0xFFu << (8 * i));
+                    if (at < t1 && nan) atomicMin(&bad[my_at >> 1], at);
+                }
+            }
+            const h2 s0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(z.s, kScaleUp, false);
+            const h2 s1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(z.s, kScaleUp, true);
+            const int G = my_tok >> 2;
+            uint8_t *d = dst + C::KF * 1024 + ((G >> 2) * 64 + my_at + 32 * (G & 1)) * 16 + 8 * ((G >> 1) & 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t x = __builtin_amdgcn_perm(z.w[1], z.w[0], 0x04040000u + 0x01010101u * j);
+                const uint32_t y = __builtin_amdgcn_perm(z.w[3], z.w[2], 0x04040000u + 0x01010101u * j);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int cc = 2 * j + e;
+                    const uint2 v = make_uint2(scaled((e ? x : x << 4) & kCodeMask, s0), scaled((e ? y : y << 4) & kCodeMask, s1));
+                    *reinterpret_cast<uint2 *>(d + (cc / CPT) * 2048 + WD * (cc % CPT) * 16) = v;
+                }
+            }
+        }
+    };
+
+    auto scores = [&](const uint8_t *src, f32x16 (&s)[NC]) {
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[n][v] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < C::KF; ++j) {
+            const h8 kf = *reinterpret_cast<const h8 *>(src + j * 1024 + lane * 16);
+#pragma unroll
+            for (int n = 0; n < NC; ++n) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[n][j], s[n], 0, 0, 0);
+        }
+    };
+    auto weigh = [&](int t, f32x16 (&s)[NC], uint32_t (&p)[NC][8]) {
+        if (t + 32 > wsee_least) {                                       // uniform
+#pragma unroll
+            for (int n = 0; n < NC; ++n)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (t + 8 * (v >> 2) + 4 * up + (v & 3) >= see[n]) s[n][v] = -__builtin_inff();
+        }
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            float top = s[n][0];
+#pragma unroll
+            for (int v = 1; v < 16; ++v) top = __builtin_fmaxf(top, s[n][v]);
+            if (__any(__builtin_fmaf(top, c[n], -ref[n]) > kBelow + kSlack)) {
+                const float m = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+                const float next = __builtin_fmaf(m, c[n], -ref[n]) > kBelow + kSlack ? m * c[n] - kBelow : ref[n];
+                const float f = __builtin_amdgcn_exp2f(ref[n] - next);
+                ref[n] = next;
+                sum[n] *= f;
+#pragma unroll
+                for (int x = 0; x < VT; ++x)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[x][n][v] *= f;
+            }
+            float e[16];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][v], c[n], -ref[n]));
+            float part_sum = 0.0f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) part_sum += e[v];
+            sum[n] += part_sum;
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+                const h2 y = {(_Float16)e[2 * v], (_Float16)e[2 * v + 1]};
+                p[n][v] = __builtin_bit_cast(uint32_t, y);
+            }
+        }
+    };
+    auto values = [&](const uint8_t *src, const uint32_t (&p)[NC][8]) {
+#pragma unroll
+        for (int x = 0; x < VT; ++x)
+#pragma unroll
+            for (int kc = 0; kc < 2; ++kc) {
+                const h8 vf = *reinterpret_cast<const h8 *>(src + C::KF * 1024 + (2 * x + kc) * 1024 + lane * 16);
+#pragma unroll
+                for (int n = 0; n < NC; ++n) {
+                    const h8 pf = frag(p[n][4 * kc], p[n][4 * kc + 1], p[n][4 * kc + 2], p[n][4 * kc + 3]);
+                    o[x][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf, o[x][n], 0, 0, 0);
+                }
+            }
+    };
+
+    const int steps = t1 > t0 ? (t1 - t0 + 31) / 32 : 0;
+    Codes z;
+    __syncthreads();                                                     // bad[] is set
+    if (steps > 0) {
+        fetch(t0, z);
+        unpack(t0, z, ring);
+        if (steps > 1) {
+            fetch(t0 + 32, z);
+            unpack(t0 + 32, z, ring + C::kBytes);
+        }
+        if (steps > 2) fetch(t0 + 64, z);
+        __syncthreads();
+        f32x16 s[NC], s2[NC];
+        scores(ring, s);
+        for (int k = 0; k < steps; ++k) {
+            const int t = t0 + 32 * k;
+            if (k + 2 < steps) {
+                unpack(t + 64, z, ring + ((k + 2) & 3) * C::kBytes);
+                if (k + 3 < steps) fetch(t + 96, z);
+            }
+            if (k + 1 < steps && t + 32 < wsee_most) scores(ring + ((k + 1) & 3) * C::kBytes, s2);
+            if (t < wsee_most) {
+                uint32_t p[NC][8];
+                weigh(t, s, p);
+                values(ring + (k & 3) * C::kBytes, p);
+            }
+#pragma unroll
+            for (int n = 0; n < NC; ++n) s[n] = s2[n];
+            __syncthreads();
+        }
+    }
+    {
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int x = 0; x < VT; ++x)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int w = (8 * (v >> 2) + 4 * up + (v & 3)) % WD;
+                    if (bad[w >> 1] < see[n]) o[x][n][v] = __builtin_nanf("");
+                }
+    }
+
+    // rows through LDS, 32 at a time, each wave in its own part; a row's channels are turned by its number
+    float *mine = reinterpret_cast<float *>(ring) + wave * 32 * D;
+    const float gv = *a.c.gv * 4096.0f;
+    float *po = reinterpret_cast<float *>(a.workspace);
+    const int64_t all = a.T * a.q_heads;
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        sum[n] += __shfl_xor(sum[n], 32, 64);
+        const int row = wrow0 + 32 * n + col;
+        const int i = row / group;
+        const int64_t at = (sq.q0 + i) * a.q_heads + h * group + (row - i * group);
+        const bool none = see[n] == 0 && !sq.lost;
+        const float f = splits > 1 ? 1.0f : sq.lost ? __builtin_nanf("") : none ? 0.0f : gv / sum[n];
+        if (up == 0 && row < rows) {
+            if (splits > 1) {
+                float *pm = po + (int64_t)splits * all * D + 2 * (split * all + at);
+                pm[0] = ref[n];
+                pm[1] = sum[n];
+            } else if (a.lse) {
+                a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (ref[n] + __builtin_log2f(sum[n])) * kLn2;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < VT; ++x)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int rho = 8 * (v >> 2) + 4 * up + (v & 3);
+                const int ch = 8 * (rho % WD) + CPT * x + rho / WD;
+                mine[col * D + (ch ^ col)] = none ? 0.0f : o[x][n][v] * f;
+            }
+        __builtin_amdgcn_wave_barrier();
+        for (int rr = 0; rr < 32; ++rr) {
+            const int row2 = wrow0 + 32 * n + rr;
+            if (row2 >= rows) break;
+            const int i2 = row2 / group, hq = h * group + (row2 - i2 * group);
+            if (splits > 1) {
+                float *dst = po + (split * all + (sq.q0 + i2) * a.q_heads + hq) * D;
+                for (int ch = lane; ch < D; ch += 64) dst[ch] = mine[rr * D + (ch ^ rr)];
+            } else {
+                uint16_t *dst = a.out + (sq.q0 + i2) * a.ldo + (int64_t)hq * D;
+                if (2 * lane < D) {
+                    const float y0 = mine[rr * D + ((2 * lane) ^ rr)], y1 = mine[rr * D + ((2 * lane + 1) ^ rr)];
+                    *reinterpret_cast<uint32_t *>(dst + 2 * lane) = bf16_rne_from_float(y0) | (bf16_rne_from_float(y1) << 16);
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -474,8 +811,14 @@ template <int D> void join(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t s
 }
 
 template <int D> void attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
-    if (p.tiles == 1) decode<D, 1, 4>(a, p, stream);
-    else decode<D, 2, 4>(a, p, stream);
+    if (p.tiles == 1) {
+        decode<D, 1, 4>(a, p, stream);
+    } else if (p.tiles == 2) {
+        decode<D, 2, 4>(a, p, stream);
+    } else {
+        const int64_t n = a.B * a.c.heads * p.splits * p.qtiles;
+        kv4_prompt_kernel<D><<<(unsigned)n, 256, 0, stream>>>(a, p.qtiles, p.splits, p.chunk);
+    }
     if (p.splits > 1) join<D>(a, p, stream);
 }
 
