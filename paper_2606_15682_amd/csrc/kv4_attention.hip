@@ -26,6 +26,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr uint32_t kCodeMask = 0x80708070u;    // sign and magnitude of a code in either half word
 constexpr float kScaleUp = 128.0f;             // FP16 scales are s 2^7
 constexpr float kBelow = 7.0f, kSlack = 8.0f;  // r = maximum - kBelow, renewed when the maximum has grown by kSlack
+constexpr float kMostSum = 32768.0f;           // 2^(kBelow + kSlack): no single weight above it
 constexpr int kNoToken = 0x7FFFFFFF;
 constexpr float kLowest = -3.4028234663852886e38f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -414,25 +415,27 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
 
 // ------------------------------------------------------------------ prompts
 
-// A workgroup of four waves takes 256 rows, 64 a wave, and 32 tokens a step.  The codes of a step become FP16
-// once, in LDS, in the order of the matrix cores' operands (two waves the keys, two the values, two steps ahead;
+// A workgroup of eight waves takes 256 rows, 32 a wave, and 64 tokens a step.  The codes of a step become FP16
+// once, in LDS, in the order of the matrix cores' operands (four waves the keys, four the values, two steps ahead;
 // their codes are loaded three steps ahead), and every wave reads them from there:
 //   S^T = K Q^T  (32 tokens x 32 rows, K = 16 channels): lane (c, u) = (lane % 32, lane / 32) gets the scores of row c
 //     and tokens 8 x + 4 u .. 8 x + 4 u + 3.
 //   O^T = V^T P^T (32 channels x 32 rows, K = 16 tokens): eight of those, two groups of four, are its K share.
-// 64 rows a wave read an operand of 1 KB from LDS for two products of 32 cycles; 32 rows would need all of
-// the LDS bandwidth.  The scores of a step are computed beside the weights of the one before.
-template <int D> struct Tile {
-    static constexpr int KF = D / 16, VF = D / 16;       // operands of keys; of values (D / 32 tiles of channels x 2)
-    static constexpr int kBytes = (KF + VF) * 1024;
-    static constexpr int kRing = 4;
+// The scores of 32 tokens are computed beside the weights of the 32 before.
+template <int D> struct Prompt {
+    static constexpr int F = D / 16;                     // operands of 1 KB: of 32 tokens' keys; of their values
+    static constexpr int kSub = 2 * F * 1024;            // 32 tokens: keys, then values
+    static constexpr int kStage = 2 * kSub;
+    static constexpr int kRing = 3;
+    static constexpr int kOut = 8 * 32 * D * 4;          // the rows on their way out
+    static constexpr int kLds = kRing * kStage > kOut ? kRing * kStage : kOut;
 };
 
 template <int D>
-__global__ __launch_bounds__(256, 1) void kv4_prompt_kernel(const Kv4AttnArgs a, int qtiles, int splits, int chunk) {
-    using C = Tile<D>;
-    constexpr int NC = 2, VT = D / 32, WD = D / 8, CPT = 32 / WD, kRows = 256;
-    __shared__ __attribute__((aligned(16))) uint8_t ring[C::kRing * C::kBytes > 4 * 32 * D * 4 ? C::kRing * C::kBytes : 4 * 32 * D * 4];
+__global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a, int qtiles, int splits, int chunk) {
+    using C = Prompt<D>;
+    constexpr int VT = D / 32, WD = D / 8, CPT = 32 / WD, kRows = 256;
+    extern __shared__ __attribute__((aligned(16))) uint8_t ring[];
     __shared__ int bad[D / 16];
     const int lane = threadIdx.x & 63, col = lane & 31, up = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -455,26 +458,21 @@ __global__ __launch_bounds__(256, 1) void kv4_prompt_kernel(const Kv4AttnArgs a,
     const int t1 = sq.lost ? 0 : see_most < t0 + chunk ? see_most : t0 + chunk;
     if (split > 0 && t0 >= t1) return;
 
-    const int wrow0 = row0 + 64 * wave;                                 // this wave's rows
-    const int wlast = wrow0 + 64 < rows ? wrow0 + 63 : rows - 1;
-    const int wsee_least = wrow0 < rows ? visible(a, sq, wrow0 / group) : 0;
-    const int wsee_most = wrow0 < rows ? visible(a, sq, wlast / group) : 0;
+    const int row = row0 + 32 * wave + col;                             // this lane's row
+    const bool there = row < rows;
+    const int qi = there ? row / group : 0;
+    const int hq = h * group + (there ? row - qi * group : 0);
+    const int see = there ? visible(a, sq, qi) : 0;
+    const int wsee_least = row0 + 32 * wave < rows ? visible(a, sq, (row0 + 32 * wave) / group) : 0;
 
-    h8 qf[NC][C::KF];
-    float c[NC], ref[NC], sum[NC];
-    int see[NC];
-    const float gk = *a.c.gk;
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-        const int row = wrow0 + 32 * n + col;
-        const bool there = row < rows;
-        const int i = there ? row / group : 0;
-        see[n] = there ? visible(a, sq, i) : 0;
-        const uint16_t *src = a.q + (sq.q0 + i) * a.ldq + (int64_t)(h * group + (there ? row - i * group : 0)) * D + 8 * up;
-        uint4 w[C::KF];
+    h8 qf[C::F];
+    float c, ref = kLowest, sum = 0.0f;
+    {
+        const uint16_t *src = a.q + (sq.q0 + qi) * a.ldq + (int64_t)hq * D + 8 * up;
+        uint4 w[C::F];
         float top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < C::KF; ++j) {
+        for (int j = 0; j < C::F; ++j) {
             w[j] = there ? *reinterpret_cast<const uint4 *>(src + 16 * j) : make_uint4(0, 0, 0, 0);
             const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
 #pragma unroll
@@ -486,261 +484,245 @@ __global__ __launch_bounds__(256, 1) void kv4_prompt_kernel(const Kv4AttnArgs a,
         top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
         const int sh = top > 0.0f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
 #pragma unroll
-        for (int j = 0; j < C::KF; ++j) {
+        for (int j = 0; j < C::F; ++j) {
             const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
             _Float16 y[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 y[e] = (_Float16)__builtin_ldexpf(f32_from_bits((e & 1) ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16), sh);
-            qf[n][j] = h8{y[0], y[2], y[1], y[3], y[4], y[6], y[5], y[7]};   // the order of unpacked key codes
+            qf[j] = h8{y[0], y[2], y[1], y[3], y[4], y[6], y[5], y[7]};   // the order of unpacked key codes
         }
-        c[n] = __builtin_fmaxf(__builtin_ldexpf(a.scale * kLog2e * gk * 4096.0f, -sh), 0x1p-126f);
-        ref[n] = kLowest;
-        sum[n] = 0.0f;
+        c = __builtin_fmaxf(__builtin_ldexpf(a.scale * kLog2e * *a.c.gk * 4096.0f, -sh), 0x1p-126f);
     }
-    f32x16 o[VT][NC];
+    f32x16 o[VT];
 #pragma unroll
     for (int x = 0; x < VT; ++x)
 #pragma unroll
-        for (int n = 0; n < NC; ++n)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) o[x][n][v] = 0.0f;
+        for (int v = 0; v < 16; ++v) o[x][v] = 0.0f;
 
-    // this thread's part of the codes: keys (waves 0, 1): D / 4 channels of a token; values (2, 3): eight channels of four tokens
-    const bool keys = wave < 2;
-    const int part = threadIdx.x & 127;
-    const int my_tok = keys ? part >> 2 : (part / WD) * 4, my_at = keys ? part & 3 : part % WD;
-    const bool has = keys || part < 8 * WD;
+    // this thread's part of the codes, 16 tokens a wave: keys (waves 0 .. 3) D / 4 channels of a token, values
+    // (4 .. 7) eight channels of four tokens
+    const bool keys = wave < 4;
+    const int my_tok = keys ? lane >> 2 : (lane / WD) * 4, my_at = keys ? lane & 3 : lane % WD;
+    const bool has = keys || lane < 4 * WD;
     const int *table = a.table + (int64_t)b * a.ld_table;
     const int plog = a.c.page_log2, pmask = (1 << plog) - 1;
+    const uint32_t code_at = my_tok * (D / 2) + my_at * (keys ? D / 8 : 16);
+    const uint32_t scale_at = my_tok * (D / 16) + (keys ? my_at * (D / 64) : (my_at >> 1) * 4);
+    const uint8_t *codes = keys ? a.c.kc : a.c.vc, *scales = keys ? a.c.ks : a.c.vs;
+    // where its operands go: keys: dwords my_at (D / 32) + j of token my_tok; values: channel cc of dword my_at, tokens my_tok ..
+    const int sub_tok = 16 * (wave & 1) + my_tok, G = sub_tok >> 2;
+    const uint32_t put_at = ((wave & 3) >> 1) * C::kSub +
+                            (keys ? my_at * (D / 64) * 1024 + sub_tok * 16
+                                  : C::F * 1024 + ((G >> 2) * 64 + my_at + 32 * (G & 1)) * 16 + 8 * ((G >> 1) & 1));
     if (threadIdx.x < D / 16) bad[threadIdx.x] = kNoToken;
 
-    struct Codes {
-        uint32_t w[4], s;
+    uint32_t zw[4], zs = 0;
+    auto page_of = [&](int t) {
+        const int tt = t + 16 * (wave & 3);
+        return tt < t1 ? __builtin_amdgcn_readfirstlane(table[tt >> plog]) : 0;
     };
-    auto fetch = [&](int t, Codes &z) {
-        const int u = wave & 1;                                          // 16 tokens lie in one page
-        const int tt = keys ? t + 16 * u : D == 128 ? t + 16 * u : t + 16 * (part >> 5);
-        int page = tt < t1 ? table[tt >> plog] : 0;
-        const bool in = page >= 0 && page < a.c.pages;
-        const int tok = (t + my_tok) & pmask;
-        const int64_t run = a.c.run(in ? page : 0, h) + tok;
+    auto fetch = [&](int t, int page) {
+        const bool in = page >= 0 && page < a.c.pages;                   // uniform
+        const int64_t run = a.c.run(in ? page : 0, h) + ((t + 16 * (wave & 3)) & pmask);
+        const uint8_t *p = codes + run * (D / 2) + code_at, *q = scales + run * (D / 16) + scale_at;
         if (keys) {
-            const uint8_t *p = a.c.kc + run * (D / 2) + my_at * (D / 8);
             if constexpr (D == 128) {
                 const uint4 x = *reinterpret_cast<const uint4 *>(p);
-                z.w[0] = x.x; z.w[1] = x.y; z.w[2] = x.z; z.w[3] = x.w;
-                z.s = *reinterpret_cast<const uint16_t *>(a.c.ks + run * (D / 16) + my_at * 2);
+                zw[0] = x.x; zw[1] = x.y; zw[2] = x.z; zw[3] = x.w;
+                zs = *reinterpret_cast<const uint16_t *>(q);
             } else {
                 const uint2 x = *reinterpret_cast<const uint2 *>(p);
-                z.w[0] = x.x; z.w[1] = x.y;
-                z.s = a.c.ks[run * (D / 16) + my_at];
+                zw[0] = x.x; zw[1] = x.y;
+                zs = *q;
             }
-            if (!in) z.s = 0x7F7Fu;
+            zs = in ? zs : 0x7F7Fu;
         } else if (has) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(a.c.vc + run * (D / 2) + my_at * 16);
-            z.w[0] = x.x; z.w[1] = x.y; z.w[2] = x.z; z.w[3] = x.w;
-            z.s = *reinterpret_cast<const uint32_t *>(a.c.vs + run * (D / 16) + (my_at >> 1) * 4);
-            if (!in) z.s = 0u;
+            const uint4 x = *reinterpret_cast<const uint4 *>(p);
+            zw[0] = x.x; zw[1] = x.y; zw[2] = x.z; zw[3] = x.w;
+            zs = *reinterpret_cast<const uint32_t *>(q);
+            zs = in ? zs : 0u;
         }
     };
-    auto unpack = [&](int t, Codes &z, uint8_t *dst) {
+    auto unpack = [&](int t, uint8_t *stage) {
+        uint8_t *d = stage + put_at;
         if (keys) {
-            const h2 sc = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(z.s, kScaleUp, false);
+            const h2 sc = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(zs, kScaleUp, false);
             const h2 sc0 = {sc[0], sc[0]}, sc1 = {sc[1], sc[1]};
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
                 const h2 sj = j < 2 ? sc0 : sc1;
-                const uint32_t x = __builtin_amdgcn_perm(z.w[j], z.w[j], 0x01010000u);
-                const uint32_t y = __builtin_amdgcn_perm(z.w[j], z.w[j], 0x03030202u);
-                const int dw = my_at * (D / 32) + j;
-                *reinterpret_cast<uint4 *>(dst + (dw >> 1) * 1024 + (my_tok + 32 * (dw & 1)) * 16) =
+                const uint32_t x = __builtin_amdgcn_perm(zw[j], zw[j], 0x01010000u);
+                const uint32_t y = __builtin_amdgcn_perm(zw[j], zw[j], 0x03030202u);
+                *reinterpret_cast<uint4 *>(d + (j >> 1) * 1024 + (j & 1) * 512) =
                     make_uint4(scaled((x << 4) & kCodeMask, sj), scaled(x & kCodeMask, sj), scaled((y << 4) & kCodeMask, sj),
                                scaled(y & kCodeMask, sj));
             }
         } else if (has) {
-            if (t + 32 > see_least) {
+            if (t + 64 > see_least) {
                 // hidden values, as in the kernel above
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int at = t + my_tok + i;
-                    const bool nan = ((z.s >> (8 * i)) & 0x7Fu) == 0x7Fu;
-                    if (at >= t1 || nan) z.s &= ~(0xFFu << (8 * i));
+                    const int at = t + 16 * (wave & 3) + my_tok + i;
+                    const bool nan = ((zs >> (8 * i)) & 0x7Fu) == 0x7Fu;
+                    if (at >= t1 || nan) zs &= ~(0xFFu << (8 * i));
                     if (at < t1 && nan) atomicMin(&bad[my_at >> 1], at);
                 }
             }
-            const h2 s0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(z.s, kScaleUp, false);
-            const h2 s1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(z.s, kScaleUp, true);
-            const int G = my_tok >> 2;
-            uint8_t *d = dst + C::KF * 1024 + ((G >> 2) * 64 + my_at + 32 * (G & 1)) * 16 + 8 * ((G >> 1) & 1);
+            const h2 s0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(zs, kScaleUp, false);
+            const h2 s1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(zs, kScaleUp, true);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t x = __builtin_amdgcn_perm(z.w[1], z.w[0], 0x04040000u + 0x01010101u * j);
-                const uint32_t y = __builtin_amdgcn_perm(z.w[3], z.w[2], 0x04040000u + 0x01010101u * j);
+                const uint32_t x = __builtin_amdgcn_perm(zw[1], zw[0], 0x04040000u + 0x01010101u * j);
+                const uint32_t y = __builtin_amdgcn_perm(zw[3], zw[2], 0x04040000u + 0x01010101u * j);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int cc = 2 * j + e;
-                    const uint2 v = make_uint2(scaled((e ? x : x << 4) & kCodeMask, s0), scaled((e ? y : y << 4) & kCodeMask, s1));
-                    *reinterpret_cast<uint2 *>(d + (cc / CPT) * 2048 + WD * (cc % CPT) * 16) = v;
+                    *reinterpret_cast<uint2 *>(d + (cc / CPT) * 2048 + WD * (cc % CPT) * 16) =
+                        make_uint2(scaled((e ? x : x << 4) & kCodeMask, s0), scaled((e ? y : y << 4) & kCodeMask, s1));
                 }
             }
         }
     };
 
-    auto scores = [&](const uint8_t *src, f32x16 (&s)[NC]) {
+    auto scores = [&](const uint8_t *sub, f32x16 &s) {
 #pragma unroll
-        for (int n = 0; n < NC; ++n)
+        for (int v = 0; v < 16; ++v) s[v] = 0.0f;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) s[n][v] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < C::KF; ++j) {
-            const h8 kf = *reinterpret_cast<const h8 *>(src + j * 1024 + lane * 16);
-#pragma unroll
-            for (int n = 0; n < NC; ++n) s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[n][j], s[n], 0, 0, 0);
-        }
+        for (int j = 0; j < C::F; ++j)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(sub + j * 1024 + lane * 16), qf[j], s, 0, 0, 0);
     };
-    auto weigh = [&](int t, f32x16 (&s)[NC], uint32_t (&p)[NC][8]) {
-        if (t + 32 > wsee_least) {                                       // uniform
+    // The weights of 32 tokens (s), the scores of the next 32 beside them (ahead).  The reference needs no
+    // maximum as long as the sum of a lane's weights stays below the largest single one allowed.
+    auto weigh = [&](int t, f32x16 &s, uint32_t (&p)[8], bool edge) {
+        if (edge) {                                                      // uniform
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (t + 8 * (v >> 2) + 4 * up + (v & 3) >= see[n]) s[n][v] = -__builtin_inff();
+            for (int v = 0; v < 16; ++v)
+                if (t + 8 * (v >> 2) + 4 * up + (v & 3) >= see) s[v] = -__builtin_inff();
         }
+        float e[16], total = 0.0f;
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            float top = s[n][0];
-#pragma unroll
-            for (int v = 1; v < 16; ++v) top = __builtin_fmaxf(top, s[n][v]);
-            if (__any(__builtin_fmaf(top, c[n], -ref[n]) > kBelow + kSlack)) {
-                const float m = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
-                const float next = __builtin_fmaf(m, c[n], -ref[n]) > kBelow + kSlack ? m * c[n] - kBelow : ref[n];
-                const float f = __builtin_amdgcn_exp2f(ref[n] - next);
-                ref[n] = next;
-                sum[n] *= f;
-#pragma unroll
-                for (int x = 0; x < VT; ++x)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) o[x][n][v] *= f;
-            }
-            float e[16];
-#pragma unroll
-            for (int v = 0; v < 16; ++v) e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][v], c[n], -ref[n]));
-            float part_sum = 0.0f;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) part_sum += e[v];
-            sum[n] += part_sum;
-#pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                const h2 y = {(_Float16)e[2 * v], (_Float16)e[2 * v + 1]};
-                p[n][v] = __builtin_bit_cast(uint32_t, y);
-            }
+        for (int v = 0; v < 16; ++v) {
+            e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -ref));
+            total += e[v];
         }
-    };
-    auto values = [&](const uint8_t *src, const uint32_t (&p)[NC][8]) {
+        if (__any(total > kMostSum)) {
+            const bool need = __builtin_fmaxf(total, __shfl_xor(total, 32, 64)) > kMostSum;   // a row moves by its own scores alone
+            float top = s[0];
 #pragma unroll
-        for (int x = 0; x < VT; ++x)
-#pragma unroll
-            for (int kc = 0; kc < 2; ++kc) {
-                const h8 vf = *reinterpret_cast<const h8 *>(src + C::KF * 1024 + (2 * x + kc) * 1024 + lane * 16);
-#pragma unroll
-                for (int n = 0; n < NC; ++n) {
-                    const h8 pf = frag(p[n][4 * kc], p[n][4 * kc + 1], p[n][4 * kc + 2], p[n][4 * kc + 3]);
-                    o[x][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf, o[x][n], 0, 0, 0);
-                }
-            }
-    };
-
-    const int steps = t1 > t0 ? (t1 - t0 + 31) / 32 : 0;
-    Codes z;
-    __syncthreads();                                                     // bad[] is set
-    if (steps > 0) {
-        fetch(t0, z);
-        unpack(t0, z, ring);
-        if (steps > 1) {
-            fetch(t0 + 32, z);
-            unpack(t0 + 32, z, ring + C::kBytes);
-        }
-        if (steps > 2) fetch(t0 + 64, z);
-        __syncthreads();
-        f32x16 s[NC], s2[NC];
-        scores(ring, s);
-        for (int k = 0; k < steps; ++k) {
-            const int t = t0 + 32 * k;
-            if (k + 2 < steps) {
-                unpack(t + 64, z, ring + ((k + 2) & 3) * C::kBytes);
-                if (k + 3 < steps) fetch(t + 96, z);
-            }
-            if (k + 1 < steps && t + 32 < wsee_most) scores(ring + ((k + 1) & 3) * C::kBytes, s2);
-            if (t < wsee_most) {
-                uint32_t p[NC][8];
-                weigh(t, s, p);
-                values(ring + (k & 3) * C::kBytes, p);
-            }
-#pragma unroll
-            for (int n = 0; n < NC; ++n) s[n] = s2[n];
-            __syncthreads();
-        }
-    }
-    {
-#pragma unroll
-        for (int n = 0; n < NC; ++n)
+            for (int v = 1; v < 16; ++v) top = __builtin_fmaxf(top, s[v]);
+            top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+            const float next = need ? top * c - kBelow : ref;
+            const float f = __builtin_amdgcn_exp2f(ref - next);
+            ref = next;
+            sum *= f;
 #pragma unroll
             for (int x = 0; x < VT; ++x)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int w = (8 * (v >> 2) + 4 * up + (v & 3)) % WD;
-                    if (bad[w >> 1] < see[n]) o[x][n][v] = __builtin_nanf("");
-                }
-    }
-
-    // rows through LDS, 32 at a time, each wave in its own part; a row's channels are turned by its number
-    float *mine = reinterpret_cast<float *>(ring) + wave * 32 * D;
-    const float gv = *a.c.gv * 4096.0f;
-    float *po = reinterpret_cast<float *>(a.workspace);
-    const int64_t all = a.T * a.q_heads;
+                for (int v = 0; v < 16; ++v) o[x][v] *= f;
+            total = 0.0f;
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-        sum[n] += __shfl_xor(sum[n], 32, 64);
-        const int row = wrow0 + 32 * n + col;
-        const int i = row / group;
-        const int64_t at = (sq.q0 + i) * a.q_heads + h * group + (row - i * group);
-        const bool none = see[n] == 0 && !sq.lost;
-        const float f = splits > 1 ? 1.0f : sq.lost ? __builtin_nanf("") : none ? 0.0f : gv / sum[n];
-        if (up == 0 && row < rows) {
-            if (splits > 1) {
-                float *pm = po + (int64_t)splits * all * D + 2 * (split * all + at);
-                pm[0] = ref[n];
-                pm[1] = sum[n];
-            } else if (a.lse) {
-                a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (ref[n] + __builtin_log2f(sum[n])) * kLn2;
+            for (int v = 0; v < 16; ++v) {
+                e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -ref));
+                total += e[v];
             }
         }
+        sum += total;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            const h2 y = {(_Float16)e[2 * v], (_Float16)e[2 * v + 1]};
+            p[v] = __builtin_bit_cast(uint32_t, y);
+        }
+    };
+    auto values = [&](const uint8_t *sub, const uint32_t (&p)[8]) {
 #pragma unroll
         for (int x = 0; x < VT; ++x)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int rho = 8 * (v >> 2) + 4 * up + (v & 3);
-                const int ch = 8 * (rho % WD) + CPT * x + rho / WD;
-                mine[col * D + (ch ^ col)] = none ? 0.0f : o[x][n][v] * f;
-            }
-        __builtin_amdgcn_wave_barrier();
-        for (int rr = 0; rr < 32; ++rr) {
-            const int row2 = wrow0 + 32 * n + rr;
-            if (row2 >= rows) break;
-            const int i2 = row2 / group, hq = h * group + (row2 - i2 * group);
-            if (splits > 1) {
-                float *dst = po + (split * all + (sq.q0 + i2) * a.q_heads + hq) * D;
-                for (int ch = lane; ch < D; ch += 64) dst[ch] = mine[rr * D + (ch ^ rr)];
-            } else {
-                uint16_t *dst = a.out + (sq.q0 + i2) * a.ldo + (int64_t)hq * D;
-                if (2 * lane < D) {
-                    const float y0 = mine[rr * D + ((2 * lane) ^ rr)], y1 = mine[rr * D + ((2 * lane + 1) ^ rr)];
-                    *reinterpret_cast<uint32_t *>(dst + 2 * lane) = bf16_rne_from_float(y0) | (bf16_rne_from_float(y1) << 16);
-                }
-            }
+            for (int kc = 0; kc < 2; ++kc)
+                o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                    *reinterpret_cast<const h8 *>(sub + (C::F + 2 * x + kc) * 1024 + lane * 16),
+                    frag(p[4 * kc], p[4 * kc + 1], p[4 * kc + 2], p[4 * kc + 3]), o[x], 0, 0, 0);
+    };
+
+    const int steps = t1 > t0 ? (t1 - t0 + 63) / 64 : 0;
+    __syncthreads();                                                     // bad[] is set
+    if (steps > 0) {
+        // the ring's slots of this step, the next and the one after; the last steps unpack what lies beyond (page 0, unused)
+        uint8_t *now = ring, *next = ring + C::kStage, *after = ring + 2 * C::kStage;
+        fetch(t0, page_of(t0));
+        unpack(t0, now);
+        fetch(t0 + 64, page_of(t0 + 64));
+        unpack(t0 + 64, next);
+        fetch(t0 + 128, page_of(t0 + 128));
+        int page = page_of(t0 + 192);
+        __syncthreads();
+        f32x16 s0, s1;
+        scores(now, s0);
+        for (int k = 0, t = t0; k < steps; ++k, t += 64) {
+            const bool edge = t + 64 > wsee_least;
+            uint32_t p[8];
+            scores(now + C::kSub, s1);
+            weigh(t, s0, p, edge);
+            unpack(t + 128, after);
+            fetch(t + 192, page);
+            page = page_of(t + 256);
+            values(now, p);
+            scores(next, s0);
+            weigh(t + 32, s1, p, edge);
+            values(now + C::kSub, p);
+            __syncthreads();
+            uint8_t *x = now;
+            now = next;
+            next = after;
+            after = x;
         }
-        __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int x = 0; x < VT; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int w = (8 * (v >> 2) + 4 * up + (v & 3)) % WD;
+            if (bad[w >> 1] < see) o[x][v] = __builtin_nanf("");
+        }
+
+    // rows through LDS, each wave in its own part; a row's channels are turned by its number
+    float *mine = reinterpret_cast<float *>(ring) + wave * 32 * D;
+    float *po = reinterpret_cast<float *>(a.workspace);
+    const int64_t all = a.T * a.q_heads;
+    sum += __shfl_xor(sum, 32, 64);
+    const bool none = see == 0 && !sq.lost;
+    const float f = splits > 1 ? 1.0f : sq.lost ? __builtin_nanf("") : none ? 0.0f : *a.c.gv * 4096.0f / sum;
+    if (up == 0 && there) {
+        const int64_t at = (sq.q0 + qi) * a.q_heads + hq;
+        if (splits > 1) {
+            float *pm = po + (int64_t)splits * all * D + 2 * (split * all + at);
+            pm[0] = ref;
+            pm[1] = sum;
+        } else if (a.lse) {
+            a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (ref + __builtin_log2f(sum)) * kLn2;
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < VT; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int rho = 8 * (v >> 2) + 4 * up + (v & 3);
+            const int ch = 8 * (rho % WD) + CPT * x + rho / WD;
+            mine[col * D + (ch ^ col)] = none ? 0.0f : o[x][v] * f;
+        }
+    __builtin_amdgcn_wave_barrier();
+    for (int rr = 0; rr < 32; ++rr) {
+        const int row2 = row0 + 32 * wave + rr;
+        if (row2 >= rows) break;
+        const int i2 = row2 / group, hq2 = h * group + (row2 - i2 * group);
+        if (splits > 1) {
+            float *dst = po + (split * all + (sq.q0 + i2) * a.q_heads + hq2) * D;
+            for (int ch = lane; ch < D; ch += 64) dst[ch] = mine[rr * D + (ch ^ rr)];
+        } else if (2 * lane < D) {
+            uint16_t *dst = a.out + (sq.q0 + i2) * a.ldo + (int64_t)hq2 * D;
+            const float y0 = mine[rr * D + ((2 * lane) ^ rr)], y1 = mine[rr * D + ((2 * lane + 1) ^ rr)];
+            *reinterpret_cast<uint32_t *>(dst + 2 * lane) = bf16_rne_from_float(y0) | (bf16_rne_from_float(y1) << 16);
+        }
     }
 }
 
@@ -810,16 +792,20 @@ template <int D> void join(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t s
     else kv4_join_kernel<D, 8><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
 }
 
-template <int D> void attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
+template <int D> hipError_t attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
     if (p.tiles == 1) {
         decode<D, 1, 4>(a, p, stream);
     } else if (p.tiles == 2) {
         decode<D, 2, 4>(a, p, stream);
     } else {
         const int64_t n = a.B * a.c.heads * p.splits * p.qtiles;
-        kv4_prompt_kernel<D><<<(unsigned)n, 256, 0, stream>>>(a, p.qtiles, p.splits, p.chunk);
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kv4_prompt_kernel<D>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, Prompt<D>::kLds);
+        if (e != hipSuccess) return e;
+        kv4_prompt_kernel<D><<<(unsigned)n, 512, Prompt<D>::kLds, stream>>>(a, p.qtiles, p.splits, p.chunk);
     }
     if (p.splits > 1) join<D>(a, p, stream);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -831,9 +817,7 @@ size_t kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_
 
 hipError_t launch_kv4_attention(const Kv4AttnArgs &a, hipStream_t stream) {
     const Kv4Plan p = kv4_plan(a.B, a.max_q, a.max_kv, a.q_heads, a.c.heads);
-    if (a.c.D == 128) attend<128>(a, p, stream);
-    else attend<64>(a, p, stream);
-    return hipGetLastError();
+    return a.c.D == 128 ? attend<128>(a, p, stream) : attend<64>(a, p, stream);
 }
 
 }  // namespace reqat
