@@ -11,6 +11,8 @@
 // 2^(s - r) are rounded to FP16 (11 bits, 3 more than the output has): r trails the running maximum,
 // at least 7 and at most 15 below it, so p is at most 2^15 and the FP16 range reaches 2^-31 of the largest
 // weight or below; the sum of weights is taken in FP32 before that rounding.
+#include <type_traits>
+
 #include "fp4_device.h"
 #include "internal.h"
 
@@ -91,6 +93,7 @@ __device__ __forceinline__ int visible(const Kv4AttnArgs &a, const Seq &s, int i
 template <int D> struct Step {
     uint32_t k[2][D / 32], ks[2];
     uint32_t v[2][4], vs[2];
+    bool in[2];                          // the page lies in the cache (looked at when the loads have long been issued)
 };
 
 template <int D, int NT, int W>
@@ -212,10 +215,7 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
             st.v[u][2] = y.z;
             st.v[u][3] = y.w;
             st.vs[u] = *reinterpret_cast<const uint32_t *>(a.c.vs + run * (D / 16) + vs_at);
-            if (!in) {                                                 // nothing of it is used
-                st.ks[u] = 0x7F7Fu;
-                st.vs[u] = 0u;
-            }
+            st.in[u] = in;
         }
     };
 
@@ -223,6 +223,10 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
         f32x4 s[2][NT];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+            if (!st.in[u]) {                                           // uniform: scores NaN, values zero
+                st.ks[u] = 0x7F7Fu;
+                st.vs[u] = 0u;
+            }
             const h2 sc = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(st.ks[u], kScaleUp, false);
             const h2 sc0 = {sc[0], sc[0]}, sc1 = {sc[1], sc[1]};
 #pragma unroll
@@ -426,7 +430,7 @@ template <int D> struct Prompt {
     static constexpr int F = D / 16;                     // operands of 1 KB: of 32 tokens' keys; of their values
     static constexpr int kSub = 2 * F * 1024;            // 32 tokens: keys, then values
     static constexpr int kStage = 2 * kSub;
-    static constexpr int kRing = 3;
+    static constexpr int kRing = 4;
     static constexpr int kOut = 8 * 32 * D * 4;          // the rows on their way out
     static constexpr int kLds = kRing * kStage > kOut ? kRing * kStage : kOut;
 };
@@ -510,21 +514,28 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     const uint32_t code_at = my_tok * (D / 2) + my_at * (keys ? D / 8 : 16);
     const uint32_t scale_at = my_tok * (D / 16) + (keys ? my_at * (D / 64) : (my_at >> 1) * 4);
     const uint8_t *codes = keys ? a.c.kc : a.c.vc, *scales = keys ? a.c.ks : a.c.vs;
-    // where its operands go: keys: dwords my_at (D / 32) + j of token my_tok; values: channel cc of dword my_at, tokens my_tok ..
-    const int sub_tok = 16 * (wave & 1) + my_tok, G = sub_tok >> 2;
+    // where its operands go.  Keys: dwords my_at (D / 32) + j of token my_tok; a quarter's operands have their lanes turned
+    // by 2 my_at, so that eight lanes of a write (two tokens) fall on all banks.  Values: tokens my_tok .. my_tok + 3 and + 8 ..
+    // are one operand row: lanes a half (D = 64: a quarter) wave apart swap, the lower ones keep the dword's channels 0 .. 3,
+    // the upper ones 4 .. 7.
+    const int half = D == 128 ? lane >> 5 : (lane >> 4) & 1, odd = D == 128 ? (lane >> 4) & 1 : (lane >> 3) & 1;
     const uint32_t put_at = ((wave & 3) >> 1) * C::kSub +
-                            (keys ? my_at * (D / 64) * 1024 + sub_tok * 16
-                                  : C::F * 1024 + ((G >> 2) * 64 + my_at + 32 * (G & 1)) * 16 + 8 * ((G >> 1) & 1));
+                            (keys ? my_at * (D / 64) * 1024 + (((16 * (wave & 1) + my_tok) ^ (2 * my_at)) * 16)
+                                  : (C::F + (wave & 1)) * 1024 + (my_at + 32 * odd) * 16 + half * (4 / CPT) * 2048);
+    uint32_t turned[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) turned[j] = (lane ^ (2 * j)) * 16;
     if (threadIdx.x < D / 16) bad[threadIdx.x] = kNoToken;
 
     uint32_t zw[4], zs = 0;
+    bool z_in = true;                    // the page lies in the cache (looked at when the loads have long been issued)
     auto page_of = [&](int t) {
         const int tt = t + 16 * (wave & 3);
         return tt < t1 ? __builtin_amdgcn_readfirstlane(table[tt >> plog]) : 0;
     };
     auto fetch = [&](int t, int page) {
-        const bool in = page >= 0 && page < a.c.pages;                   // uniform
-        const int64_t run = a.c.run(in ? page : 0, h) + ((t + 16 * (wave & 3)) & pmask);
+        z_in = page >= 0 && page < a.c.pages;                            // uniform
+        const int64_t run = a.c.run(z_in ? page : 0, h) + ((t + 16 * (wave & 3)) & pmask);
         const uint8_t *p = codes + run * (D / 2) + code_at, *q = scales + run * (D / 16) + scale_at;
         if (keys) {
             if constexpr (D == 128) {
@@ -536,16 +547,15 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
                 zw[0] = x.x; zw[1] = x.y;
                 zs = *q;
             }
-            zs = in ? zs : 0x7F7Fu;
         } else if (has) {
             const uint4 x = *reinterpret_cast<const uint4 *>(p);
             zw[0] = x.x; zw[1] = x.y; zw[2] = x.z; zw[3] = x.w;
             zs = *reinterpret_cast<const uint32_t *>(q);
-            zs = in ? zs : 0u;
         }
     };
     auto unpack = [&](int t, uint8_t *stage) {
         uint8_t *d = stage + put_at;
+        if (!z_in) zs = keys ? 0x7F7Fu : 0u;
         if (keys) {
             const h2 sc = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(zs, kScaleUp, false);
             const h2 sc0 = {sc[0], sc[0]}, sc1 = {sc[1], sc[1]};
@@ -571,16 +581,23 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
             }
             const h2 s0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(zs, kScaleUp, false);
             const h2 s1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(zs, kScaleUp, true);
+            uint32_t x[8], y[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t x = __builtin_amdgcn_perm(zw[1], zw[0], 0x04040000u + 0x01010101u * j);
-                const uint32_t y = __builtin_amdgcn_perm(zw[3], zw[2], 0x04040000u + 0x01010101u * j);
+                const uint32_t lo = __builtin_amdgcn_perm(zw[1], zw[0], 0x04040000u + 0x01010101u * j);
+                const uint32_t hi = __builtin_amdgcn_perm(zw[3], zw[2], 0x04040000u + 0x01010101u * j);
+                x[2 * j] = scaled((lo << 4) & kCodeMask, s0);
+                y[2 * j] = scaled((hi << 4) & kCodeMask, s1);
+                x[2 * j + 1] = scaled(lo & kCodeMask, s0);
+                y[2 * j + 1] = scaled(hi & kCodeMask, s1);
+            }
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int cc = 2 * j + e;
-                    *reinterpret_cast<uint2 *>(d + (cc / CPT) * 2048 + WD * (cc % CPT) * 16) =
-                        make_uint2(scaled((e ? x : x << 4) & kCodeMask, s0), scaled((e ? y : y << 4) & kCodeMask, s1));
-                }
+            for (int j = 0; j < 4; ++j) {
+                const auto px = D == 128 ? __builtin_amdgcn_permlane32_swap(x[j], x[j + 4], false, false)
+                                         : __builtin_amdgcn_permlane16_swap(x[j], x[j + 4], false, false);
+                const auto py = D == 128 ? __builtin_amdgcn_permlane32_swap(y[j], y[j + 4], false, false)
+                                         : __builtin_amdgcn_permlane16_swap(y[j], y[j + 4], false, false);
+                *reinterpret_cast<uint4 *>(d + (j / CPT) * 2048 + WD * (j % CPT) * 16) = make_uint4(px[0], py[0], px[1], py[1]);
             }
         }
     };
@@ -590,12 +607,12 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         for (int v = 0; v < 16; ++v) s[v] = 0.0f;
 #pragma unroll
         for (int j = 0; j < C::F; ++j)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(sub + j * 1024 + lane * 16), qf[j], s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(sub + j * 1024 + turned[j / (C::F / 4)]), qf[j], s, 0, 0, 0);
     };
-    // The weights of 32 tokens (s), the scores of the next 32 beside them (ahead).  The reference needs no
-    // maximum as long as the sum of a lane's weights stays below the largest single one allowed.
-    auto weigh = [&](int t, f32x16 &s, uint32_t (&p)[8], bool edge) {
-        if (edge) {                                                      // uniform
+    // The weights of 32 tokens.  The reference needs no maximum as long as the sum of a lane's weights stays below
+    // the largest single one allowed.
+    auto weigh = [&](int t, f32x16 &s, uint32_t (&p)[8], auto edge) {
+        if constexpr (decltype(edge)::value) {
 #pragma unroll
             for (int v = 0; v < 16; ++v)
                 if (t + 8 * (v >> 2) + 4 * up + (v & 3) >= see) s[v] = -__builtin_inff();
@@ -634,11 +651,25 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
             p[v] = __builtin_bit_cast(uint32_t, y);
         }
     };
+    // The product with 32 tokens' values (of sub) and the scores of 32 later tokens (keys), in turn: neither waits for
+    // itself, and the exponentials that come next in program order do not depend on them.
+    auto products = [&](const uint8_t *sub, const uint32_t (&p)[8], const uint8_t *keys_at, f32x16 &s) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C::F; ++i) {
+            const int x = i % VT, kc = i / VT;
+            o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                *reinterpret_cast<const h8 *>(sub + (C::F + 2 * x + kc) * 1024 + lane * 16),
+                frag(p[4 * kc], p[4 * kc + 1], p[4 * kc + 2], p[4 * kc + 3]), o[x], 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(keys_at + i * 1024 + turned[i / (C::F / 4)]), qf[i], s, 0, 0, 0);
+        }
+    };
     auto values = [&](const uint8_t *sub, const uint32_t (&p)[8]) {
 #pragma unroll
-        for (int x = 0; x < VT; ++x)
+        for (int kc = 0; kc < 2; ++kc)
 #pragma unroll
-            for (int kc = 0; kc < 2; ++kc)
+            for (int x = 0; x < VT; ++x)
                 o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
                     *reinterpret_cast<const h8 *>(sub + (C::F + 2 * x + kc) * 1024 + lane * 16),
                     frag(p[4 * kc], p[4 * kc + 1], p[4 * kc + 2], p[4 * kc + 3]), o[x], 0, 0, 0);
@@ -647,35 +678,40 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     const int steps = t1 > t0 ? (t1 - t0 + 63) / 64 : 0;
     __syncthreads();                                                     // bad[] is set
     if (steps > 0) {
-        // the ring's slots of this step, the next and the one after; the last steps unpack what lies beyond (page 0, unused)
-        uint8_t *now = ring, *next = ring + C::kStage, *after = ring + 2 * C::kStage;
+        // Slots of the ring: the step before (its last values are still to come), this one, the next, and the one unpacked
+        // into.  The last steps unpack what lies beyond the tokens (of page 0), which nothing uses.
+        uint32_t slot = 0;
+        auto stage = [&](uint32_t k) { return ring + (k & 3) * C::kStage; };
         fetch(t0, page_of(t0));
-        unpack(t0, now);
+        unpack(t0, stage(0));
         fetch(t0 + 64, page_of(t0 + 64));
-        unpack(t0 + 64, next);
+        unpack(t0 + 64, stage(1));
         fetch(t0 + 128, page_of(t0 + 128));
-        int page = page_of(t0 + 192);
+        int page = page_of(t0 + 192), t = t0;
         __syncthreads();
         f32x16 s0, s1;
-        scores(now, s0);
-        for (int k = 0, t = t0; k < steps; ++k, t += 64) {
-            const bool edge = t + 64 > wsee_least;
-            uint32_t p[8];
-            scores(now + C::kSub, s1);
-            weigh(t, s0, p, edge);
-            unpack(t + 128, after);
+        scores(stage(0), s0);
+        uint32_t p[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        const uint8_t *before = stage(0) + C::kSub;                     // no weights yet
+        auto step = [&](auto edge) {
+            const uint8_t *now = stage(slot);
+            unpack(t + 128, stage(slot + 2));
             fetch(t + 192, page);
             page = page_of(t + 256);
-            values(now, p);
-            scores(next, s0);
+            products(before, p, now + C::kSub, s1);
+            weigh(t, s0, p, edge);
+            products(now, p, stage(slot + 1), s0);
             weigh(t + 32, s1, p, edge);
-            values(now + C::kSub, p);
+            before = now + C::kSub;
+            ++slot;
+            t += 64;
             __syncthreads();
-            uint8_t *x = now;
-            now = next;
-            next = after;
-            after = x;
-        }
+        };
+        const int open = t1 < wsee_least ? t1 : wsee_least;              // steps below it hide nothing from this wave
+        while (t + 64 <= open) step(std::false_type{});
+        while (t < t1) step(std::true_type{});
+        values(before, p);
+        __syncthreads();
     }
 #pragma unroll
     for (int x = 0; x < VT; ++x)
