@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "fp4_device.h"
+#include "g2l.h"
 #include "internal.h"
 
 namespace reqat {
@@ -533,7 +534,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         const int tt = t + 16 * (wave & 3);
         return tt < t1 ? __builtin_amdgcn_readfirstlane(table[tt >> plog]) : 0;
     };
-    auto fetch = [&](int t, int page) {
+    auto fetch = [&](int t, int page) __attribute__((always_inline)) {
         z_in = page >= 0 && page < a.c.pages;                            // uniform
         const int64_t run = a.c.run(z_in ? page : 0, h) + ((t + 16 * (wave & 3)) & pmask);
         const uint8_t *p = codes + run * (D / 2) + code_at, *q = scales + run * (D / 16) + scale_at;
@@ -553,7 +554,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
             zs = *reinterpret_cast<const uint32_t *>(q);
         }
     };
-    auto unpack = [&](int t, uint8_t *stage) {
+    auto unpack = [&](int t, uint8_t *stage) __attribute__((always_inline)) {
         uint8_t *d = stage + put_at;
         if (!z_in) zs = keys ? 0x7F7Fu : 0u;
         if (keys) {
@@ -602,27 +603,50 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         }
     };
 
-    auto scores = [&](const uint8_t *sub, f32x16 &s) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) s[v] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < C::F; ++j)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(sub + j * 1024 + turned[j / (C::F / 4)]), qf[j], s, 0, 0, 0);
+    // Operand m of a block: the products with 32 tokens' values (sub) and with the keys of 32 later ones, in turn.
+    auto operand = [&](const uint8_t *sub, const uint8_t *keys_at, int m) __attribute__((always_inline)) {
+        const int i = m >> 1;
+        return m & 1 ? *reinterpret_cast<const h8 *>(keys_at + i * 1024 + turned[i / (C::F / 4)])
+                     : *reinterpret_cast<const h8 *>(sub + (C::F + 2 * (i % VT) + i / VT) * 1024 + lane * 16);
     };
-    // The weights of 32 tokens.  The reference needs no maximum as long as the sum of a lane's weights stays below
-    // the largest single one allowed.
-    auto weigh = [&](int t, f32x16 &s, uint32_t (&p)[8], auto edge) {
+    h8 ops[4];                                                           // the next four
+    // A block: O += V^T P^T of the 32 tokens whose weights are p, the scores `ahead` of 32 later tokens, and the weights of
+    // the 32 between (scores s, first token t), which replace p.  An MFMA takes 32 cycles and its wave issues the
+    // exponential of one element and the operand read four MFMAs ahead beside it: pinned in this order, since a wave
+    // issues in order and stands still where two MFMAs meet.  The reference needs no maximum as long as
+    // the sum of a lane's weights stays below the largest single one allowed.
+    auto block = [&](const uint8_t *sub, const uint8_t *keys_at, const uint8_t *sub2, const uint8_t *keys2, int t,
+                     f32x16 &s, f32x16 &ahead, uint32_t (&p)[8], auto edge) __attribute__((always_inline)) {
         if constexpr (decltype(edge)::value) {
 #pragma unroll
             for (int v = 0; v < 16; ++v)
                 if (t + 8 * (v >> 2) + 4 * up + (v & 3) >= see) s[v] = -__builtin_inff();
         }
-        float e[16], total = 0.0f;
+        constexpr int kOps = 2 * C::F, kEach = 16 / kOps;
+        uint32_t w[8];
+        float total = 0.0f, last = 0.0f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -ref));
-            total += e[v];
-        }
+        for (int v = 0; v < 16; ++v) ahead[v] = 0.0f;
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<0, kOps>([&](auto M) __attribute__((always_inline)) {
+            constexpr int m = M, i = m >> 1, x = i % VT, kc = i / VT;
+            if constexpr (m & 1) ahead = __builtin_amdgcn_mfma_f32_32x32x16_f16(ops[m & 3], qf[i], ahead, 0, 0, 0);
+            else o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ops[m & 3], frag(p[4 * kc], p[4 * kc + 1], p[4 * kc + 2], p[4 * kc + 3]), o[x], 0, 0, 0);
+            if constexpr (m + 4 < kOps) ops[m & 3] = operand(sub, keys_at, m + 4);
+            else ops[m & 3] = operand(sub2, keys2, m + 4 - kOps);
+#pragma unroll
+            for (int y = 0; y < kEach; ++y) {
+                const int v = m * kEach + y;
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -ref));
+                total += e;
+                if (v & 1) {
+                    const h2 z = {(_Float16)last, (_Float16)e};
+                    w[v >> 1] = __builtin_bit_cast(uint32_t, z);
+                }
+                last = e;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
         if (__any(total > kMostSum)) {
             const bool need = __builtin_fmaxf(total, __shfl_xor(total, 32, 64)) > kMostSum;   // a row moves by its own scores alone
             float top = s[0];
@@ -639,40 +663,18 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
                 for (int v = 0; v < 16; ++v) o[x][v] *= f;
             total = 0.0f;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -ref));
-                total += e[v];
+            for (int v = 0; v < 16; v += 2) {
+                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -ref));
+                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v + 1], c, -ref));
+                total += e0;
+                total += e1;
+                const h2 z = {(_Float16)e0, (_Float16)e1};
+                w[v >> 1] = __builtin_bit_cast(uint32_t, z);
             }
         }
         sum += total;
 #pragma unroll
-        for (int v = 0; v < 8; ++v) {
-            const h2 y = {(_Float16)e[2 * v], (_Float16)e[2 * v + 1]};
-            p[v] = __builtin_bit_cast(uint32_t, y);
-        }
-    };
-    // The product with 32 tokens' values (of sub) and the scores of 32 later tokens (keys), in turn: neither waits for
-    // itself, and the exponentials that come next in program order do not depend on them.
-    auto products = [&](const uint8_t *sub, const uint32_t (&p)[8], const uint8_t *keys_at, f32x16 &s) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) s[v] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < C::F; ++i) {
-            const int x = i % VT, kc = i / VT;
-            o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                *reinterpret_cast<const h8 *>(sub + (C::F + 2 * x + kc) * 1024 + lane * 16),
-                frag(p[4 * kc], p[4 * kc + 1], p[4 * kc + 2], p[4 * kc + 3]), o[x], 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8 *>(keys_at + i * 1024 + turned[i / (C::F / 4)]), qf[i], s, 0, 0, 0);
-        }
-    };
-    auto values = [&](const uint8_t *sub, const uint32_t (&p)[8]) {
-#pragma unroll
-        for (int kc = 0; kc < 2; ++kc)
-#pragma unroll
-            for (int x = 0; x < VT; ++x)
-                o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                    *reinterpret_cast<const h8 *>(sub + (C::F + 2 * x + kc) * 1024 + lane * 16),
-                    frag(p[4 * kc], p[4 * kc + 1], p[4 * kc + 2], p[4 * kc + 3]), o[x], 0, 0, 0);
+        for (int v = 0; v < 8; ++v) p[v] = w[v];
     };
 
     const int steps = t1 > t0 ? (t1 - t0 + 63) / 64 : 0;
@@ -690,18 +692,26 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         int page = page_of(t0 + 192), t = t0;
         __syncthreads();
         f32x16 s0, s1;
-        scores(stage(0), s0);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s0[v] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C::F; ++i) s0 = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand(ring, ring, 2 * i + 1), qf[i], s0, 0, 0, 0);
         uint32_t p[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        const uint8_t *before = stage(0) + C::kSub;                     // no weights yet
-        auto step = [&](auto edge) {
-            const uint8_t *now = stage(slot);
+        const uint8_t *before = ring + C::kSub;                          // no weights yet
+#pragma unroll
+        for (int m = 0; m < 4; ++m) ops[m] = operand(before, ring + C::kSub, m);
+        auto turn = [&]() __attribute__((always_inline)) {
             unpack(t + 128, stage(slot + 2));
             fetch(t + 192, page);
             page = page_of(t + 256);
-            products(before, p, now + C::kSub, s1);
-            weigh(t, s0, p, edge);
-            products(now, p, stage(slot + 1), s0);
-            weigh(t + 32, s1, p, edge);
+        };
+        // the waves of a SIMD (one with keys, one with values) unpack in different halves of a step
+        auto step = [&](auto edge) __attribute__((always_inline)) {
+            const uint8_t *now = stage(slot), *next = stage(slot + 1);
+            if (keys) turn();
+            block(before, now + C::kSub, now, next, t, s0, s1, p, edge);
+            if (!keys) turn();
+            block(now, next, now + C::kSub, next + C::kSub, t + 32, s1, s0, p, edge);
             before = now + C::kSub;
             ++slot;
             t += 64;
@@ -710,7 +720,12 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         const int open = t1 < wsee_least ? t1 : wsee_least;              // steps below it hide nothing from this wave
         while (t + 64 <= open) step(std::false_type{});
         while (t < t1) step(std::true_type{});
-        values(before, p);
+#pragma unroll
+        for (int i = 0; i < C::F; ++i) {
+            const int x = i % VT, kc = i / VT;
+            o[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand(before, before, 2 * i),
+                                                          frag(p[4 * kc], p[4 * kc + 1], p[4 * kc + 2], p[4 * kc + 3]), o[x], 0, 0, 0);
+        }
         __syncthreads();
     }
 #pragma unroll
