@@ -531,10 +531,14 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     uint32_t zw[4], zs = 0;
     bool z_in = true;                    // the page lies in the cache (looked at when the loads have long been issued)
     auto page_of = [&](int t) {
+        // a vector load: a scalar one would share the counter that the operand reads are waited for with
         const int tt = t + 16 * (wave & 3);
-        return tt < t1 ? __builtin_amdgcn_readfirstlane(table[tt >> plog]) : 0;
+        int at = tt < t1 ? tt >> plog : 0;
+        asm volatile("" : "+v"(at));
+        return table[at];
     };
-    auto fetch = [&](int t, int page) __attribute__((always_inline)) {
+    auto fetch = [&](int t, int entry) __attribute__((always_inline)) {
+        const int page = t + 16 * (wave & 3) < t1 ? __builtin_amdgcn_readfirstlane(entry) : 0;
         z_in = page >= 0 && page < a.c.pages;                            // uniform
         const int64_t run = a.c.run(z_in ? page : 0, h) + ((t + 16 * (wave & 3)) & pmask);
         const uint8_t *p = codes + run * (D / 2) + code_at, *q = scales + run * (D / 16) + scale_at;
@@ -623,8 +627,12 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
                 if (t + 8 * (v >> 2) + 4 * up + (v & 3) >= see) s[v] = -__builtin_inff();
         }
         constexpr int kOps = 2 * C::F, kEach = 16 / kOps;
+        auto pack = [](float a, float b) {
+            const h2 z = {(_Float16)a, (_Float16)b};
+            return __builtin_bit_cast(uint32_t, z);
+        };
         uint32_t w[8];
-        float total = 0.0f, last = 0.0f;
+        float total = 0.0f, e[2], arg = __builtin_fmaf(s[0], c, -ref);
 #pragma unroll
         for (int v = 0; v < 16; ++v) ahead[v] = 0.0f;
         __builtin_amdgcn_sched_barrier(0);
@@ -637,16 +645,16 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
 #pragma unroll
             for (int y = 0; y < kEach; ++y) {
                 const int v = m * kEach + y;
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -ref));
-                total += e;
-                if (v & 1) {
-                    const h2 z = {(_Float16)last, (_Float16)e};
-                    w[v >> 1] = __builtin_bit_cast(uint32_t, z);
-                }
-                last = e;
+                const float now = __builtin_amdgcn_exp2f(arg);           // used one element later: it takes a while
+                if (v < 15) arg = __builtin_fmaf(s[(v + 1) & 15], c, -ref);
+                if (v > 0) total += e[(v - 1) & 1];
+                if (v > 0 && !(v & 1)) w[(v - 2) >> 1] = pack(e[0], e[1]);
+                e[v & 1] = now;
             }
             __builtin_amdgcn_sched_barrier(0);
         });
+        total += e[1];
+        w[7] = pack(e[0], e[1]);
         if (__any(total > kMostSum)) {
             const bool need = __builtin_fmaxf(total, __shfl_xor(total, 32, 64)) > kMostSum;   // a row moves by its own scores alone
             float top = s[0];
@@ -668,8 +676,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
                 const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v + 1], c, -ref));
                 total += e0;
                 total += e1;
-                const h2 z = {(_Float16)e0, (_Float16)e1};
-                w[v >> 1] = __builtin_bit_cast(uint32_t, z);
+                w[v >> 1] = pack(e0, e1);
             }
         }
         sum += total;
