@@ -262,19 +262,32 @@ inline int pick_w4a16(int64_t M, int64_t N, int64_t K, int64_t ldx) {
 
 // How a call is cut: rows (queries x heads of a group) into qtiles of 16 x tiles, tokens into splits of `chunk`.
 struct Kv4Plan {
-    int tiles, qtiles, splits, chunk;
+    int tiles, qtiles, waves, splits, chunk;
 };
+constexpr int kKv4MaxSplits = 256;      // what the join takes
 
+#ifndef KVWD
+#define KVWD 512
+#endif
+#ifndef KVONE
+#define KVONE 1024
+#endif
 inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads) {
     Kv4Plan p;
     const int64_t rows = max_q * (q_heads / kv_heads);
     p.tiles = rows > 32 ? 16 : rows > 16 ? 2 : 1;
     p.qtiles = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
     const int64_t groups = B * kv_heads * p.qtiles;
-    const int64_t want = p.tiles == 16 ? 256 : 1024;
+    const int64_t want = p.tiles == 16 ? 256 : KVWD;
+    p.waves = 4;
     int64_t splits = groups > 0 ? (want + groups - 1) / groups : 1;
+    if (p.tiles == 1 && max_kv <= KVONE && groups <= 256) {
+        p.waves = 8;
+        splits = 1;
+    }
     const int64_t most = (max_kv + 255) / 256;
     splits = splits > most ? most : splits;
+    splits = splits > kKv4MaxSplits ? kKv4MaxSplits : splits;
     splits = splits < 1 ? 1 : splits;
     const int64_t chunk = ((max_kv + splits - 1) / splits + 127) / 128 * 128;
     p.chunk = (int)(chunk < 128 ? 128 : chunk > 0x7FFFFF80 ? 0x7FFFFF80 : chunk);

@@ -28,8 +28,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kCodeMask = 0x80708070u;    // sign and magnitude of a code in either half word
 constexpr float kScaleUp = 128.0f;             // FP16 scales are s 2^7
-constexpr float kBelow = 7.0f, kSlack = 8.0f;  // r = maximum - kBelow, renewed when the maximum has grown by kSlack
-constexpr float kMostSum = 32768.0f;           // 2^(kBelow + kSlack): no single weight above it
+constexpr float kBelow = 7.0f;                 // r = maximum - kBelow when it is renewed
+constexpr float kMostSum = 32768.0f;           // ... which it is when a lane's weights of a step sum to more: none is above
 constexpr int kNoToken = 0x7FFFFFFF;
 constexpr float kLowest = -3.4028234663852886e38f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -97,8 +97,9 @@ template <int D> struct Step {
     bool in[2];                          // the page lies in the cache (looked at when the loads have long been issued)
 };
 
+
 template <int D, int NT, int W>
-__global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a, int qtiles, int splits, int chunk) {
+__global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs a, int qtiles, int splits, int chunk) {
     constexpr int KW = D / 32, VT = D / 16;
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -196,26 +197,28 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
             const bool in = p[u] >= 0 && p[u] < a.c.pages;             // uniform
             const int tok = (t + 16 * u) & pmask;
             const int64_t run = a.c.run(in ? p[u] : 0, h) + tok;      // tokens (values: a multiple of 4 of them)
-            const uint8_t *kp = a.c.kc + run * (D / 2) + k_at, *vp = a.c.vc + run * (D / 2) + v_at;
+            const uint8_t *kb = a.c.kc + run * (D / 2), *vb = a.c.vc + run * (D / 2);
+            const uint8_t *ksb = a.c.ks + run * (D / 16), *vsb = a.c.vs + run * (D / 16);
+            const uint8_t *kp = kb + k_at, *vp = vb + v_at;
             if constexpr (D == 128) {
                 const uint4 x = *reinterpret_cast<const uint4 *>(kp);
                 st.k[u][0] = x.x;
                 st.k[u][1] = x.y;
                 st.k[u][2] = x.z;
                 st.k[u][3] = x.w;
-                st.ks[u] = *reinterpret_cast<const uint16_t *>(a.c.ks + run * (D / 16) + ks_at);
+                st.ks[u] = *reinterpret_cast<const uint16_t *>(ksb + ks_at);
             } else {
                 const uint2 x = *reinterpret_cast<const uint2 *>(kp);
                 st.k[u][0] = x.x;
                 st.k[u][1] = x.y;
-                st.ks[u] = a.c.ks[run * (D / 16) + ks_at];
+                st.ks[u] = ksb[ks_at];
             }
             const uint4 y = *reinterpret_cast<const uint4 *>(vp);
             st.v[u][0] = y.x;
             st.v[u][1] = y.y;
             st.v[u][2] = y.z;
             st.v[u][3] = y.w;
-            st.vs[u] = *reinterpret_cast<const uint32_t *>(a.c.vs + run * (D / 16) + vs_at);
+            st.vs[u] = *reinterpret_cast<const uint32_t *>(vsb + vs_at);
             st.in[u] = in;
         }
     };
@@ -267,12 +270,19 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
         uint32_t p[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float top = s[0][n][0];
+            float e[8], total = 0.0f;
 #pragma unroll
-            for (int i = 1; i < 8; ++i) top = __builtin_fmaxf(top, s[i >> 2][n][i & 3]);
-            if (__any(__builtin_fmaf(top, c[n], -ref[n]) > kBelow + kSlack)) {
-                const float m = max16(top);                            // a row moves by its own scores alone
-                const float next = __builtin_fmaf(m, c[n], -ref[n]) > kBelow + kSlack ? m * c[n] - kBelow : ref[n];
+            for (int i = 0; i < 8; ++i) {
+                e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][n][i & 3], c[n], -ref[n]));
+                total += e[i];
+            }
+            if (__any(total > kMostSum)) {
+                const bool need = max16(total) > kMostSum;              // a row moves by its own scores alone
+                float top = s[0][n][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top = __builtin_fmaxf(top, s[i >> 2][n][i & 3]);
+                top = max16(top);
+                const float next = need ? top * c[n] - kBelow : ref[n];
                 const float f = __builtin_amdgcn_exp2f(ref[n] - next);
                 ref[n] = next;
                 sum[n] *= f;
@@ -280,16 +290,18 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
                 for (int x = 0; x < VT; ++x)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[x][n][i] *= f;
+                total = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][n][i & 3], c[n], -ref[n]));
+                    total += e[i];
+                }
             }
+            sum[n] += total;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float e[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][n][i], c[n], -ref[n]));
-                sum[n] += (e[0] + e[1]) + (e[2] + e[3]);
-                const h2 lo = {(_Float16)e[0], (_Float16)e[1]}, hi = {(_Float16)e[2], (_Float16)e[3]};
-                p[n][2 * u] = __builtin_bit_cast(uint32_t, lo);
-                p[n][2 * u + 1] = __builtin_bit_cast(uint32_t, hi);
+            for (int i = 0; i < 4; ++i) {
+                const h2 z = {(_Float16)e[2 * i], (_Float16)e[2 * i + 1]};
+                p[n][i] = __builtin_bit_cast(uint32_t, z);
             }
         }
         h2 sv[2][2];
@@ -357,11 +369,11 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
                     if ((i < 2 ? first : second) < see[n]) o[x][n][i] = __builtin_nanf("");
     }
 
-    // join the waves: references and sums first, then the rows through LDS
+    // Join the waves: references and sums first, then the rows through LDS.  `finish` turns a row's joined sum into
+    // its output; a split leaves its rows as they are, with their reference and sum of weights beside them.
     constexpr int kLd = D + 4;
     __shared__ float part[W][16][kLd];
-    __shared__ float refs[W][16 * NT], sums[W][16 * NT];
-    const float gv = *a.c.gv * 4096.0f;
+    __shared__ float refs[W][16 * NT], sums[W][16 * NT], finish[16 * NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         sum[n] = sum16(sum[n]);
@@ -371,10 +383,32 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
         }
     }
     __syncthreads();
+    float *po = reinterpret_cast<float *>(a.workspace);
+    const int64_t all = a.T * a.q_heads;
+    if (threadIdx.x < 16 * NT && row0 + (int)threadIdx.x < rows) {
+        const int row = row0 + threadIdx.x, i = row / group;
+        const int64_t at = (sq.q0 + i) * a.q_heads + h * group + (row - i * group);
+        float top = kLowest, total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = __builtin_fmaxf(top, refs[w][threadIdx.x]);
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            total = __builtin_fmaf(sums[w][threadIdx.x], __builtin_amdgcn_exp2f(refs[w][threadIdx.x] - top), total);
+        if (splits > 1) {
+            float *pm = po + (int64_t)splits * all * D + 2 * (split * all + at);
+            pm[0] = top;
+            pm[1] = total;
+        } else {
+            const bool none = visible(a, sq, i) == 0 && !sq.lost;
+            finish[threadIdx.x] = sq.lost ? __builtin_nanf("") : none ? 0.0f : *a.c.gv * 4096.0f / total;
+            if (a.lse) a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (top + __builtin_log2f(total)) * kLn2;
+        }
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        float m = kLowest;
-        for (int w = 0; w < W; ++w) m = __builtin_fmaxf(m, refs[w][16 * n + r]);
+        float m = refs[0][16 * n + r];
+#pragma unroll
+        for (int w = 1; w < W; ++w) m = __builtin_fmaxf(m, refs[w][16 * n + r]);
         const float f = __builtin_amdgcn_exp2f(ref[n] - m);
         if (n > 0) __syncthreads();
 #pragma unroll
@@ -387,32 +421,21 @@ __global__ __launch_bounds__(64 * W) void kv4_decode_kernel(const Kv4AttnArgs a,
             }
         __syncthreads();
         const int have = rows - row0 - 16 * n;
-        for (int x = threadIdx.x; x < (have < 16 ? have : 16) * D; x += 64 * W) {
-            const int rr = x / D, ch = x % D;
-            float top = kLowest;
-            for (int w = 0; w < W; ++w) top = __builtin_fmaxf(top, refs[w][16 * n + rr]);
-            float total = 0.0f, y = 0.0f;
+        for (int x = threadIdx.x; x < (have < 16 ? have : 16) * (D / 2); x += 64 * W) {
+            const int rr = x / (D / 2), ch = x % (D / 2) * 2;
+            float y0 = 0.0f, y1 = 0.0f;
+#pragma unroll
             for (int w = 0; w < W; ++w) {
-                total = __builtin_fmaf(sums[w][16 * n + rr], __builtin_amdgcn_exp2f(refs[w][16 * n + rr] - top), total);
-                y += part[w][rr][ch];
+                y0 += part[w][rr][ch];
+                y1 += part[w][rr][ch + 1];
             }
-            const int row = row0 + 16 * n + rr, i = row / group;
-            const int64_t at = (sq.q0 + i) * a.q_heads + h * group + (row - i * group);
+            const int row = row0 + 16 * n + rr, i = row / group, hq = h * group + (row - i * group);
             if (splits > 1) {
-                float *po = reinterpret_cast<float *>(a.workspace);
-                float *pm = po + (int64_t)splits * a.T * a.q_heads * D;
-                const int64_t slot = (int64_t)split * a.T * a.q_heads + at;
-                po[slot * D + ch] = y;
-                if (ch == 0) {
-                    pm[2 * slot] = top;
-                    pm[2 * slot + 1] = total;
-                }
+                *reinterpret_cast<float2 *>(po + (split * all + (sq.q0 + i) * a.q_heads + hq) * D + ch) = make_float2(y0, y1);
             } else {
-                const bool none = visible(a, sq, i) == 0 && !sq.lost;
-                const float out = sq.lost ? __builtin_nanf("") : none ? 0.0f : y * gv / total;
-                a.out[(sq.q0 + i) * a.ldo + (int64_t)(h * group + (row - i * group)) * D + ch] = (uint16_t)bf16_rne_from_float(out);
-                if (a.lse && ch == 0)
-                    a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (top + __builtin_log2f(total)) * kLn2;
+                const float f1 = finish[16 * n + rr];
+                *reinterpret_cast<uint32_t *>(a.out + (sq.q0 + i) * a.ldo + (int64_t)hq * D + ch) =
+                    bf16_rne_from_float(y0 * f1) | (bf16_rne_from_float(y1 * f1) << 16);
             }
         }
     }
@@ -784,56 +807,71 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     }
 }
 
-// Joins the splits of a row: one workgroup of W waves per query and head, the waves take the splits in turn.
-template <int D, int W>
+// Joins the splits of a row: one workgroup of W waves per query and head, a wave up to S of the splits.  Every load
+// is on its way before the first is waited for; what was not written is not used.
+template <int D, int W, int S>
 __global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, int splits, int chunk) {
     constexpr int C = D / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hq = blockIdx.x % a.q_heads;
     const int64_t bi = blockIdx.x / a.q_heads;
     const int i = (int)(bi % a.max_q), b = (int)(bi / a.max_q);
     const Seq sq = sequence(a, b);
     if (i >= sq.nq) return;
-    const int n = visible(a, sq, i);
-    // the splits that a workgroup of the row's tile has written: those before the last token that the row sees
-    const int have = sq.lost ? 0 : (n + chunk - 1) / chunk;
     const int64_t at = (sq.q0 + i) * a.q_heads + hq, all = a.T * a.q_heads;
     const float *po = reinterpret_cast<const float *>(a.workspace);
     const float *pm = po + (int64_t)splits * all * D;
-    float m = kLowest;
-    for (int s = lane; s < have; s += 64) m = __builtin_fmaxf(m, pm[2 * (s * all + at)]);
-    for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off, 64));
-    float total = 0.0f, y[C] = {};
-#pragma unroll 8
-    for (int s = wave; s < have; s += W) {
-        const int64_t slot = s * all + at;
-        const float f = __builtin_amdgcn_exp2f(pm[2 * slot] - m);
-        total = __builtin_fmaf(pm[2 * slot + 1], f, total);
+    float ref[S], weight[S], y[S][C];
 #pragma unroll
-        for (int e = 0; e < C; ++e) y[e] = __builtin_fmaf(po[slot * D + lane * C + e], f, y[e]);
+    for (int k = 0; k < S; ++k) {
+        const int s = wave + k * W;
+        const int64_t slot = (s < splits ? s : 0) * all + at;
+        ref[k] = pm[2 * slot];
+        weight[k] = pm[2 * slot + 1];
+#pragma unroll
+        for (int e = 0; e < C; ++e) y[k][e] = po[slot * D + lane * C + e];
     }
-    if constexpr (W > 1) {
-        __shared__ float part[W][C + 1][64];
+    const int n = visible(a, sq, i);
+    const int have = sq.lost ? 0 : (n + chunk - 1) / chunk;              // the splits with a token that the row sees
+    float m = kLowest;
 #pragma unroll
-        for (int e = 0; e < C; ++e) part[wave][e][lane] = y[e];
+    for (int k = 0; k < S; ++k)
+        if (wave + k * W < have) m = __builtin_fmaxf(m, ref[k]);
+    float total = 0.0f, z[C] = {};
+#pragma unroll
+    for (int k = 0; k < S; ++k)
+        if (wave + k * W < have) {
+            const float f = __builtin_amdgcn_exp2f(ref[k] - m);
+            total = __builtin_fmaf(weight[k], f, total);
+#pragma unroll
+            for (int e = 0; e < C; ++e) z[e] = __builtin_fmaf(y[k][e], f, z[e]);
+        }
+    if constexpr (W > 1) {
+        __shared__ float part[W][C + 2][64];
+#pragma unroll
+        for (int e = 0; e < C; ++e) part[wave][e][lane] = z[e];
         part[wave][C][lane] = total;
+        part[wave][C + 1][lane] = m;
         __syncthreads();
         if (wave > 0) return;
-        for (int w = 1; w < W; ++w) {
 #pragma unroll
-            for (int e = 0; e < C; ++e) y[e] += part[w][e][lane];
-            total += part[w][C][lane];
+        for (int w = 1; w < W; ++w) m = __builtin_fmaxf(m, part[w][C + 1][lane]);
+        total = 0.0f;
+#pragma unroll
+        for (int e = 0; e < C; ++e) z[e] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float f = __builtin_amdgcn_exp2f(part[w][C + 1][lane] - m);
+            total = __builtin_fmaf(part[w][C][lane], f, total);
+#pragma unroll
+            for (int e = 0; e < C; ++e) z[e] = __builtin_fmaf(part[w][e][lane], f, z[e]);
         }
     }
-    const float gv = *a.c.gv * 4096.0f;
     const bool none = n == 0 && !sq.lost;
-    uint32_t bits[C];
-#pragma unroll
-    for (int e = 0; e < C; ++e)
-        bits[e] = bf16_rne_from_float(sq.lost ? __builtin_nanf("") : none ? 0.0f : y[e] * gv / total);
+    const float f = sq.lost ? __builtin_nanf("") : none ? 0.0f : *a.c.gv * 4096.0f / total;
     uint16_t *dst = a.out + (sq.q0 + i) * a.ldo + (int64_t)hq * D + lane * C;
-    if constexpr (C == 2) *reinterpret_cast<uint32_t *>(dst) = bits[0] | (bits[1] << 16);
-    else dst[0] = (uint16_t)bits[0];
+    if constexpr (C == 2) *reinterpret_cast<uint32_t *>(dst) = bf16_rne_from_float(z[0] * f) | (bf16_rne_from_float(z[1] * f) << 16);
+    else dst[0] = (uint16_t)bf16_rne_from_float(z[0] * f);
     if (a.lse && lane == 0)
         a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (m + __builtin_log2f(total)) * kLn2;
 }
@@ -845,13 +883,16 @@ template <int D, int NT, int W> void decode(const Kv4AttnArgs &a, const Kv4Plan 
 
 template <int D> void join(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
     const unsigned n = (unsigned)(a.B * a.max_q * a.q_heads);
-    if (p.splits <= 8) kv4_join_kernel<D, 1><<<n, 64, 0, stream>>>(a, p.splits, p.chunk);
-    else if (p.splits <= 32) kv4_join_kernel<D, 4><<<n, 256, 0, stream>>>(a, p.splits, p.chunk);
-    else kv4_join_kernel<D, 8><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
+    if (p.splits <= 4) kv4_join_kernel<D, 1, 4><<<n, 64, 0, stream>>>(a, p.splits, p.chunk);
+    else if (p.splits <= 16) kv4_join_kernel<D, 4, 4><<<n, 256, 0, stream>>>(a, p.splits, p.chunk);
+    else if (p.splits <= 64) kv4_join_kernel<D, 8, 8><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
+    else kv4_join_kernel<D, 16, 16><<<n, 1024, 0, stream>>>(a, p.splits, p.chunk);
 }
 
 template <int D> hipError_t attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
-    if (p.tiles == 1) {
+    if (p.tiles == 1 && p.waves == 8) {
+        decode<D, 1, 8>(a, p, stream);
+    } else if (p.tiles == 1) {
         decode<D, 1, 4>(a, p, stream);
     } else if (p.tiles == 2) {
         decode<D, 2, 4>(a, p, stream);
