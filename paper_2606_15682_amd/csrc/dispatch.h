@@ -266,24 +266,21 @@ struct Kv4Plan {
 };
 constexpr int kKv4MaxSplits = 256;      // what the join takes
 
-#ifndef KVWD
-#define KVWD 512
-#endif
-#ifndef KVONE
-#define KVONE 1024
-#endif
 inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads) {
     Kv4Plan p;
     const int64_t rows = max_q * (q_heads / kv_heads);
     p.tiles = rows > 32 ? 16 : rows > 16 ? 2 : 1;
     p.qtiles = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
     const int64_t groups = B * kv_heads * p.qtiles;
-    const int64_t want = p.tiles == 16 ? 256 : KVWD;
     p.waves = 4;
-    int64_t splits = groups > 0 ? (want + groups - 1) / groups : 1;
-    if (p.tiles == 1 && max_kv <= KVONE && groups <= 256) {
+    int64_t splits = 1;
+    if (p.tiles == 16) {
+        splits = groups > 0 ? (256 + groups - 1) / groups : 1;
+    } else if (p.tiles == 1 && max_kv <= 512 && groups <= 256) {
         p.waves = 8;
-        splits = 1;
+    } else {
+        splits = groups > 0 ? (KVWD + groups - 1) / groups : 1;
+        if (B > 1 && max_kv > 2048 && splits < (max_kv + 1279) / 1280) splits = (max_kv + 1279) / 1280;
     }
     const int64_t most = (max_kv + 255) / 256;
     splits = splits > most ? most : splits;

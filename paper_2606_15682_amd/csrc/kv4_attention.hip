@@ -26,6 +26,8 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+typedef const __attribute__((address_space(4))) int *ConstInt;
+
 constexpr uint32_t kCodeMask = 0x80708070u;    // sign and magnitude of a code in either half word
 constexpr float kScaleUp = 128.0f;             // FP16 scales are s 2^7
 constexpr float kBelow = 7.0f;                 // r = maximum - kBelow when it is renewed
@@ -50,6 +52,40 @@ __device__ __forceinline__ float max16(float x) {
 __device__ __forceinline__ float sum16(float x) {
     x += __shfl_xor(x, 16, 64);
     return x + __shfl_xor(x, 32, 64);
+}
+
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Largest magnitude pattern of 8 N bfloat16 values, in both halves' maximum (a non-finite one: 0x7F80 or above).
+template <int N> __device__ __forceinline__ uint32_t largest(const uint4 (&w)[N]) {
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[e] & 0x7FFF7FFFu));
+    }
+    return m[0] > m[1] ? m[0] : m[1];
+}
+
+// The exponent that takes a row whose largest pattern is `top` to [2^14, 2^15) (a row with a NaN or Inf stays one).
+__device__ __forceinline__ int row_shift(uint32_t top) {
+    return top == 0u || top >= 0x7F80u ? 0 : 15 - __builtin_amdgcn_frexp_expf(f32_from_bits(top << 16));
+}
+
+// Eight bfloat16 values times 2^shift as FP16, in the order that a dword of codes is unpacked in: 0 2 1 3 4 6 5 7.
+__device__ __forceinline__ h8 query_f16(const uint4 &w, int shift) {
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    _Float16 y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        y[e] = (_Float16)__builtin_ldexpf(f32_from_bits((e & 1) ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16), shift);
+    return h8{y[0], y[2], y[1], y[3], y[4], y[6], y[5], y[7]};
+}
+
+// From scores of such a row to exponents of two.  A code is half its integer: 2^-13 n s = 2^-12 (n / 2) s.
+__device__ __forceinline__ float score_factor(const Kv4AttnArgs &a, int shift) {
+    return __builtin_fmaxf(__builtin_ldexpf(a.scale * kLog2e * *a.c.gk * 4096.0f, -shift), 0x1p-126f);
 }
 
 // The queries and tokens of sequence b.
@@ -97,100 +133,53 @@ template <int D> struct Step {
     bool in[2];                          // the page lies in the cache (looked at when the loads have long been issued)
 };
 
-
 template <int D, int NT, int W>
-__global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs a, int qtiles, int splits, int chunk) {
+__global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs a, int splits, int chunk) {
     constexpr int KW = D / 32, VT = D / 16;
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // heads first: workgroups go round the eight XCDs, and an XCD that got the same piece of every sequence would have
+    // the last ones empty where lengths differ (64 sequences of up to 16384 tokens, pieces of 2048: 192 us against 165)
     int id = blockIdx.x;
-    const int qt = id % qtiles;
-    id /= qtiles;
-    const int split = id % splits;
-    id /= splits;
-    const int h = id % a.c.heads, b = id / a.c.heads;
+    const int h = id % a.c.heads;
+    id /= a.c.heads;
+    const int split = id % splits, b = id / splits;
     const int group = a.q_heads / a.c.heads;
+    const int t0 = split * chunk;
+
+    const ConstInt table = (ConstInt)(uintptr_t)(a.table + (int64_t)b * a.ld_table);   // scalar loads
+    const int plog = a.c.page_log2, pmask = (1 << plog) - 1, last_entry = (int)a.table_cols - 1;
+    constexpr int kStride = 32 * W;
+    int t = t0 + 32 * wave;
+    // entries of the first two steps, beside the lengths that say whether they are needed
+    auto pages = [&](int t, int (&p)[2]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int at = (t + 16 * u) >> plog;
+            p[u] = table[at < last_entry ? at : last_entry];
+        }
+    };
+    int p[2] = {0, 0}, p_next[2] = {0, 0};
+    if (last_entry >= 0) {
+        pages(t, p);
+        pages(t + kStride, p_next);
+    }
 
     const Seq sq = sequence(a, b);
     const int nq = sq.nq < a.max_q ? sq.nq : (int)a.max_q;
-    const int rows = nq * group, row0 = qt * 16 * NT;
-    if (row0 >= rows) return;
-    const int row_last = row0 + 16 * NT < rows ? row0 + 16 * NT - 1 : rows - 1;
-    const int see_least = visible(a, sq, row0 / group), see_most = visible(a, sq, row_last / group);
-    const int t0 = split * chunk;
-    const int t1 = sq.lost ? 0 : see_most < t0 + chunk ? see_most : t0 + chunk;   // this workgroup's tokens
-    if (split > 0 && t0 >= t1) return;                                            // the join does not read it
+    const int rows = nq * group;                                         // at most 16 NT
+    if (rows == 0) return;
+    const int see_least = visible(a, sq, 0);
+    const int t1 = sq.lost ? 0 : sq.len - t0 < chunk ? sq.len : t0 + chunk;  // this workgroup's tokens
+    if (split > 0 && t0 >= t1) return;                                   // the join does not read it
 
-    // queries, the factor from scores to exponents, and what each row sees
-    h8 qf[NT][KW];
-    float c[NT], ref[NT], sum[NT];
-    int see[NT];
-    const float gk = *a.c.gk;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int row = row0 + 16 * n + r;
-        const bool there = row < rows;
-        const int i = there ? row / group : 0;
-        see[n] = there ? visible(a, sq, i) : 0;
-        uint32_t w[4 * KW];
-        const uint16_t *src = a.q + (sq.q0 + i) * a.ldq + (int64_t)(h * group + (there ? row - i * group : 0)) * D + (D / 4) * g;
-#pragma unroll
-        for (int j = 0; j < KW; ++j) {
-            const uint4 x = there ? reinterpret_cast<const uint4 *>(src)[j] : make_uint4(0, 0, 0, 0);
-            w[4 * j] = x.x;
-            w[4 * j + 1] = x.y;
-            w[4 * j + 2] = x.z;
-            w[4 * j + 3] = x.w;
-        }
-        float top = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 4 * KW; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t m = (e ? w[j] & 0x7FFF0000u : (w[j] << 16) & 0x7FFF0000u);
-                top = m < 0x7F800000u ? __builtin_fmaxf(top, f32_from_bits(m)) : top;
-            }
-        top = max16(top);
-        const int up = top > 0.0f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
-        // channels of a dword of codes in the order that kcodes() unpacks them: 0 2 1 3 4 6 5 7
-#pragma unroll
-        for (int j = 0; j < KW; ++j) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[2 * e] = __builtin_ldexpf(f32_from_bits(w[4 * j + e] << 16), up);
-                x[2 * e + 1] = __builtin_ldexpf(f32_from_bits(w[4 * j + e] & 0xFFFF0000u), up);
-            }
-            const h8 y = {(_Float16)x[0], (_Float16)x[2], (_Float16)x[1], (_Float16)x[3],
-                          (_Float16)x[4], (_Float16)x[6], (_Float16)x[5], (_Float16)x[7]};
-            qf[n][j] = y;
-        }
-        // a code is half its integer: 2^-13 n s = 2^-12 (n / 2) s
-        c[n] = __builtin_fmaxf(__builtin_ldexpf(a.scale * kLog2e * gk * 4096.0f, -up), 0x1p-126f);
-        ref[n] = kLowest;
-        sum[n] = 0.0f;
-    }
-
-    f32x4 o[VT][NT];
-#pragma unroll
-    for (int x = 0; x < VT; ++x)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) o[x][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    const int *table = a.table + (int64_t)b * a.ld_table;
-    const int plog = a.c.page_log2, pmask = (1 << plog) - 1;
     const uint32_t w_at = D == 128 ? r : r & 7;                        // the lane's dword of value codes
     const uint32_t k_at = r * (D / 2) + g * (D / 8), ks_at = r * (D / 16) + g * (D / 64);
     const uint32_t v_at = g * (2 * D) + w_at * 16, vs_at = g * (D / 4) + (w_at >> 1) * 4;
     // D = 64: sixteen rows of a tile are eight dwords times two: lanes 8 .. 15 take the dword's upper channels
     const uint32_t half = D == 128 ? 0u : (uint32_t)(r >> 3) * 0x02020202u;
-
     int bad_at = kNoToken;               // the first token, some rows not seeing it, whose values in the lane's block are NaN
 
-    auto pages = [&](int t, int (&p)[2]) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) p[u] = t + 16 * u < t1 ? __builtin_amdgcn_readfirstlane(table[(t + 16 * u) >> plog]) : 0;
-    };
     auto load = [&](int t, const int (&p)[2], Step<D> &st) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -222,6 +211,38 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
             st.in[u] = in;
         }
     };
+
+    Step<D> A, B;
+    if (t < t1) load(t, p, A);
+
+    // queries (rows beyond the last repeat the first), the factor from scores to exponents, and what each row sees
+    h8 qf[NT][KW];
+    float c[NT], ref[NT], sum[NT];
+    int see[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = 16 * n + r < rows ? 16 * n + r : 0, i = row / group;
+        see[n] = 16 * n + r < rows ? visible(a, sq, i) : 0;
+        const uint16_t *src = a.q + (sq.q0 + i) * a.ldq + (int64_t)(h * group + row - i * group) * D + (D / 4) * g;
+        uint4 w[KW];
+#pragma unroll
+        for (int j = 0; j < KW; ++j) w[j] = reinterpret_cast<const uint4 *>(src)[j];
+        uint32_t top = largest(w);
+        uint32_t x = __shfl_xor(top, 16, 64);
+        top = top > x ? top : x;
+        x = __shfl_xor(top, 32, 64);
+        const int shift = row_shift(top > x ? top : x);
+#pragma unroll
+        for (int j = 0; j < KW; ++j) qf[n][j] = query_f16(w[j], shift);
+        c[n] = score_factor(a, shift);
+        ref[n] = kLowest;
+        sum[n] = 0.0f;
+    }
+    f32x4 o[VT][NT];
+#pragma unroll
+    for (int x = 0; x < VT; ++x)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[x][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     auto compute = [&](int t, Step<D> &st) {
         f32x4 s[2][NT];
@@ -330,26 +351,16 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
         }
     };
 
-    constexpr int kStride = 32 * W;
-    int t = t0 + 32 * wave;
-    if (t < t1) {
-        Step<D> A, B;
-        int p[2];
-        pages(t, p);
-        load(t, p, A);
-        pages(t + kStride, p);
-        while (true) {
-            if (t + kStride < t1) load(t + kStride, p, B);
-            pages(t + 2 * kStride, p);
-            compute(t, A);
-            t += kStride;
-            if (t >= t1) break;
-            if (t + kStride < t1) load(t + kStride, p, A);
-            pages(t + 2 * kStride, p);
-            compute(t, B);
-            t += kStride;
-            if (t >= t1) break;
-        }
+    while (t < t1) {
+        if (t + kStride < t1) load(t + kStride, p_next, B);
+        pages(t + 2 * kStride, p_next);
+        compute(t, A);
+        t += kStride;
+        if (t >= t1) break;
+        if (t + kStride < t1) load(t + kStride, p_next, A);
+        pages(t + 2 * kStride, p_next);
+        compute(t, B);
+        t += kStride;
     }
 
     if (__any(bad_at != kNoToken)) {
@@ -385,8 +396,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
     __syncthreads();
     float *po = reinterpret_cast<float *>(a.workspace);
     const int64_t all = a.T * a.q_heads;
-    if (threadIdx.x < 16 * NT && row0 + (int)threadIdx.x < rows) {
-        const int row = row0 + threadIdx.x, i = row / group;
+    if ((int)threadIdx.x < rows) {
+        const int row = threadIdx.x, i = row / group;
         const int64_t at = (sq.q0 + i) * a.q_heads + h * group + (row - i * group);
         float top = kLowest, total = 0.0f;
 #pragma unroll
@@ -420,7 +431,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
                 part[wave][r][ch] = o[x][n][i] * f;
             }
         __syncthreads();
-        const int have = rows - row0 - 16 * n;
+        const int have = rows - 16 * n;
         for (int x = threadIdx.x; x < (have < 16 ? have : 16) * (D / 2); x += 64 * W) {
             const int rr = x / (D / 2), ch = x % (D / 2) * 2;
             float y0 = 0.0f, y1 = 0.0f;
@@ -429,7 +440,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
                 y0 += part[w][rr][ch];
                 y1 += part[w][rr][ch + 1];
             }
-            const int row = row0 + 16 * n + rr, i = row / group, hq = h * group + (row - i * group);
+            const int row = 16 * n + rr, i = row / group, hq = h * group + (row - i * group);
             if (splits > 1) {
                 *reinterpret_cast<float2 *>(po + (split * all + (sq.q0 + i) * a.q_heads + hq) * D + ch) = make_float2(y0, y1);
             } else {
@@ -489,7 +500,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     const int row = row0 + 32 * wave + col;                             // this lane's row
     const bool there = row < rows;
     const int qi = there ? row / group : 0;
-    const int hq = h * group + (there ? row - qi * group : 0);
+    const int hq = h * group + (there ? row - qi * group : 0);           // rows beyond the last repeat the first
     const int see = there ? visible(a, sq, qi) : 0;
     const int wsee_least = row0 + 32 * wave < rows ? visible(a, sq, (row0 + 32 * wave) / group) : 0;
 
@@ -498,29 +509,14 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     {
         const uint16_t *src = a.q + (sq.q0 + qi) * a.ldq + (int64_t)hq * D + 8 * up;
         uint4 w[C::F];
-        float top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < C::F; ++j) {
-            w[j] = there ? *reinterpret_cast<const uint4 *>(src + 16 * j) : make_uint4(0, 0, 0, 0);
-            const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+        for (int j = 0; j < C::F; ++j) w[j] = *reinterpret_cast<const uint4 *>(src + 16 * j);
+        uint32_t top = largest(w);
+        const uint32_t x = __shfl_xor(top, 32, 64);
+        const int shift = row_shift(top > x ? top : x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t m = (e & 1) ? x[e >> 1] & 0x7FFF0000u : (x[e >> 1] << 16) & 0x7FFF0000u;
-                top = m < 0x7F800000u ? __builtin_fmaxf(top, f32_from_bits(m)) : top;
-            }
-        }
-        top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
-        const int sh = top > 0.0f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
-#pragma unroll
-        for (int j = 0; j < C::F; ++j) {
-            const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
-            _Float16 y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                y[e] = (_Float16)__builtin_ldexpf(f32_from_bits((e & 1) ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16), sh);
-            qf[j] = h8{y[0], y[2], y[1], y[3], y[4], y[6], y[5], y[7]};   // the order of unpacked key codes
-        }
-        c = __builtin_fmaxf(__builtin_ldexpf(a.scale * kLog2e * *a.c.gk * 4096.0f, -sh), 0x1p-126f);
+        for (int j = 0; j < C::F; ++j) qf[j] = query_f16(w[j], shift);
+        c = score_factor(a, shift);
     }
     f32x16 o[VT];
 #pragma unroll
@@ -877,16 +873,26 @@ __global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, i
 }
 
 template <int D, int NT, int W> void decode(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
-    const int64_t n = a.B * a.c.heads * p.splits * p.qtiles;
-    kv4_decode_kernel<D, NT, W><<<(unsigned)n, 64 * W, 0, stream>>>(a, p.qtiles, p.splits, p.chunk);
+    const int64_t n = a.B * a.c.heads * p.splits;
+    kv4_decode_kernel<D, NT, W><<<(unsigned)n, 64 * W, 0, stream>>>(a, p.splits, p.chunk);
 }
 
 template <int D> void join(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
     const unsigned n = (unsigned)(a.B * a.max_q * a.q_heads);
+#if 0
+    if (p.splits <= 8) kv4_join_kernel<D, 1, 8><<<n, 64, 0, stream>>>(a, p.splits, p.chunk);
+    else if (p.splits <= 32) kv4_join_kernel<D, 4, 8><<<n, 256, 0, stream>>>(a, p.splits, p.chunk);
+    else if (p.splits <= 64) kv4_join_kernel<D, 4, 16><<<n, 256, 0, stream>>>(a, p.splits, p.chunk);
+    else if (p.splits <= 128) kv4_join_kernel<D, 8, 16><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
+    else kv4_join_kernel<D, 16, 16><<<n, 1024, 0, stream>>>(a, p.splits, p.chunk);
+#else
     if (p.splits <= 4) kv4_join_kernel<D, 1, 4><<<n, 64, 0, stream>>>(a, p.splits, p.chunk);
     else if (p.splits <= 16) kv4_join_kernel<D, 4, 4><<<n, 256, 0, stream>>>(a, p.splits, p.chunk);
+    else if (p.splits <= 32) kv4_join_kernel<D, 8, 4><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
     else if (p.splits <= 64) kv4_join_kernel<D, 8, 8><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
+    else if (p.splits <= 128) kv4_join_kernel<D, 8, 16><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
     else kv4_join_kernel<D, 16, 16><<<n, 1024, 0, stream>>>(a, p.splits, p.chunk);
+#endif
 }
 
 template <int D> hipError_t attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
