@@ -127,10 +127,16 @@ __device__ __forceinline__ int visible(const Kv4AttnArgs &a, const Seq &s, int i
 //   O^T = V^T P^T (16 channels x 16 rows, K = 32 tokens): those eight tokens are its share of the K axis, so the weights
 //     are the operand as they stand, and the cache holds the values of four tokens together.  Tile c has channels
 //     8 w + c of the dwords w.
+// A step's codes and scales wait in LDS, kDepth steps ahead, each lane's where the lane finds them again: a queue that
+// takes no registers.
 template <int D> struct Step {
     uint32_t k[2][D / 32], ks[2];
     uint32_t v[2][4], vs[2];
-    bool in[2];                          // the page lies in the cache (looked at when the loads have long been issued)
+};
+struct Queue {
+    static constexpr int kDepth = 1;
+    static constexpr int kLoads = 8;                                     // of a step, in each wave
+    static constexpr int kStage = 4 * 1024 + 4 * 256;                    // keys, values of 16 + 16 tokens; their scales
 };
 
 template <int D, int NT, int W>
@@ -151,7 +157,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
     const int plog = a.c.page_log2, pmask = (1 << plog) - 1, last_entry = (int)a.table_cols - 1;
     constexpr int kStride = 32 * W;
     int t = t0 + 32 * wave;
-    // entries of the first two steps, beside the lengths that say whether they are needed
+    // page entries of the first steps, beside the lengths that say whether they are needed
     auto pages = [&](int t, int (&p)[2]) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -159,10 +165,10 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
             p[u] = table[at < last_entry ? at : last_entry];
         }
     };
-    int p[2] = {0, 0}, p_next[2] = {0, 0};
+    int p[Queue::kDepth + 1][2] = {};
     if (last_entry >= 0) {
-        pages(t, p);
-        pages(t + kStride, p_next);
+#pragma unroll
+        for (int k = 0; k <= Queue::kDepth; ++k) pages(t + k * kStride, p[k]);
     }
 
     const Seq sq = sequence(a, b);
@@ -174,46 +180,70 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
     if (split > 0 && t0 >= t1) return;                                   // the join does not read it
 
     const uint32_t w_at = D == 128 ? r : r & 7;                        // the lane's dword of value codes
-    const uint32_t k_at = r * (D / 2) + g * (D / 8), ks_at = r * (D / 16) + g * (D / 64);
     const uint32_t v_at = g * (2 * D) + w_at * 16, vs_at = g * (D / 4) + (w_at >> 1) * 4;
+    // keys: 16 bytes and a dword of scales hold what the lane needs (D = 64: half of the 16 bytes, and lanes 32 .. load
+    // what the lower ones do)
+    const uint32_t k_at = D == 128 ? r * 64 + g * 16 : r * 32 + (g & 1) * 16, ks_at = D == 128 ? r * 8 + (g >> 1) * 4 : r * 4;
+    const uint32_t k_read = D == 128 ? lane * 16 : (r + 16 * (g >> 1)) * 16 + (g & 1) * 8;
+    const uint32_t ks_shift = D == 128 ? 16 * (g & 1) : 8 * g;
     // D = 64: sixteen rows of a tile are eight dwords times two: lanes 8 .. 15 take the dword's upper channels
     const uint32_t half = D == 128 ? 0u : (uint32_t)(r >> 3) * 0x02020202u;
     int bad_at = kNoToken;               // the first token, some rows not seeing it, whose values in the lane's block are NaN
 
-    auto load = [&](int t, const int (&p)[2], Step<D> &st) {
+    constexpr int kLd = D + 4;
+    constexpr int kParts = W < 2 ? W : 2;                                // waves whose rows are in LDS at once
+    constexpr int kQueue = W * Queue::kDepth * Queue::kStage, kPart = kParts * 16 * kLd * 4;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kQueue > kPart ? kQueue : kPart];
+    uint8_t *queue = lds + wave * (Queue::kDepth * Queue::kStage);
+    uint32_t in_bits = 0;                // two for each step on its way, the newest lowest: its pages lie in the cache
+    auto issue = [&](int t, const int (&p)[2], uint8_t *stage) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const bool in = p[u] >= 0 && p[u] < a.c.pages;             // uniform
+            in_bits = in_bits << 1 | (in ? 1u : 0u);
             const int tok = (t + 16 * u) & pmask;
             const int64_t run = a.c.run(in ? p[u] : 0, h) + tok;      // tokens (values: a multiple of 4 of them)
-            const uint8_t *kb = a.c.kc + run * (D / 2), *vb = a.c.vc + run * (D / 2);
-            const uint8_t *ksb = a.c.ks + run * (D / 16), *vsb = a.c.vs + run * (D / 16);
-            const uint8_t *kp = kb + k_at, *vp = vb + v_at;
+            g2l16(a.c.kc + run * (D / 2), k_at, stage + u * 1024);
+            g2l16(a.c.vc + run * (D / 2), v_at, stage + 2048 + u * 1024);
+            g2l4(a.c.ks + run * (D / 16), ks_at, stage + 4096 + u * 256);
+            g2l4(a.c.vs + run * (D / 16), vs_at, stage + 4608 + u * 256);
+        }
+    };
+    auto take = [&](const uint8_t *stage, uint32_t bits, Step<D> &st) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
             if constexpr (D == 128) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(kp);
+                const uint4 x = *reinterpret_cast<const uint4 *>(stage + u * 1024 + k_read);
                 st.k[u][0] = x.x;
                 st.k[u][1] = x.y;
                 st.k[u][2] = x.z;
                 st.k[u][3] = x.w;
-                st.ks[u] = *reinterpret_cast<const uint16_t *>(ksb + ks_at);
             } else {
-                const uint2 x = *reinterpret_cast<const uint2 *>(kp);
+                const uint2 x = *reinterpret_cast<const uint2 *>(stage + u * 1024 + k_read);
                 st.k[u][0] = x.x;
                 st.k[u][1] = x.y;
-                st.ks[u] = ksb[ks_at];
             }
-            const uint4 y = *reinterpret_cast<const uint4 *>(vp);
+            const uint4 y = *reinterpret_cast<const uint4 *>(stage + 2048 + u * 1024 + lane * 16);
             st.v[u][0] = y.x;
             st.v[u][1] = y.y;
             st.v[u][2] = y.z;
             st.v[u][3] = y.w;
-            st.vs[u] = *reinterpret_cast<const uint32_t *>(vsb + vs_at);
-            st.in[u] = in;
+            st.ks[u] = *reinterpret_cast<const uint32_t *>(stage + 4096 + u * 256 + lane * 4) >> ks_shift;
+            st.vs[u] = *reinterpret_cast<const uint32_t *>(stage + 4608 + u * 256 + lane * 4);
+            if (!(bits >> (1 - u) & 1u)) {                             // uniform: scores NaN, values zero
+                st.ks[u] = 0x7F7Fu;
+                st.vs[u] = 0u;
+            }
         }
     };
-
-    Step<D> A, B;
-    if (t < t1) load(t, p, A);
+    int ahead = 0;                       // steps on their way
+#pragma unroll
+    for (int k = 0; k < Queue::kDepth; ++k)
+        if (t + k * kStride < t1) {
+            issue(t + k * kStride, p[k], queue + k * Queue::kStage);
+            ++ahead;
+        }
+    int (&p_next)[2] = p[Queue::kDepth];
 
     // queries (rows beyond the last repeat the first), the factor from scores to exponents, and what each row sees
     h8 qf[NT][KW];
@@ -248,10 +278,6 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
         f32x4 s[2][NT];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            if (!st.in[u]) {                                           // uniform: scores NaN, values zero
-                st.ks[u] = 0x7F7Fu;
-                st.vs[u] = 0u;
-            }
             const h2 sc = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(st.ks[u], kScaleUp, false);
             const h2 sc0 = {sc[0], sc[0]}, sc1 = {sc[1], sc[1]};
 #pragma unroll
@@ -351,16 +377,20 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
         }
     };
 
-    while (t < t1) {
-        if (t + kStride < t1) load(t + kStride, p_next, B);
-        pages(t + 2 * kStride, p_next);
-        compute(t, A);
-        t += kStride;
-        if (t >= t1) break;
-        if (t + kStride < t1) load(t + kStride, p_next, A);
-        pages(t + 2 * kStride, p_next);
-        compute(t, B);
-        t += kStride;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    for (uint8_t *stage = queue; t < t1; t += kStride) {
+        if (ahead == Queue::kDepth) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Queue::kLoads * (Queue::kDepth - 1)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        Step<D> st;
+        take(stage, in_bits >> (2 * (ahead - 1)), st);
+        __builtin_amdgcn_s_waitcnt(0xC07F);                              // lgkmcnt(0): the stage is free
+        asm volatile("" ::: "memory");
+        const int later = t + Queue::kDepth * kStride;
+        if (later < t1) issue(later, p_next, stage);
+        else --ahead;
+        pages(later + kStride, p_next);
+        stage = stage == queue + (Queue::kDepth - 1) * Queue::kStage ? queue : stage + Queue::kStage;
+        compute(t, st);
     }
 
     if (__any(bad_at != kNoToken)) {
@@ -382,8 +412,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
 
     // Join the waves: references and sums first, then the rows through LDS.  `finish` turns a row's joined sum into
     // its output; a split leaves its rows as they are, with their reference and sum of weights beside them.
-    constexpr int kLd = D + 4;
-    __shared__ float part[W][16][kLd];
+    float (*part)[16][kLd] = reinterpret_cast<float (*)[16][kLd]>(lds);
     __shared__ float refs[W][16 * NT], sums[W][16 * NT], finish[16 * NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -422,21 +451,26 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
         for (int w = 1; w < W; ++w) m = __builtin_fmaxf(m, refs[w][16 * n + r]);
         const float f = __builtin_amdgcn_exp2f(ref[n] - m);
         if (n > 0) __syncthreads();
+        auto at = [&](int x, int i) -> float & {
+            const int rho = 4 * g + i;
+            return part[wave % kParts][r][D == 128 ? 8 * rho + x : 8 * (rho & 7) + 4 * (rho >> 3) + x];
+        };
 #pragma unroll
-        for (int x = 0; x < VT; ++x)
+        for (int round = W / kParts - 1; round >= 0; --round) {          // the later waves' rows first, the earlier add theirs
+            if (wave / kParts == round) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int rho = 4 * g + i;
-                const int ch = D == 128 ? 8 * rho + x : 8 * (rho & 7) + 4 * (rho >> 3) + x;
-                part[wave][r][ch] = o[x][n][i] * f;
+                for (int x = 0; x < VT; ++x)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) at(x, i) = round == W / kParts - 1 ? o[x][n][i] * f : __builtin_fmaf(o[x][n][i], f, at(x, i));
             }
-        __syncthreads();
+            __syncthreads();
+        }
         const int have = rows - 16 * n;
         for (int x = threadIdx.x; x < (have < 16 ? have : 16) * (D / 2); x += 64 * W) {
             const int rr = x / (D / 2), ch = x % (D / 2) * 2;
             float y0 = 0.0f, y1 = 0.0f;
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
+            for (int w = 0; w < kParts; ++w) {
                 y0 += part[w][rr][ch];
                 y1 += part[w][rr][ch + 1];
             }
@@ -466,9 +500,22 @@ template <int D> struct Prompt {
     static constexpr int kSub = 2 * F * 1024;            // 32 tokens: keys, then values
     static constexpr int kStage = 2 * kSub;
     static constexpr int kRing = 4;
-    static constexpr int kOut = 8 * 32 * D * 4;          // the rows on their way out
+    static constexpr int kOut = 8 * 32 * (D + 1) * 4;         // the rows on their way out
     static constexpr int kLds = kRing * kStage > kOut ? kRing * kStage : kOut;
 };
+
+// The sequence with the place-th longest cache (of equal ones the first): what is left to the last workgroups is short.
+// Of up to 64 sequences; more are taken as they come.  Uniform.
+__device__ __forceinline__ int longest(const Kv4AttnArgs &a, int place) {
+    if (a.B == 1 || a.B > 64) return place;
+    const int lane = threadIdx.x & 63, mine = lane < a.B ? a.kv_len[lane] : 0;
+    int before = 0;
+    for (int i = 0; i < (int)a.B; ++i) {
+        const int other = __builtin_amdgcn_readlane(mine, i);
+        before += other > mine || (other == mine && i < lane) ? 1 : 0;
+    }
+    return __builtin_ctzll(__ballot(lane < a.B && before == place));
+}
 
 template <int D>
 __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a, int qtiles, int splits, int chunk) {
@@ -483,8 +530,8 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     id /= a.c.heads;
     const int split = id % splits;
     id /= splits;
-    const int b = id % (int)a.B;
-    const int qt = qtiles - 1 - id / (int)a.B;                          // the longest rows first
+    const int qt = qtiles - 1 - id % qtiles;                            // the longest rows first,
+    const int b = longest(a, id / qtiles);                              // of the longest sequence first
     const int group = a.q_heads / a.c.heads;
 
     const Seq sq = sequence(a, b);
@@ -504,20 +551,6 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     const int see = there ? visible(a, sq, qi) : 0;
     const int wsee_least = row0 + 32 * wave < rows ? visible(a, sq, (row0 + 32 * wave) / group) : 0;
 
-    h8 qf[C::F];
-    float c, ref = kLowest, sum = 0.0f;
-    {
-        const uint16_t *src = a.q + (sq.q0 + qi) * a.ldq + (int64_t)hq * D + 8 * up;
-        uint4 w[C::F];
-#pragma unroll
-        for (int j = 0; j < C::F; ++j) w[j] = *reinterpret_cast<const uint4 *>(src + 16 * j);
-        uint32_t top = largest(w);
-        const uint32_t x = __shfl_xor(top, 32, 64);
-        const int shift = row_shift(top > x ? top : x);
-#pragma unroll
-        for (int j = 0; j < C::F; ++j) qf[j] = query_f16(w[j], shift);
-        c = score_factor(a, shift);
-    }
     f32x16 o[VT];
 #pragma unroll
     for (int x = 0; x < VT; ++x)
@@ -547,8 +580,10 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     for (int j = 0; j < 4; ++j) turned[j] = (lane ^ (2 * j)) * 16;
     if (threadIdx.x < D / 16) bad[threadIdx.x] = kNoToken;
 
-    uint32_t zw[4], zs = 0;
-    bool z_in = true;                    // the page lies in the cache (looked at when the loads have long been issued)
+    struct Codes {
+        uint32_t w[4], s;
+        bool in;                         // the page lies in the cache (looked at when the loads have long been issued)
+    };
     auto page_of = [&](int t) {
         // a vector load: a scalar one would share the counter that the operand reads are waited for with
         const int tt = t + 16 * (wave & 3);
@@ -556,38 +591,38 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         asm volatile("" : "+v"(at));
         return table[at];
     };
-    auto fetch = [&](int t, int entry) __attribute__((always_inline)) {
+    auto fetch = [&](int t, int entry, Codes &z) __attribute__((always_inline)) {
         const int page = t + 16 * (wave & 3) < t1 ? __builtin_amdgcn_readfirstlane(entry) : 0;
-        z_in = page >= 0 && page < a.c.pages;                            // uniform
-        const int64_t run = a.c.run(z_in ? page : 0, h) + ((t + 16 * (wave & 3)) & pmask);
+        z.in = page >= 0 && page < a.c.pages;                            // uniform
+        const int64_t run = a.c.run(z.in ? page : 0, h) + ((t + 16 * (wave & 3)) & pmask);
         const uint8_t *p = codes + run * (D / 2) + code_at, *q = scales + run * (D / 16) + scale_at;
         if (keys) {
             if constexpr (D == 128) {
                 const uint4 x = *reinterpret_cast<const uint4 *>(p);
-                zw[0] = x.x; zw[1] = x.y; zw[2] = x.z; zw[3] = x.w;
-                zs = *reinterpret_cast<const uint16_t *>(q);
+                z.w[0] = x.x; z.w[1] = x.y; z.w[2] = x.z; z.w[3] = x.w;
+                z.s = *reinterpret_cast<const uint16_t *>(q);
             } else {
                 const uint2 x = *reinterpret_cast<const uint2 *>(p);
-                zw[0] = x.x; zw[1] = x.y;
-                zs = *q;
+                z.w[0] = x.x; z.w[1] = x.y;
+                z.s = *q;
             }
         } else if (has) {
             const uint4 x = *reinterpret_cast<const uint4 *>(p);
-            zw[0] = x.x; zw[1] = x.y; zw[2] = x.z; zw[3] = x.w;
-            zs = *reinterpret_cast<const uint32_t *>(q);
+            z.w[0] = x.x; z.w[1] = x.y; z.w[2] = x.z; z.w[3] = x.w;
+            z.s = *reinterpret_cast<const uint32_t *>(q);
         }
     };
-    auto unpack = [&](int t, uint8_t *stage) __attribute__((always_inline)) {
+    auto unpack = [&](int t, Codes &z, uint8_t *stage) __attribute__((always_inline)) {
         uint8_t *d = stage + put_at;
-        if (!z_in) zs = keys ? 0x7F7Fu : 0u;
+        if (!z.in) z.s = keys ? 0x7F7Fu : 0u;
         if (keys) {
-            const h2 sc = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(zs, kScaleUp, false);
+            const h2 sc = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(z.s, kScaleUp, false);
             const h2 sc0 = {sc[0], sc[0]}, sc1 = {sc[1], sc[1]};
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
                 const h2 sj = j < 2 ? sc0 : sc1;
-                const uint32_t x = __builtin_amdgcn_perm(zw[j], zw[j], 0x01010000u);
-                const uint32_t y = __builtin_amdgcn_perm(zw[j], zw[j], 0x03030202u);
+                const uint32_t x = __builtin_amdgcn_perm(z.w[j], z.w[j], 0x01010000u);
+                const uint32_t y = __builtin_amdgcn_perm(z.w[j], z.w[j], 0x03030202u);
                 *reinterpret_cast<uint4 *>(d + (j >> 1) * 1024 + (j & 1) * 512) =
                     make_uint4(scaled((x << 4) & kCodeMask, sj), scaled(x & kCodeMask, sj), scaled((y << 4) & kCodeMask, sj),
                                scaled(y & kCodeMask, sj));
@@ -598,18 +633,18 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int at = t + 16 * (wave & 3) + my_tok + i;
-                    const bool nan = ((zs >> (8 * i)) & 0x7Fu) == 0x7Fu;
-                    if (at >= t1 || nan) zs &= ~(0xFFu << (8 * i));
+                    const bool nan = ((z.s >> (8 * i)) & 0x7Fu) == 0x7Fu;
+                    if (at >= t1 || nan) z.s &= ~(0xFFu << (8 * i));
                     if (at < t1 && nan) atomicMin(&bad[my_at >> 1], at);
                 }
             }
-            const h2 s0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(zs, kScaleUp, false);
-            const h2 s1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(zs, kScaleUp, true);
+            const h2 s0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(z.s, kScaleUp, false);
+            const h2 s1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(z.s, kScaleUp, true);
             uint32_t x[8], y[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t lo = __builtin_amdgcn_perm(zw[1], zw[0], 0x04040000u + 0x01010101u * j);
-                const uint32_t hi = __builtin_amdgcn_perm(zw[3], zw[2], 0x04040000u + 0x01010101u * j);
+                const uint32_t lo = __builtin_amdgcn_perm(z.w[1], z.w[0], 0x04040000u + 0x01010101u * j);
+                const uint32_t hi = __builtin_amdgcn_perm(z.w[3], z.w[2], 0x04040000u + 0x01010101u * j);
                 x[2 * j] = scaled((lo << 4) & kCodeMask, s0);
                 y[2 * j] = scaled((hi << 4) & kCodeMask, s1);
                 x[2 * j + 1] = scaled(lo & kCodeMask, s0);
@@ -626,6 +661,29 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         }
     };
 
+    // the first codes are on their way while the queries are made ready
+    Codes z, z1;
+    int entries[4] = {0, 0, 0, 0};
+    if (t0 < t1) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) entries[k] = page_of(t0 + 64 * k);
+        fetch(t0, entries[0], z);
+        fetch(t0 + 64, entries[1], z1);
+    }
+    h8 qf[C::F];
+    float c, ref = kLowest, sum = 0.0f;
+    {
+        const uint16_t *src = a.q + (sq.q0 + qi) * a.ldq + (int64_t)hq * D + 8 * up;
+        uint4 w[C::F];
+#pragma unroll
+        for (int j = 0; j < C::F; ++j) w[j] = *reinterpret_cast<const uint4 *>(src + 16 * j);
+        uint32_t top = largest(w);
+        const uint32_t x = __shfl_xor(top, 32, 64);
+        const int shift = row_shift(top > x ? top : x);
+#pragma unroll
+        for (int j = 0; j < C::F; ++j) qf[j] = query_f16(w[j], shift);
+        c = score_factor(a, shift);
+    }
     // Operand m of a block: the products with 32 tokens' values (sub) and with the keys of 32 later ones, in turn.
     auto operand = [&](const uint8_t *sub, const uint8_t *keys_at, int m) __attribute__((always_inline)) {
         const int i = m >> 1;
@@ -703,19 +761,16 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         for (int v = 0; v < 8; ++v) p[v] = w[v];
     };
 
-    const int steps = t1 > t0 ? (t1 - t0 + 63) / 64 : 0;
     __syncthreads();                                                     // bad[] is set
-    if (steps > 0) {
+    if (t0 < t1) {
         // Slots of the ring: the step before (its last values are still to come), this one, the next, and the one unpacked
         // into.  The last steps unpack what lies beyond the tokens (of page 0), which nothing uses.
         uint32_t slot = 0;
         auto stage = [&](uint32_t k) { return ring + (k & 3) * C::kStage; };
-        fetch(t0, page_of(t0));
-        unpack(t0, stage(0));
-        fetch(t0 + 64, page_of(t0 + 64));
-        unpack(t0 + 64, stage(1));
-        fetch(t0 + 128, page_of(t0 + 128));
-        int page = page_of(t0 + 192), t = t0;
+        unpack(t0, z, stage(0));
+        unpack(t0 + 64, z1, stage(1));
+        fetch(t0 + 128, entries[2], z);
+        int page = entries[3], t = t0;
         __syncthreads();
         f32x16 s0, s1;
 #pragma unroll
@@ -727,17 +782,19 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
 #pragma unroll
         for (int m = 0; m < 4; ++m) ops[m] = operand(before, ring + C::kSub, m);
         auto turn = [&]() __attribute__((always_inline)) {
-            unpack(t + 128, stage(slot + 2));
-            fetch(t + 192, page);
+            unpack(t + 128, z, stage(slot + 2));
+            fetch(t + 192, page, z);
             page = page_of(t + 256);
         };
-        // the waves of a SIMD (one with keys, one with values) unpack in different halves of a step
+        // the waves of a SIMD (one with keys, one with values) unpack in different halves of a step; a wave without rows
+        // does nothing else
+        const bool busy = row0 + 32 * wave < rows;                       // uniform
         auto step = [&](auto edge) __attribute__((always_inline)) {
             const uint8_t *now = stage(slot), *next = stage(slot + 1);
             if (keys) turn();
-            block(before, now + C::kSub, now, next, t, s0, s1, p, edge);
+            if (busy) block(before, now + C::kSub, now, next, t, s0, s1, p, edge);
             if (!keys) turn();
-            block(now, next, now + C::kSub, next + C::kSub, t + 32, s1, s0, p, edge);
+            if (busy) block(now, next, now + C::kSub, next + C::kSub, t + 32, s1, s0, p, edge);
             before = now + C::kSub;
             ++slot;
             t += 64;
@@ -762,15 +819,15 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
             if (bad[w >> 1] < see) o[x][v] = __builtin_nanf("");
         }
 
-    // rows through LDS, each wave in its own part; a row's channels are turned by its number
-    float *mine = reinterpret_cast<float *>(ring) + wave * 32 * D;
+    // rows through LDS, each wave in its own part, then out eight channels a lane
+    constexpr int kLd = D + 1, kPer = D / 8;                             // lanes of a row
+    float *mine = reinterpret_cast<float *>(ring) + wave * 32 * kLd;
     float *po = reinterpret_cast<float *>(a.workspace);
-    const int64_t all = a.T * a.q_heads;
+    const int64_t all = a.T * a.q_heads, at = (sq.q0 + qi) * a.q_heads + hq;
     sum += __shfl_xor(sum, 32, 64);
     const bool none = see == 0 && !sq.lost;
     const float f = splits > 1 ? 1.0f : sq.lost ? __builtin_nanf("") : none ? 0.0f : *a.c.gv * 4096.0f / sum;
     if (up == 0 && there) {
-        const int64_t at = (sq.q0 + qi) * a.q_heads + hq;
         if (splits > 1) {
             float *pm = po + (int64_t)splits * all * D + 2 * (split * all + at);
             pm[0] = ref;
@@ -784,21 +841,28 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int rho = 8 * (v >> 2) + 4 * up + (v & 3);
-            const int ch = 8 * (rho % WD) + CPT * x + rho / WD;
-            mine[col * D + (ch ^ col)] = none ? 0.0f : o[x][v] * f;
+            mine[col * kLd + 8 * (rho % WD) + CPT * x + rho / WD] = none ? 0.0f : o[x][v] * f;
         }
     __builtin_amdgcn_wave_barrier();
-    for (int rr = 0; rr < 32; ++rr) {
-        const int row2 = row0 + 32 * wave + rr;
-        if (row2 >= rows) break;
-        const int i2 = row2 / group, hq2 = h * group + (row2 - i2 * group);
-        if (splits > 1) {
-            float *dst = po + (split * all + (sq.q0 + i2) * a.q_heads + hq2) * D;
-            for (int ch = lane; ch < D; ch += 64) dst[ch] = mine[rr * D + (ch ^ rr)];
-        } else if (2 * lane < D) {
-            uint16_t *dst = a.out + (sq.q0 + i2) * a.ldo + (int64_t)hq2 * D;
-            const float y0 = mine[rr * D + ((2 * lane) ^ rr)], y1 = mine[rr * D + ((2 * lane + 1) ^ rr)];
-            *reinterpret_cast<uint32_t *>(dst + 2 * lane) = bf16_rne_from_float(y0) | (bf16_rne_from_float(y1) << 16);
+    const int64_t my_out = splits > 1 ? (split * all + at) * D : (sq.q0 + qi) * a.ldo + (int64_t)hq * D;
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += 64 / kPer) {
+        const int rr = r0 + lane / kPer, ch = lane % kPer * 8;
+        const int64_t out = ((int64_t)__shfl((int)(my_out >> 32), rr, 64) << 32) | (uint32_t)__shfl((int)my_out, rr, 64);
+        if (row0 + 32 * wave + rr < rows) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = mine[rr * kLd + ch + e];
+            if (splits > 1) {
+                float4 *dst = reinterpret_cast<float4 *>(po + out + ch);
+                dst[0] = make_float4(y[0], y[1], y[2], y[3]);
+                dst[1] = make_float4(y[4], y[5], y[6], y[7]);
+            } else {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = bf16_rne_from_float(y[2 * e]) | (bf16_rne_from_float(y[2 * e + 1]) << 16);
+                *reinterpret_cast<uint4 *>(a.out + out + ch) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
         }
     }
 }
@@ -879,20 +943,12 @@ template <int D, int NT, int W> void decode(const Kv4AttnArgs &a, const Kv4Plan 
 
 template <int D> void join(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
     const unsigned n = (unsigned)(a.B * a.max_q * a.q_heads);
-#if 0
-    if (p.splits <= 8) kv4_join_kernel<D, 1, 8><<<n, 64, 0, stream>>>(a, p.splits, p.chunk);
-    else if (p.splits <= 32) kv4_join_kernel<D, 4, 8><<<n, 256, 0, stream>>>(a, p.splits, p.chunk);
-    else if (p.splits <= 64) kv4_join_kernel<D, 4, 16><<<n, 256, 0, stream>>>(a, p.splits, p.chunk);
-    else if (p.splits <= 128) kv4_join_kernel<D, 8, 16><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
-    else kv4_join_kernel<D, 16, 16><<<n, 1024, 0, stream>>>(a, p.splits, p.chunk);
-#else
     if (p.splits <= 4) kv4_join_kernel<D, 1, 4><<<n, 64, 0, stream>>>(a, p.splits, p.chunk);
     else if (p.splits <= 16) kv4_join_kernel<D, 4, 4><<<n, 256, 0, stream>>>(a, p.splits, p.chunk);
     else if (p.splits <= 32) kv4_join_kernel<D, 8, 4><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
     else if (p.splits <= 64) kv4_join_kernel<D, 8, 8><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
     else if (p.splits <= 128) kv4_join_kernel<D, 8, 16><<<n, 512, 0, stream>>>(a, p.splits, p.chunk);
     else kv4_join_kernel<D, 16, 16><<<n, 1024, 0, stream>>>(a, p.splits, p.chunk);
-#endif
 }
 
 template <int D> hipError_t attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
