@@ -27,10 +27,17 @@ __device__ __forceinline__ void load16(const uint16_t *__restrict__ p, float (&x
     }
 }
 
+// Two FP32 values rounded to bfloat16 (nearest even).
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    const b2 y = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, y);
+}
+
 __device__ __forceinline__ void store16(uint16_t *__restrict__ p, const float (&x)[16]) {
     uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = bf16_rne_from_float(x[2 * i]) | (bf16_rne_from_float(x[2 * i + 1]) << 16);
+    for (int i = 0; i < 8; ++i) w[i] = bf16_pair(x[2 * i], x[2 * i + 1]);
     reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
     reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
@@ -53,33 +60,45 @@ struct AppendArgs {
     uint16_t *q_out;
     const float *cos, *sin;                // [rope_len][D / 2], or null: no rotation
     const int32_t *positions;
-    int64_t T, ldq, ldk, ldv, ldq_out, rope_len;
-    int q_heads;                           // 0: no queries
+    int64_t ldq, ldk, ldv, ldq_out, rope_len;
+    int T, q_heads;                        // tokens of this launch; 0 heads: no queries
+    int kv_blocks;                         // workgroups of the keys, and of the values
 };
 
-// A thread's item is channels 16 p .. 16 p + 15 and the same of the other half of one head of
-// one token; heads count queries, then keys, then values.
+// Quantizes 16 values into block b of token `tok`.  kBf16: they are bfloat16 numbers, where midpoints are common.
+template <int D, bool kValues, bool kBf16>
+__device__ __forceinline__ void put_block(const AppendArgs &a, const float (&x)[16], const Kv4G &G, int64_t run, int tok, int b) {
+    const Kv4Rounded R = kv4_round<kBf16>(x, kv4_block_max(x), G);
+    const uint2 w = kv4_codes(x, R, G);
+    if constexpr (kValues) {
+        uint8_t *d = a.c.vc + kv4_v_codes(run, tok, b, D);
+        *reinterpret_cast<uint32_t *>(d) = w.x;
+        *reinterpret_cast<uint32_t *>(d + 16) = w.y;
+        a.c.vs[kv4_v_scales(run, tok, b, D)] = (uint8_t)R.sbyte;
+    } else {
+        *reinterpret_cast<uint2 *>(a.c.kc + kv4_k_codes(run, tok, D) + 8 * b) = w;
+        a.c.ks[kv4_k_scales(run, tok, D) + b] = (uint8_t)R.sbyte;
+    }
+}
+
+// A thread's item is channels 16 p .. 16 p + 15 and the same of the other half of one head of one token.  The first
+// workgroups take the keys, the next the values, the last the queries: a wave does one of the three (with heads of
+// all kinds in a wave, 5003 tokens of 28 + 4 + 4 heads took 32 us; rounding by bit arithmetic in FP32 was part of that).
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv4_append_kernel(const AppendArgs a) {
     constexpr int kPairs = D / 32;
-    const int heads = a.q_heads + 2 * a.c.heads;
-    const int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (item >= a.T * heads * kPairs) return;
-    const int p = (int)(item % kPairs);
-    const int64_t th = item / kPairs, t = th / heads;
-    int h = (int)(th - t * heads);
-    const bool is_q = h < a.q_heads;
-    h -= is_q ? 0 : a.q_heads;
-    const bool is_v = !is_q && h >= a.c.heads;
-    h -= is_v ? a.c.heads : 0;
-    const int64_t slot = is_q ? 0 : a.slots[t];
-    if (slot < 0 || slot >= a.c.slots()) return;           // padding
+    const int kind = (int)blockIdx.x < a.kv_blocks ? 0 : (int)blockIdx.x < 2 * a.kv_blocks ? 1 : 2;   // keys, values, queries
+    const int heads = kind == 2 ? a.q_heads : a.c.heads;
+    const uint32_t item = (blockIdx.x - kind * a.kv_blocks) * kThreads + threadIdx.x;
+    const uint32_t th = item / kPairs, t = th / heads;
+    if (t >= (uint32_t)a.T) return;
+    const int p = (int)(item % kPairs), h = (int)(th - t * heads);
     const int c0 = 16 * p, c1 = c0 + D / 2;
-    const uint16_t *src = (is_q ? a.q + t * a.ldq : is_v ? a.v + t * a.ldv : a.k + t * a.ldk) + h * D;
+    const uint16_t *src = (kind == 2 ? a.q + t * a.ldq : kind == 1 ? a.v + t * a.ldv : a.k + t * a.ldk) + h * D;
     float x[2][16];
     load16(src + c0, x[0]);
     load16(src + c1, x[1]);
-    if (!is_v && a.cos) {
+    if (kind != 1 && a.cos) {
         const int64_t pos = a.positions[t];
         if (pos >= 0 && pos < a.rope_len) {
             float c[16], s[16];
@@ -96,91 +115,97 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(const AppendArgs a
             for (int j = 0; j < 16; ++j) x[0][j] = x[1][j] = __builtin_nanf("");
         }
     }
-    if (is_q) {
+    if (kind == 2) {
         uint16_t *dst = a.q_out + t * a.ldq_out + h * D;
         store16(dst + c0, x[0]);
         store16(dst + c1, x[1]);
         return;
     }
-    const int64_t page = slot >> a.c.page_log2;
+    const int64_t slot = a.slots[t];
+    if (slot < 0 || slot >= a.c.slots()) return;           // padding
     const int tok = (int)(slot & ((int64_t(1) << a.c.page_log2) - 1));
-    const int64_t run = a.c.run(page, h);
-    const Kv4G G = kv4_make_g(is_v ? *a.c.gv : *a.c.gk);
+    const int64_t run = a.c.run(slot >> a.c.page_log2, h);
+    if (kind == 1) {
+        const Kv4G G = kv4_make_g(*a.c.gv);
+        put_block<D, true, true>(a, x[0], G, run, tok, p);
+        put_block<D, true, true>(a, x[1], G, run, tok, p + D / 32);
+        return;
+    }
+    const Kv4G G = kv4_make_g(*a.c.gk);
+    if (a.c.shift) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int b = p + half * (D / 32);
-        if (!is_v && a.c.shift) {
+        for (int half = 0; half < 2; ++half) {
             float m[16];
-            load_f32x16(a.c.shift + h * D + 16 * b, m);
+            load_f32x16(a.c.shift + h * D + (half ? c1 : c0), m);
 #pragma unroll
             for (int j = 0; j < 16; ++j) x[half][j] = x[half][j] - m[j];
         }
-        const uint32_t am = kv4_block_max(x[half]);
-        // values, and keys without rotation and shift, are bfloat16: midpoints are common there
-        const bool bf16 = is_v || (!a.cos && !a.c.shift);
-        uint2 w;
-        uint32_t sbyte;
-        if (bf16) {
-            const Kv4Rounded R = kv4_round<true>(x[half], am, G);
-            w = kv4_codes(x[half], R, G);
-            sbyte = R.sbyte;
-        } else {
-            const Kv4Rounded R = kv4_round<false>(x[half], am, G);
-            w = kv4_codes(x[half], R, G);
-            sbyte = R.sbyte;
-        }
-        if (is_v) {
-            uint8_t *d = a.c.vc + kv4_v_codes(run, tok, b, D);
-            *reinterpret_cast<uint32_t *>(d) = w.x;
-            *reinterpret_cast<uint32_t *>(d + 16) = w.y;
-            a.c.vs[kv4_v_scales(run, tok, b, D)] = (uint8_t)sbyte;
-        } else {
-            *reinterpret_cast<uint2 *>(a.c.kc + kv4_k_codes(run, tok, D) + 8 * b) = w;
-            a.c.ks[kv4_k_scales(run, tok, D) + b] = (uint8_t)sbyte;
-        }
+    }
+    if (a.cos || a.c.shift) {
+        put_block<D, false, false>(a, x[0], G, run, tok, p);
+        put_block<D, false, false>(a, x[1], G, run, tok, p + D / 32);
+    } else {
+        put_block<D, false, true>(a, x[0], G, run, tok, p);
+        put_block<D, false, true>(a, x[1], G, run, tok, p + D / 32);
     }
 }
 
-// The 16 values of a block as bfloat16: RN(c s g), or RN(RN32(c s g) + shift).  With a
-// power-of-two g that keeps s g inside FP32's normal range c s g is exact there; FP64 otherwise.
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+
+// The 16 values of a block as bfloat16: RN(c s g), or RN(RN32(c s g) + shift).  With a power-of-two g in the range
+// below c s g is exact in FP32: a code's bits in a half word are n 2^-20 as FP16 (sign at bit 15, n at bits 6:4), and
+// one mixed FMA per value multiplies them by H 2^20 (H = s g / 2) and adds the shift.  FP64 otherwise.
 __device__ __forceinline__ void decode16(uint2 w, uint32_t sbyte, const Kv4G &G, const float *__restrict__ shift,
                                          uint16_t *__restrict__ y) {
-    uint32_t o[16];
+    uint32_t o[8];
     float m[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) m[j] = -0.0f;             // keeps the sign of a zero
     if (shift) load_f32x16(shift, m);
     const bool bad = (sbyte & 0x7Fu) == 0x7Fu;
-    const float H = 0.5f * e4m3_value(sbyte) * G.g;
-    const bool f32 = G.f32 && (H == 0.0f || H >= 0x1p-126f);
-    const double Hd = 0.5 * (double)e4m3_value(sbyte) * G.gd;
+    if (G.f32 && G.kg >= -100 && G.kg <= 90) {
+        const float up = 0x1p19f * e4m3_value(sbyte) * G.g;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const uint32_t c = ((j < 8 ? w.x : w.y) >> (4 * (j & 7))) & 15u;
-        const float mag = (float)(c & 7u);
-        const float n = (c & 8u) ? -mag : mag;
-        if (shift) {
-            const float v = f32 ? n * H : (float)((double)n * Hd);
-            o[j] = bf16_rne_from_float(v + m[j]);
-        } else {
-            o[j] = f32 ? bf16_rne_from_float(n * H) : bf16_rne_from_double((double)n * Hd);
+        for (int k = 0; k < 4; ++k) {
+            // bytes 2 k, 2 k + 1: elements 4 k (low nibble), 4 k + 1 (high) and 4 k + 2, 4 k + 3, each byte twice in its half
+            const uint32_t d = k < 2 ? w.x : w.y;
+            const uint32_t b = __builtin_amdgcn_perm(d, d, k & 1 ? 0x03030202u : 0x01010000u);
+            const h2 lo = __builtin_bit_cast(h2, (b << 4) & 0x80708070u), hi = __builtin_bit_cast(h2, b & 0x80708070u);
+            o[2 * k] = bf16_pair(__builtin_fmaf((float)lo[0], up, m[4 * k]), __builtin_fmaf((float)hi[0], up, m[4 * k + 1]));
+            o[2 * k + 1] = bf16_pair(__builtin_fmaf((float)lo[1], up, m[4 * k + 2]), __builtin_fmaf((float)hi[1], up, m[4 * k + 3]));
         }
-        if (bad) o[j] = 0x7FC0u;
+    } else {
+        const double H = 0.5 * (double)e4m3_value(sbyte) * G.gd;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            uint32_t z[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t c = ((k < 4 ? w.x : w.y) >> (4 * ((2 * k + e) & 7))) & 15u;
+                const double v = (c & 8u ? -H : H) * (double)(c & 7u);
+                z[e] = shift ? bf16_rne_from_float((float)v + m[2 * k + e]) : bf16_rne_from_double(v);
+            }
+            o[k] = z[0] | (z[1] << 16);
+        }
     }
+    if (bad)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = 0x7FC07FC0u;
     uint4 *dst = reinterpret_cast<uint4 *>(y);
-    dst[0] = make_uint4(o[0] | (o[1] << 16), o[2] | (o[3] << 16), o[4] | (o[5] << 16), o[6] | (o[7] << 16));
-    dst[1] = make_uint4(o[8] | (o[9] << 16), o[10] | (o[11] << 16), o[12] | (o[13] << 16), o[14] | (o[15] << 16));
+    dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
 }
 
 // A thread's item is one block of 16 channels of one head of one slot, keys and values.
 template <int D>
-__global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const Kv4View c, const int64_t *__restrict__ slots, int64_t T,
+__global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const Kv4View c, const int64_t *__restrict__ slots, int T,
                                                               uint16_t *__restrict__ ky, int64_t ldk,
                                                               uint16_t *__restrict__ vy, int64_t ldv, bool add_shift) {
     constexpr int kBlocks = D / 16;
-    const int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (item >= T * c.heads * kBlocks) return;
-    const int b = (int)(item % kBlocks);
-    const int64_t th = item / kBlocks, t = th / c.heads;
-    const int h = (int)(th - t * c.heads);
+    const uint32_t item = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t th = item / kBlocks, t = th / c.heads;
+    if (t >= (uint32_t)T) return;
+    const int b = (int)(item % kBlocks), h = (int)(th - t * c.heads);
     const int64_t slot = slots[t];
     const int64_t at = h * D + 16 * b;
     if (slot < 0 || slot >= c.slots()) {                   // padding
@@ -203,6 +228,12 @@ __global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const Kv4View c, c
     }
 }
 
+// Tokens of one launch, so that items and workgroups are 32-bit numbers with at most 65535 heads of 128 channels.
+constexpr int64_t kSlice = int64_t(1) << 13;
+constexpr int64_t kSliceHeads = int64_t(1) << 28;
+
+int64_t slice_of(int heads) { return kSliceHeads / heads > kSlice ? kSliceHeads / heads / 8 * 8 : kSlice; }
+
 unsigned blocks_for(int64_t items) { return (unsigned)((items + kThreads - 1) / kThreads); }
 
 }  // namespace
@@ -211,20 +242,36 @@ hipError_t launch_kv4_append(const Kv4View &c, int64_t T, const int64_t *slots, 
                              const uint16_t *v, int64_t ldv, const uint16_t *q, int64_t ldq, int q_heads,
                              uint16_t *q_out, int64_t ldq_out, const float *cos, const float *sin,
                              const int32_t *positions, int64_t rope_len, hipStream_t stream) {
-    const AppendArgs a = {c, slots, q, k, v, q_out, cos, sin, positions, T, ldq, ldk, ldv, ldq_out, rope_len, q_heads};
-    const unsigned n = blocks_for(T * (q_heads + 2 * c.heads) * (c.D / 32));
-    if (c.D == 128) kv4_append_kernel<128><<<n, kThreads, 0, stream>>>(a);
-    else kv4_append_kernel<64><<<n, kThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    const int64_t slice = slice_of(c.heads > q_heads ? c.heads : q_heads);
+    for (int64_t t = 0; t < T; t += slice) {
+        const int n = (int)(T - t < slice ? T - t : slice);
+        const int kv_blocks = (int)blocks_for((int64_t)n * c.heads * (c.D / 32));
+        const AppendArgs a = {c, slots + t, q_heads ? q + t * ldq : q, k + t * ldk, v + t * ldv,
+                              q_heads ? q_out + t * ldq_out : q_out, cos, sin, positions ? positions + t : positions,
+                              ldq, ldk, ldv, ldq_out, rope_len, n, q_heads, kv_blocks};
+        const unsigned grid = 2 * kv_blocks + blocks_for((int64_t)n * q_heads * (c.D / 32));
+        if (c.D == 128) kv4_append_kernel<128><<<grid, kThreads, 0, stream>>>(a);
+        else kv4_append_kernel<64><<<grid, kThreads, 0, stream>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_kv4_gather(const Kv4View &c, int64_t T, const int64_t *slots, uint16_t *k, int64_t ldk, uint16_t *v,
                              int64_t ldv, bool add_shift, hipStream_t stream) {
-    const unsigned n = blocks_for(T * c.heads * (c.D / 16));
+    const int64_t slice = slice_of(c.heads);
     const bool sh = add_shift && c.shift;
-    if (c.D == 128) kv4_gather_kernel<128><<<n, kThreads, 0, stream>>>(c, slots, T, k, ldk, v, ldv, sh);
-    else kv4_gather_kernel<64><<<n, kThreads, 0, stream>>>(c, slots, T, k, ldk, v, ldv, sh);
-    return hipGetLastError();
+    for (int64_t t = 0; t < T; t += slice) {
+        const int n = (int)(T - t < slice ? T - t : slice);
+        const unsigned grid = blocks_for((int64_t)n * c.heads * (c.D / 16));
+        uint16_t *kt = k ? k + t * ldk : k, *vt = v ? v + t * ldv : v;
+        if (c.D == 128) kv4_gather_kernel<128><<<grid, kThreads, 0, stream>>>(c, slots + t, n, kt, ldk, vt, ldv, sh);
+        else kv4_gather_kernel<64><<<grid, kThreads, 0, stream>>>(c, slots + t, n, kt, ldk, vt, ldv, sh);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace reqat
