@@ -15,6 +15,7 @@ namespace reqat {
 namespace {
 
 constexpr int kThreads = 256;
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 
 // 16 bfloat16 values as FP32
 __device__ __forceinline__ void load16(const uint16_t *__restrict__ p, float (&x)[16]) {
@@ -150,26 +151,25 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(const AppendArgs a
     }
 }
 
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-
-// The 16 values of a block as bfloat16: RN(c s g), or RN(RN32(c s g) + shift).  With a power-of-two g in the range
-// below c s g is exact in FP32: a code's bits in a half word are n 2^-20 as FP16 (sign at bit 15, n at bits 6:4), and
+// The eight values of a dword of codes as bfloat16: RN(c s g), or RN(RN32(c s g) + shift).  With a power-of-two g in the
+// range below c s g is exact in FP32: a code's bits in a half word are n 2^-20 as FP16 (sign at bit 15, n at bits 6:4), and
 // one mixed FMA per value multiplies them by H 2^20 (H = s g / 2) and adds the shift.  FP64 otherwise.
-__device__ __forceinline__ void decode16(uint2 w, uint32_t sbyte, const Kv4G &G, const float *__restrict__ shift,
-                                         uint16_t *__restrict__ y) {
-    uint32_t o[8];
-    float m[16];
+__device__ __forceinline__ uint4 decode8(uint32_t w, uint32_t sbyte, const Kv4G &G, const float *__restrict__ shift) {
+    uint32_t o[4];
+    float m[8];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) m[j] = -0.0f;             // keeps the sign of a zero
-    if (shift) load_f32x16(shift, m);
-    const bool bad = (sbyte & 0x7Fu) == 0x7Fu;
+    for (int j = 0; j < 8; ++j) m[j] = -0.0f;              // keeps the sign of a zero
+    if (shift) {
+        const float4 x = reinterpret_cast<const float4 *>(shift)[0], y = reinterpret_cast<const float4 *>(shift)[1];
+        m[0] = x.x; m[1] = x.y; m[2] = x.z; m[3] = x.w;
+        m[4] = y.x; m[5] = y.y; m[6] = y.z; m[7] = y.w;
+    }
     if (G.f32 && G.kg >= -100 && G.kg <= 90) {
         const float up = 0x1p19f * e4m3_value(sbyte) * G.g;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 2; ++k) {
             // bytes 2 k, 2 k + 1: elements 4 k (low nibble), 4 k + 1 (high) and 4 k + 2, 4 k + 3, each byte twice in its half
-            const uint32_t d = k < 2 ? w.x : w.y;
-            const uint32_t b = __builtin_amdgcn_perm(d, d, k & 1 ? 0x03030202u : 0x01010000u);
+            const uint32_t b = __builtin_amdgcn_perm(w, w, k ? 0x03030202u : 0x01010000u);
             const h2 lo = __builtin_bit_cast(h2, (b << 4) & 0x80708070u), hi = __builtin_bit_cast(h2, b & 0x80708070u);
             o[2 * k] = bf16_pair(__builtin_fmaf((float)lo[0], up, m[4 * k]), __builtin_fmaf((float)hi[0], up, m[4 * k + 1]));
             o[2 * k + 1] = bf16_pair(__builtin_fmaf((float)lo[1], up, m[4 * k + 2]), __builtin_fmaf((float)hi[1], up, m[4 * k + 3]));
@@ -177,62 +177,54 @@ __device__ __forceinline__ void decode16(uint2 w, uint32_t sbyte, const Kv4G &G,
     } else {
         const double H = 0.5 * (double)e4m3_value(sbyte) * G.gd;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 4; ++k) {
             uint32_t z[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const uint32_t c = ((k < 4 ? w.x : w.y) >> (4 * ((2 * k + e) & 7))) & 15u;
+                const uint32_t c = (w >> (4 * (2 * k + e))) & 15u;
                 const double v = (c & 8u ? -H : H) * (double)(c & 7u);
                 z[e] = shift ? bf16_rne_from_float((float)v + m[2 * k + e]) : bf16_rne_from_double(v);
             }
             o[k] = z[0] | (z[1] << 16);
         }
     }
-    if (bad)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = 0x7FC07FC0u;
-    uint4 *dst = reinterpret_cast<uint4 *>(y);
-    dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    const bool bad = (sbyte & 0x7Fu) == 0x7Fu;
+    const uint32_t nan = 0x7FC07FC0u;
+    return bad ? make_uint4(nan, nan, nan, nan) : make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// A thread's item is one block of 16 channels of one head of one slot, keys and values.
+// A thread's item is eight channels of one head of one slot, keys and values: a wave writes 1 KB of adjacent bytes
+// at a time (with 16 channels a thread and two stores of every other 16 bytes, 32768 tokens of 8 heads took 54 us).
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const Kv4View c, const int64_t *__restrict__ slots, int T,
                                                               uint16_t *__restrict__ ky, int64_t ldk,
                                                               uint16_t *__restrict__ vy, int64_t ldv, bool add_shift) {
-    constexpr int kBlocks = D / 16;
+    constexpr int kWords = D / 8;
     const uint32_t item = blockIdx.x * kThreads + threadIdx.x;
-    const uint32_t th = item / kBlocks, t = th / c.heads;
+    const uint32_t th = item / kWords, t = th / c.heads;
     if (t >= (uint32_t)T) return;
-    const int b = (int)(item % kBlocks), h = (int)(th - t * c.heads);
+    const int w = (int)(item % kWords), h = (int)(th - t * c.heads);
     const int64_t slot = slots[t];
-    const int64_t at = h * D + 16 * b;
-    if (slot < 0 || slot >= c.slots()) {                   // padding
-        const uint4 z = make_uint4(0, 0, 0, 0);
-        if (ky) reinterpret_cast<uint4 *>(ky + t * ldk + at)[0] = reinterpret_cast<uint4 *>(ky + t * ldk + at)[1] = z;
-        if (vy) reinterpret_cast<uint4 *>(vy + t * ldv + at)[0] = reinterpret_cast<uint4 *>(vy + t * ldv + at)[1] = z;
-        return;
+    const int64_t at = h * D + 8 * w;
+    uint4 k = make_uint4(0, 0, 0, 0), v = k;               // padding: zeros
+    if (slot >= 0 && slot < c.slots()) {
+        const int tok = (int)(slot & ((int64_t(1) << c.page_log2) - 1));
+        const int64_t run = c.run(slot >> c.page_log2, h);
+        if (ky) {
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(c.kc + kv4_k_codes(run, tok, D) + 4 * w);
+            k = decode8(x, c.ks[kv4_k_scales(run, tok, D) + w / 2], kv4_make_g(*c.gk), add_shift ? c.shift + at : nullptr);
+        }
+        if (vy) {
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(c.vc + kv4_v_codes(run, tok, w / 2, D) + 16 * (w & 1));
+            v = decode8(x, c.vs[kv4_v_scales(run, tok, w / 2, D)], kv4_make_g(*c.gv), nullptr);
+        }
     }
-    const int tok = (int)(slot & ((int64_t(1) << c.page_log2) - 1));
-    const int64_t run = c.run(slot >> c.page_log2, h);
-    if (ky) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(c.kc + kv4_k_codes(run, tok, D) + 8 * b);
-        decode16(w, c.ks[kv4_k_scales(run, tok, D) + b], kv4_make_g(*c.gk), add_shift ? c.shift + at : nullptr,
-                 ky + t * ldk + at);
-    }
-    if (vy) {
-        const uint8_t *s = c.vc + kv4_v_codes(run, tok, b, D);
-        const uint2 w = make_uint2(*reinterpret_cast<const uint32_t *>(s), *reinterpret_cast<const uint32_t *>(s + 16));
-        decode16(w, c.vs[kv4_v_scales(run, tok, b, D)], kv4_make_g(*c.gv), nullptr, vy + t * ldv + at);
-    }
+    if (ky) *reinterpret_cast<uint4 *>(ky + t * ldk + at) = k;
+    if (vy) *reinterpret_cast<uint4 *>(vy + t * ldv + at) = v;
 }
 
-// Tokens of one launch, so that items and workgroups are 32-bit numbers with at most 65535 heads of 128 channels.
-constexpr int64_t kSlice = int64_t(1) << 13;
-constexpr int64_t kSliceHeads = int64_t(1) << 28;
-
-int64_t slice_of(int heads) { return kSliceHeads / heads > kSlice ? kSliceHeads / heads / 8 * 8 : kSlice; }
+// Tokens of one launch: its items (at most 16 a token and head) are numbered in 32 bits.
+int64_t slice_of(int heads) { return (int64_t(1) << 27) / heads; }
 
 unsigned blocks_for(int64_t items) { return (unsigned)((items + kThreads - 1) / kThreads); }
 
@@ -264,7 +256,7 @@ hipError_t launch_kv4_gather(const Kv4View &c, int64_t T, const int64_t *slots, 
     const bool sh = add_shift && c.shift;
     for (int64_t t = 0; t < T; t += slice) {
         const int n = (int)(T - t < slice ? T - t : slice);
-        const unsigned grid = blocks_for((int64_t)n * c.heads * (c.D / 16));
+        const unsigned grid = blocks_for((int64_t)n * c.heads * (c.D / 8));
         uint16_t *kt = k ? k + t * ldk : k, *vt = v ? v + t * ldv : v;
         if (c.D == 128) kv4_gather_kernel<128><<<grid, kThreads, 0, stream>>>(c, slots + t, n, kt, ldk, vt, ldv, sh);
         else kv4_gather_kernel<64><<<grid, kThreads, 0, stream>>>(c, slots + t, n, kt, ldk, vt, ldv, sh);
