@@ -366,7 +366,8 @@ reqat_status reqat_kv4_gather(const reqat_kv4_cache *cache, int64_t T, const int
  *   kv_len [B] int32: cached tokens, the new ones included.
  *   block_table [B][ld_table] int32: the page of tokens p * page_size ..,
  *     table_cols entries of a row are used (ld_table >= table_cols).
- *   max_q, max_kv: bounds on every nq and kv_len (they size the launch).
+ *   max_q, max_kv: bounds on every nq and kv_len, at most 2^31 - 1 and 2^30 (they
+ *     size the launch).
  *   out [T][ldo] bfloat16; lse NULL or [T][q_heads] FP32, the natural logarithm
  *     of sum_j exp(sm_scale q . k^_j) (of the shifted keys).
  *   workspace: reqat_kv4_attention_workspace_bytes(...) bytes, 16-byte aligned

@@ -243,7 +243,7 @@ reqat_status reqat_kv4_gather(const reqat_kv4_cache *cache, int64_t T, const int
 static bool kv4_attention_sizes_ok(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int64_t q_heads,
                                    int64_t kv_heads) {
     return B >= 0 && B <= 65535 && T >= 0 && T <= 0x7FFFFFFF && max_q >= 0 && max_q <= 0x7FFFFFFF && max_kv >= 0 &&
-           max_kv <= 0x7FFFFFFF && kv_heads > 0 && kv_heads <= 65535 && q_heads > 0 && q_heads <= 65535 &&
+           max_kv <= (1 << 30) && kv_heads > 0 && kv_heads <= 65535 && q_heads > 0 && q_heads <= 65535 &&
            q_heads % kv_heads == 0;
 }
 
@@ -272,6 +272,7 @@ reqat_status reqat_kv4_attention(const reqat_kv4_cache *cache, int64_t B, int64_
          reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(lse)) & 3u)
         return REQAT_E_ALIGN;
     if (max_q > T) max_q = T;
+    if (!kv4_plan_fits(kv4_plan(B, max_q, max_kv, (int)q_heads, view.heads), B, view.heads)) return REQAT_E_SHAPE;
     const size_t need = kv4_attention_workspace_bytes(B, T, max_q, max_kv, (int)q_heads, view.heads, view.D);
     if (need > 0 && !workspace) return REQAT_E_NULL;
     if (!aligned16(workspace)) return REQAT_E_ALIGN;

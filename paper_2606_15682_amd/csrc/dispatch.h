@@ -276,6 +276,7 @@ struct Kv4Plan {
     int tiles, qtiles, waves, splits, chunk;
 };
 constexpr int kKv4MaxSplits = 256;
+constexpr int64_t kKv4MaxPieces = 8192; // in all, where the longest of several sequences asks for them: a workspace of 136 MB at most
 constexpr int kKv4Prompt = 16;          // tiles of the kernel for prompts: 256 rows
 
 inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads) {
@@ -292,17 +293,27 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, i
         p.waves = 8;
     } else {
         splits = groups > 0 ? (512 + groups - 1) / groups : 1;
-        if (B > 1 && max_kv > 2048 && splits < (max_kv + 1535) / 1536) splits = (max_kv + 1535) / 1536;
+        if (B > 1 && max_kv > 2048) {
+            int64_t finer = (max_kv + 1535) / 1536;
+            finer = finer * groups > kKv4MaxPieces ? kKv4MaxPieces / groups : finer;
+            splits = splits < finer ? finer : splits;
+        }
     }
     const int64_t most = (max_kv + 255) / 256;
     splits = splits > most ? most : splits;
     splits = splits > kKv4MaxSplits ? kKv4MaxSplits : splits;
     splits = splits < 1 ? 1 : splits;
     const int64_t chunk = ((max_kv + splits - 1) / splits + 127) / 128 * 128;
-    p.chunk = (int)(chunk < 128 ? 128 : chunk > 0x7FFFFF80 ? 0x7FFFFF80 : chunk);
+    p.chunk = (int)(chunk < 128 ? 128 : chunk);                          // max_kv <= 2^30
     p.splits = (int)((max_kv + p.chunk - 1) / p.chunk);
     if (p.splits < 1) p.splits = 1;
     return p;
+}
+
+// Whether the launch of a plan holds fewer than 2^32 threads (workgroups of up to 512).
+inline bool kv4_plan_fits(const Kv4Plan &p, int64_t B, int kv_heads) {
+    const int64_t n = B * kv_heads * p.splits;                           // below 2^40
+    return p.tiles == kKv4Prompt ? n < (int64_t(1) << 23) && n * p.qtiles < (int64_t(1) << 23) : n < (int64_t(1) << 23);
 }
 
 }  // namespace reqat

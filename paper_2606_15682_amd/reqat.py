@@ -14,6 +14,7 @@ marshals arguments.  It raises at load time when the library is missing.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -251,7 +252,9 @@ def reqat_abi_version() -> int:
 # ------------------------------------------------------------------ torch conveniences
 
 def _stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+    """The handle of the device's current stream (without a Stream object around it: 3 us less per call)."""
+    index = device.index
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if index is None else index)
 
 
 def _check(st: int, where: str):
@@ -561,6 +564,7 @@ class Kv4Cache:
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.num_pages, self.page_size, self.kv_heads, self.head_dim = num_pages, page_size, kv_heads, head_dim
+        self.width = kv_heads * head_dim         # channels of a token's keys, and of its values
 
         def scale(g, name):
             if isinstance(g, torch.Tensor):
@@ -578,12 +582,9 @@ class Kv4Cache:
         self.v_codes = torch.zeros(run * head_dim // 2, **u8)
         self.v_scales = torch.zeros(run * head_dim // 16, **u8)
 
-    @property
-    def width(self) -> int:
-        """Channels of a token's keys (or values): kv_heads * head_dim."""
-        return self.kv_heads * self.head_dim
-
+    @functools.cached_property
     def struct(self) -> Kv4CacheStruct:
+        """reqat_kv4_cache of this cache, whose tensors stay the same ones."""
         return Kv4CacheStruct(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
                               self.v_scales.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
                               _ptr(self.k_shift), self.num_pages, self.page_size, self.kv_heads, self.head_dim)
@@ -596,7 +597,9 @@ def _cache_arg(cache):
 
 
 def _index_arg(t, shape, dtype, device, name):
-    """A contiguous integer tensor that the kernels read on the device."""
+    """A contiguous tensor that the kernels read on the device (the whole check first: decode steps are short)."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t
     if not isinstance(t, torch.Tensor) or t.dtype != dtype:
         raise TypeError("%s must be a %s tensor" % (name, dtype))
     if tuple(t.shape) != shape:
@@ -608,7 +611,11 @@ def _index_arg(t, shape, dtype, device, name):
 
 
 def _rows_arg(x, rows, cols, device, name):
-    """A bfloat16 [rows, cols] input; returns its row stride."""
+    """A bfloat16 [rows, cols] tensor, rows possibly strided; returns its row stride."""
+    if type(x) is torch.Tensor and x.dtype is torch.bfloat16 and x.shape == (rows, cols) and x.device == device:
+        ld, one = x.stride()
+        if one == 1:
+            return ld if rows > 1 else max(cols, 1)
     if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16 or x.dim() != 2:
         raise TypeError("%s must be a 2-D bfloat16 tensor" % name)
     return _out2d(x, rows, cols, torch.bfloat16, device, name)
@@ -647,12 +654,11 @@ def kv4_append(cache, k, v, slots, q=None, rope=None, positions=None, q_out=None
         ldq = _rows_arg(q, T, q.shape[1], dev, "q")
         if q_out is None:
             q_out = torch.empty((T, q.shape[1]), dtype=torch.bfloat16, device=dev)
-        ldqo = _out2d(q_out, T, q.shape[1], torch.bfloat16, dev, "q_out")
+        ldqo = _rows_arg(q_out, T, q.shape[1], dev, "q_out")
     elif q_out is not None:
         raise ValueError("q_out without q")
     _require_cuda(k, "k")
-    cs = cache.struct()
-    st = reqat_kv4_append(cs, T, slots.data_ptr(), k.data_ptr(), ldk, v.data_ptr(), ldv, _ptr(q), ldq, q_heads,
+    st = reqat_kv4_append(cache.struct, T, slots.data_ptr(), k.data_ptr(), ldk, v.data_ptr(), ldv, _ptr(q), ldq, q_heads,
                           _ptr(q_out), ldqo, _ptr(cos), _ptr(sin), _ptr(positions), rope_len, _stream(dev))
     _check(st, "reqat_kv4_append")
     return q_out
@@ -667,16 +673,21 @@ def kv4_gather(cache, slots, add_shift=False, out=None):
         raise TypeError("slots must be a 1-D int64 tensor")
     T, dev = slots.shape[0], cache.device
     _index_arg(slots, (T,), torch.int64, dev, "slots")
-    k, v = out if out is not None else (torch.empty((T, cache.width), dtype=torch.bfloat16, device=dev)
-                                        for _ in range(2))
-    ldk = _out2d(k, T, cache.width, torch.bfloat16, dev, "out[0]")
-    ldv = _out2d(v, T, cache.width, torch.bfloat16, dev, "out[1]")
+    if out is None:
+        out = torch.empty((2, T, cache.width), dtype=torch.bfloat16, device=dev).unbind(0)
+    k, v = out
+    ldk = _rows_arg(k, T, cache.width, dev, "out[0]")
+    ldv = _rows_arg(v, T, cache.width, dev, "out[1]")
     _require_cuda(slots, "slots")
-    cs = cache.struct()
-    st = reqat_kv4_gather(cs, T, slots.data_ptr(), k.data_ptr(), ldk, v.data_ptr(), ldv, 1 if add_shift else 0,
+    st = reqat_kv4_gather(cache.struct, T, slots.data_ptr(), k.data_ptr(), ldk, v.data_ptr(), ldv, 1 if add_shift else 0,
                           _stream(dev))
     _check(st, "reqat_kv4_gather")
     return k, v
+
+
+@functools.lru_cache(maxsize=1024)
+def _kv4_workspace(B, T, max_q, max_kv, q_heads, kv_heads, head_dim) -> int:
+    return reqat_kv4_attention_workspace_bytes(B, T, max_q, max_kv, q_heads, kv_heads, head_dim)
 
 
 def kv4_attention(q, cache, block_table, kv_len, q_start=None, max_q=None, max_kv=None, causal=True, sm_scale=None,
@@ -711,20 +722,19 @@ def kv4_attention(q, cache, block_table, kv_len, q_start=None, max_q=None, max_k
     if max_q is None:
         max_q = T if q_start is not None else 1
     if max_kv is None:
-        max_kv = min(cols * cache.page_size, 0x7FFFFFFF)
+        max_kv = min(cols * cache.page_size, 1 << 30)
     if sm_scale is None:
         sm_scale = D ** -0.5
     y = out if out is not None else torch.empty((T, q.shape[1]), dtype=torch.bfloat16, device=dev)
-    ldo = _out2d(y, T, q.shape[1], torch.bfloat16, dev, "out")
+    ldo = _rows_arg(y, T, q.shape[1], dev, "out")
     lse = torch.empty((T, q_heads), dtype=torch.float32, device=dev) if return_lse else None
-    need = reqat_kv4_attention_workspace_bytes(B, T, max_q, max_kv, q_heads, cache.kv_heads, D)
+    need = _kv4_workspace(B, T, max_q, max_kv, q_heads, cache.kv_heads, D)
     if ws is not None:
         _workspace_arg(ws, need, dev)
     _require_cuda(q, "q")
     if ws is None and need > 0:
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    cs = cache.struct()
-    st = reqat_kv4_attention(cs, B, T, q.data_ptr(), ldq, q_heads, _ptr(q_start), kv_len.data_ptr(),
+    st = reqat_kv4_attention(cache.struct, B, T, q.data_ptr(), ldq, q_heads, _ptr(q_start), kv_len.data_ptr(),
                              block_table.data_ptr(), ld_table, cols, max_q, max_kv, 1 if causal else 0, sm_scale,
                              y.data_ptr(), ldo, _ptr(lse), _ptr(ws) if need > 0 else None, _stream(dev))
     _check(st, "reqat_kv4_attention")

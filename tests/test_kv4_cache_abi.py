@@ -123,7 +123,7 @@ def test_binding_checks_before_any_call():
         reqat.Kv4Cache(4, 16, 2, 128, k_shift=torch.zeros(128), device="cpu")
     c = reqat.Kv4Cache(4, 16, 2, 128, device="cpu")
     assert c.k_codes.numel() == 4 * 16 * 2 * 64 and c.v_scales.numel() == 4 * 16 * 2 * 8 and c.width == 256
-    assert ctypes.sizeof(c.struct()) == 88
+    assert ctypes.sizeof(c.struct) == 88
     bf = lambda r, n: torch.zeros((r, n), dtype=torch.bfloat16)
     slots = torch.zeros(3, dtype=torch.int64)
     cos = torch.zeros((5, 64))
