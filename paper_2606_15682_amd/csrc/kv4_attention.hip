@@ -16,6 +16,7 @@
 #include "fp4_device.h"
 #include "g2l.h"
 #include "internal.h"
+#include "kv4_queue.h"
 
 namespace reqat {
 
@@ -127,20 +128,14 @@ __device__ __forceinline__ int visible(const Kv4AttnArgs &a, const Seq &s, int i
 //   O^T = V^T P^T (16 channels x 16 rows, K = 32 tokens): those eight tokens are its share of the K axis, so the weights
 //     are the operand as they stand, and the cache holds the values of four tokens together.  Tile c has channels
 //     8 w + c of the dwords w.
-// A step's codes and scales wait in LDS, kDepth steps ahead, each lane's where the lane finds them again: a queue that
-// takes no registers.
 template <int D> struct Step {
     uint32_t k[2][D / 32], ks[2];
     uint32_t v[2][4], vs[2];
 };
-struct Queue {
-    static constexpr int kDepth = 1;
-    static constexpr int kLoads = 8;                                     // of a step, in each wave
-    static constexpr int kStage = 4 * 1024 + 4 * 256;                    // keys, values of 16 + 16 tokens; their scales
-};
 
 template <int D, int NT, int W>
 __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs a, int splits, int chunk) {
+    using Queue = Kv4Queue;
     constexpr int KW = D / 32, VT = D / 16;
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -203,33 +198,31 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
             in_bits = in_bits << 1 | (in ? 1u : 0u);
             const int tok = (t + 16 * u) & pmask;
             const int64_t run = a.c.run(in ? p[u] : 0, h) + tok;      // tokens (values: a multiple of 4 of them)
-            g2l16(a.c.kc + run * (D / 2), k_at, stage + u * 1024);
-            g2l16(a.c.vc + run * (D / 2), v_at, stage + 2048 + u * 1024);
-            g2l4(a.c.ks + run * (D / 16), ks_at, stage + 4096 + u * 256);
-            g2l4(a.c.vs + run * (D / 16), vs_at, stage + 4608 + u * 256);
+            Queue::put(a.c.kc + run * (D / 2), k_at, a.c.vc + run * (D / 2), v_at, a.c.ks + run * (D / 16), ks_at,
+                       a.c.vs + run * (D / 16), vs_at, stage, u);
         }
     };
     auto take = [&](const uint8_t *stage, uint32_t bits, Step<D> &st) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if constexpr (D == 128) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(stage + u * 1024 + k_read);
+                const uint4 x = *reinterpret_cast<const uint4 *>(stage + Queue::kKeys + u * 1024 + k_read);
                 st.k[u][0] = x.x;
                 st.k[u][1] = x.y;
                 st.k[u][2] = x.z;
                 st.k[u][3] = x.w;
             } else {
-                const uint2 x = *reinterpret_cast<const uint2 *>(stage + u * 1024 + k_read);
+                const uint2 x = *reinterpret_cast<const uint2 *>(stage + Queue::kKeys + u * 1024 + k_read);
                 st.k[u][0] = x.x;
                 st.k[u][1] = x.y;
             }
-            const uint4 y = *reinterpret_cast<const uint4 *>(stage + 2048 + u * 1024 + lane * 16);
+            const uint4 y = *reinterpret_cast<const uint4 *>(stage + Queue::kValues + u * 1024 + lane * 16);
             st.v[u][0] = y.x;
             st.v[u][1] = y.y;
             st.v[u][2] = y.z;
             st.v[u][3] = y.w;
-            st.ks[u] = *reinterpret_cast<const uint32_t *>(stage + 4096 + u * 256 + lane * 4) >> ks_shift;
-            st.vs[u] = *reinterpret_cast<const uint32_t *>(stage + 4608 + u * 256 + lane * 4);
+            st.ks[u] = *reinterpret_cast<const uint32_t *>(stage + Queue::kKeyScales + u * 256 + lane * 4) >> ks_shift;
+            st.vs[u] = *reinterpret_cast<const uint32_t *>(stage + Queue::kValueScales + u * 256 + lane * 4);
             if (!(bits >> (1 - u) & 1u)) {                             // uniform: scores NaN, values zero
                 st.ks[u] = 0x7F7Fu;
                 st.vs[u] = 0u;
