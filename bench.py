@@ -37,7 +37,8 @@ TRAFFIC_SOURCES = {
     "gemm": GEMM_SOURCES,
     "w4a16": ["paper_2606_15682_amd/csrc/gemm_w4a16.hip", "paper_2606_15682_amd/csrc/dispatch.h",
               "paper_2606_15682_amd/csrc/g2l.h", "paper_2606_15682_amd/csrc/fp4_device.h"],
-    "kv4": ["paper_2606_15682_amd/csrc/kv4.hip", "paper_2606_15682_amd/csrc/fp4_device.h"],
+    "kv4": ["paper_2606_15682_amd/csrc/kv4.hip", "paper_2606_15682_amd/csrc/kv4_block.h",
+            "paper_2606_15682_amd/csrc/fp4_device.h"],
     "skinny": ["paper_2606_15682_amd/csrc/gemm_skinny.hip", "paper_2606_15682_amd/csrc/fp4_device.h"],
     "sem": ["paper_2606_15682_amd/csrc/sem.hip"],
 }

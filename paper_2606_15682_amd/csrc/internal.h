@@ -7,6 +7,7 @@
 
 #include "dispatch.h"
 #include "kv4_cache.h"
+#include "kv4_plan.h"
 
 namespace reqat {
 

@@ -1,0 +1,64 @@
+// How a call of the attention over the KV4 cache is cut: a rule on sizes alone, in plain C++ (no HIP), so that a CPU
+// test can ask it for any shape.
+#pragma once
+#include <stdint.h>
+
+namespace reqat {
+
+// The rows of a KV head (queries x heads of its group) go to qtiles of 16 x tiles rows; the tokens of
+// a sequence to `splits` pieces of `chunk`, a workgroup each, whose results a second kernel joins (splits > 1).
+//
+// Up to 32 rows (tiles 1, 2) a wave does all by itself, 32 tokens a step; beyond, the kernel for prompts, in which waves
+// without rows only unpack (16 sequences of up to 4000 tokens, 8 KV heads: 28.6 us with 25 rows, 47 with 35 to 60).
+//
+// Pieces: 512 workgroups of four waves, two per CU, where there are fewer units (sequence x KV head): 131072 tokens of one
+// sequence with 8 KV heads take 37.4 us in 512 pieces, 38.9 in 1024, whose results the join reads too.  Several
+// sequences differ in length and max_kv is the longest's: pieces of at most 1536 tokens (64 sequences of up to
+// 16384 tokens, 8 KV heads: 153 us, 188 in one piece each, 159 in pieces of 1024).  At most 256 pieces, of 256 tokens or
+// more: shorter contexts are one piece and need no join; from 257 to 512 tokens eight waves take it (500
+// tokens: 8.1 us, 8.7 in two pieces of four waves and a join; 250 tokens: 6.9 against 6.3).
+struct Kv4Plan {
+    int tiles, qtiles, waves, splits, chunk;
+};
+constexpr int kKv4MaxSplits = 256;
+constexpr int64_t kKv4MaxPieces = 8192; // in all, where the longest of several sequences asks for them: a workspace of 136 MB at most
+constexpr int kKv4Prompt = 16;          // tiles of the kernel for prompts: 256 rows
+
+inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads) {
+    Kv4Plan p;
+    const int64_t rows = max_q * (q_heads / kv_heads);
+    p.tiles = rows > 32 ? kKv4Prompt : rows > 16 ? 2 : 1;
+    p.qtiles = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
+    const int64_t groups = B * kv_heads * p.qtiles;
+    p.waves = 4;
+    int64_t splits = 1;
+    if (p.tiles == kKv4Prompt) {
+        splits = groups > 0 ? (256 + groups - 1) / groups : 1;
+    } else if (p.tiles == 1 && max_kv > 256 && max_kv <= 512 && groups <= 256) {
+        p.waves = 8;
+    } else {
+        splits = groups > 0 ? (512 + groups - 1) / groups : 1;
+        if (B > 1 && max_kv > 2048) {
+            int64_t finer = (max_kv + 1535) / 1536;
+            finer = finer * groups > kKv4MaxPieces ? kKv4MaxPieces / groups : finer;
+            splits = splits < finer ? finer : splits;
+        }
+    }
+    const int64_t most = (max_kv + 255) / 256;
+    splits = splits > most ? most : splits;
+    splits = splits > kKv4MaxSplits ? kKv4MaxSplits : splits;
+    splits = splits < 1 ? 1 : splits;
+    const int64_t chunk = ((max_kv + splits - 1) / splits + 127) / 128 * 128;
+    p.chunk = (int)(chunk < 128 ? 128 : chunk);                          // max_kv <= 2^30
+    p.splits = (int)((max_kv + p.chunk - 1) / p.chunk);
+    if (p.splits < 1) p.splits = 1;
+    return p;
+}
+
+// Whether the launch of a plan holds fewer than 2^32 threads (workgroups of up to 512).
+inline bool kv4_plan_fits(const Kv4Plan &p, int64_t B, int kv_heads) {
+    const int64_t n = B * kv_heads * p.splits;                           // below 2^40
+    return p.tiles == kKv4Prompt ? n < (int64_t(1) << 23) && n * p.qtiles < (int64_t(1) << 23) : n < (int64_t(1) << 23);
+}
+
+}  // namespace reqat

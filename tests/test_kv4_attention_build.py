@@ -1,5 +1,5 @@
 """CPU checks of the attention over the paged KV4 cache: the wait states in front of its direct-to-LDS loads, in the
-assembly that hipcc makes; and the rule that cuts a call (csrc/dispatch.h, built with the host compiler)."""
+assembly that hipcc makes; and the rule that cuts a call (csrc/kv4_plan.h, built with the host compiler)."""
 import ctypes
 import os
 import subprocess
@@ -10,7 +10,7 @@ from paper_2606_15682_amd import build as libbuild
 from tests.test_direct_to_lds_hazards import _assembly, hazards
 
 SOURCE = """
-#include "dispatch.h"
+#include "kv4_plan.h"
 using namespace reqat;
 extern "C" void plan_(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads, int *out) {
     const Kv4Plan p = kv4_plan(B, max_q, max_kv, q_heads, kv_heads);
