@@ -193,8 +193,16 @@ __device__ __forceinline__ uint4 decode8(uint32_t w, uint32_t sbyte, const Kv4G 
     return bad ? make_uint4(nan, nan, nan, nan) : make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+// 16 bytes written past the L2, which has codes to keep: at 32768 tokens of 8 heads 34.4 us against 45.5, at 2000 tokens
+// 5.0 against 5.3.  (For the queries of the append it is no gain: 8000 tokens of 40 + 8 + 8 heads 51 us against 48.)
+__device__ __forceinline__ void stream16(uint16_t *__restrict__ p, const uint4 &x) {
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u4, x), reinterpret_cast<u4 *>(p));
+}
+
 // A thread's item is eight channels of one head of one slot, keys and values: a wave writes 1 KB of adjacent bytes
 // at a time (with 16 channels a thread and two stores of every other 16 bytes, 32768 tokens of 8 heads took 54 us).
+// 172 MB in 34.4 us, 5.0 TB/s: the rate of a copy.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const Kv4View c, const int64_t *__restrict__ slots, int T,
                                                               uint16_t *__restrict__ ky, int64_t ldk,
@@ -219,8 +227,8 @@ __global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const Kv4View c, c
             v = decode8(x, c.vs[kv4_v_scales(run, tok, w / 2, D)], kv4_make_g(*c.gv), nullptr);
         }
     }
-    if (ky) *reinterpret_cast<uint4 *>(ky + t * ldk + at) = k;
-    if (vy) *reinterpret_cast<uint4 *>(vy + t * ldv + at) = v;
+    if (ky) stream16(ky + t * ldk + at, k);
+    if (vy) stream16(vy + t * ldv + at, v);
 }
 
 // Tokens of one launch: its items (at most 16 a token and head) are numbered in 32 bits.
