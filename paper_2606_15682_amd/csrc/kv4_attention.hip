@@ -785,9 +785,13 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         auto step = [&](auto edge) __attribute__((always_inline)) {
             const uint8_t *now = stage(slot), *next = stage(slot + 1);
             if (keys) turn();
+            __builtin_amdgcn_s_setprio(1);                               // matrix instructions before the other wave's unpacking
             if (busy) block(before, now + C::kSub, now, next, t, s0, s1, p, edge);
+            __builtin_amdgcn_s_setprio(0);
             if (!keys) turn();
+            __builtin_amdgcn_s_setprio(1);
             if (busy) block(now, next, now + C::kSub, next + C::kSub, t + 32, s1, s0, p, edge);
+            __builtin_amdgcn_s_setprio(0);
             before = now + C::kSub;
             ++slot;
             t += 64;
