@@ -194,7 +194,7 @@ __device__ __forceinline__ uint4 decode8(uint32_t w, uint32_t sbyte, const Kv4G 
 }
 
 // 16 bytes written past the L2, which has codes to keep: at 32768 tokens of 8 heads 34.4 us against 45.5, at 2000 tokens
-// 5.0 against 5.3.  (For the queries of the append it is no gain: 8000 tokens of 40 + 8 + 8 heads 51 us against 48.)
+// 5.0 against 5.3 (before each XCD took a run of them).  (For the queries of the append it is no gain: 8000 tokens of 40 + 8 + 8 heads 51 us against 48.)
 __device__ __forceinline__ void stream16(uint16_t *__restrict__ p, const uint4 &x) {
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
     __builtin_nontemporal_store(__builtin_bit_cast(u4, x), reinterpret_cast<u4 *>(p));
@@ -202,13 +202,18 @@ __device__ __forceinline__ void stream16(uint16_t *__restrict__ p, const uint4 &
 
 // A thread's item is eight channels of one head of one slot, keys and values: a wave writes 1 KB of adjacent bytes
 // at a time (with 16 channels a thread and two stores of every other 16 bytes, 32768 tokens of 8 heads took 54 us).
-// 172 MB in 34.4 us, 5.0 TB/s: the rate of a copy.
+// Workgroups are dealt to the eight XCDs in turn; each XCD takes a contiguous run of items, since four adjacent tokens share
+// the 16-byte pieces of their value codes and sixteen a line of their scales, which two and eight XCDs then fetched
+// (32768 tokens of 8 heads: 86 MB read for 38, 34.5 us against 31.8; 5003 of 4 heads: 4.5 against 4.1).  172 MB in
+// 31.8 us, 5.4 TB/s: bound by memory, a copy runs at 5.2.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const Kv4View c, const int64_t *__restrict__ slots, int T,
                                                               uint16_t *__restrict__ ky, int64_t ldk,
                                                               uint16_t *__restrict__ vy, int64_t ldv, bool add_shift) {
     constexpr int kWords = D / 8;
-    const uint32_t item = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t xcd = blockIdx.x % 8, per = gridDim.x / 8, rem = gridDim.x % 8;
+    const uint32_t block = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / 8;
+    const uint32_t item = block * kThreads + threadIdx.x;
     const uint32_t th = item / kWords, t = th / c.heads;
     if (t >= (uint32_t)T) return;
     const int w = (int)(item % kWords), h = (int)(th - t * c.heads);
