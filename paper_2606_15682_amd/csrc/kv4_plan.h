@@ -12,9 +12,9 @@ namespace reqat {
 // without rows only unpack (16 sequences of up to 4000 tokens, 8 KV heads: 28.6 us with 25 rows, 47 with 35 to 60).
 //
 // Pieces: 512 workgroups of four waves, two per CU, where there are fewer units (sequence x KV head): 131072 tokens of one
-// sequence with 8 KV heads take 37.4 us in 512 pieces, 38.9 in 1024, whose results the join reads too.  Several
+// sequence with 8 KV heads take 34.4 us in 512 pieces, 37.5 in 1024, whose results the join reads too.  Several
 // sequences differ in length and max_kv is the longest's: pieces of at most 1536 tokens (64 sequences of up to
-// 16384 tokens, 8 KV heads: 153 us, 188 in one piece each, 159 in pieces of 1024).  At most 256 pieces, of 256 tokens or
+// 16384 tokens, 8 KV heads: 142 us, 169 in one piece each, 151 in pieces of 1024 or 2048).  At most 256 pieces, of 256 tokens or
 // more: shorter contexts are one piece and need no join; from 257 to 512 tokens eight waves take it (500
 // tokens: 8.1 us, 8.7 in two pieces of four waves and a join; 250 tokens: 6.9 against 6.3).
 struct Kv4Plan {
