@@ -10,7 +10,8 @@
 // numbers (those below 2^-28 of the largest are rounded, to 2^-39 of it).  The scores sum in FP32.  Weights p =
 // 2^(s - r) are rounded to FP16 (11 bits, 3 more than the output has): r trails the running maximum,
 // at least 7 and at most 15 below it, so p is at most 2^15 and the FP16 range reaches 2^-31 of the largest
-// weight or below; the sum of weights is taken in FP32 before that rounding.
+// weight or below; the sum of weights is taken in FP32 before that rounding.  In a row whose largest exponent passes 2^24,
+// where FP32 has no number 7 below it, weights count from the score itself: Reference.
 #include <type_traits>
 
 #include "fp4_device.h"
@@ -33,9 +34,14 @@ constexpr uint32_t kCodeMask = 0x80708070u;    // sign and magnitude of a code i
 constexpr float kScaleUp = 128.0f;             // FP16 scales are s 2^7
 constexpr float kBelow = 7.0f;                 // r = maximum - kBelow when it is renewed
 constexpr float kMostSum = 32768.0f;           // ... which it is when a lane's weights of a step sum to more: none is above
+constexpr float kMostLarge = 11.0f;            // and when an exponent of a large score's row is above this: the sum of 16 stays below
+constexpr float kLargeScore = 0x1p24f;         // exponents from which a reference is a score
+constexpr float kHugeFactor = 0x1p100f;        // factors from which an exponent may pass the FP32 range (scores stay below 2^21)
+constexpr double kNoPiece = -0x1p1000;         // below every reference
 constexpr int kNoToken = 0x7FFFFFFF;
 constexpr float kLowest = -3.4028234663852886e38f;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.6931471805599453;
 
 __device__ __forceinline__ uint32_t scaled(uint32_t code_bits, h2 s) {
     return __builtin_bit_cast(uint32_t, (h2)(__builtin_bit_cast(h2, code_bits) * s));
@@ -85,9 +91,55 @@ __device__ __forceinline__ h8 query_f16(const uint4 &w, int shift) {
 }
 
 // From scores of such a row to exponents of two.  A code is half its integer: 2^-13 n s = 2^-12 (n / 2) s.
+// Finite, since a score minus itself is multiplied by it: at the bound any two scores are still worlds apart.
 __device__ __forceinline__ float score_factor(const Kv4AttnArgs &a, int shift) {
-    return __builtin_fmaxf(__builtin_ldexpf(a.scale * kLog2e * *a.c.gk * 4096.0f, -shift), 0x1p-126f);
+    const float c = __builtin_ldexpf(a.scale * kLog2e * *a.c.gk * 4096.0f, -shift);
+    return __builtin_fminf(__builtin_fmaxf(c, 0x1p-126f), 0x1p127f);
 }
+
+// What a row's weights p = 2^(s c - r) are taken from.  r = RN(RN(s' c) - 7), s' the highest score when it was renewed,
+// as long as that leaves r well-defined.  From exponents of 2^24 on the step from one FP32 number to the next swallows
+// the 7 (and later the FP16 range): then p = 2^((s - s') c + 7), exact near s', and r is NaN, whose sums send every
+// step of such a row to the branch that takes this form.  FP64 holds s' c - 7 of both kinds for joining.
+struct Reference {
+    float r, score;
+
+    __device__ __forceinline__ bool large() const { return r != r; }
+    __device__ __forceinline__ void none(float c) {                      // below every score
+        r = c < kHugeFactor ? kLowest : __builtin_nanf("");
+        score = kLowest;
+    }
+    // From the highest score and the sum of a step's weights, in the first form: whether they are too large for it.
+    __device__ __forceinline__ bool outgrown(float top, float c, float total) const {
+        return large() ? __builtin_fmaf(top - score, c, kBelow) > kMostLarge : total > kMostSum;
+    }
+    // Renewed for `top`; returns what weights so far change by.
+    __device__ __forceinline__ float renew(float top, float c) {
+        const float t = top * c, next = c < kHugeFactor && __builtin_fabsf(t) < kLargeScore ? t - kBelow : __builtin_nanf("");
+        const bool next_large = next != next;
+        const float x = large() ? (next_large ? (score - top) * c : __builtin_fmaf(score, c, -next) - kBelow)
+                                : (next_large ? __builtin_fmaf(-top, c, r) + kBelow : r - next);
+        r = next;
+        score = top;
+        return __builtin_amdgcn_exp2f(x);
+    }
+    __device__ __forceinline__ float weight(float s, float c) const {
+        return __builtin_amdgcn_exp2f(__builtin_fmaf(s - (large() ? score : 0.0f), c, large() ? kBelow : -r));
+    }
+    __device__ __forceinline__ double at(float c) const { return large() ? (double)score * c - kBelow : (double)r; }
+};
+
+__device__ __forceinline__ float exp2_of(double below) { return __builtin_amdgcn_exp2f((float)below); }
+
+__device__ __forceinline__ float log_sum(double at, float sum) {
+    return (float)((at + (double)__builtin_log2f(sum)) * kLn2);
+}
+
+// A row's share of a call that is cut into pieces, beside its unfinished output: reference and sum of weights.
+struct __attribute__((aligned(16))) PieceRow {
+    double at;
+    float sum, unused;
+};
 
 // The queries and tokens of sequence b.
 struct Seq {
@@ -250,7 +302,8 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
 
     // queries (rows beyond the last repeat the first), the factor from scores to exponents, and what each row sees
     h8 qf[NT][KW];
-    float c[NT], ref[NT], sum[NT];
+    float c[NT], sum[NT];
+    Reference ref[NT];
     int see[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -268,7 +321,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
 #pragma unroll
         for (int j = 0; j < KW; ++j) qf[n][j] = query_f16(w[j], shift);
         c[n] = score_factor(a, shift);
-        ref[n] = kLowest;
+        ref[n].none(c[n]);
         sum[n] = 0.0f;
     }
     f32x4 o[VT][NT];
@@ -323,18 +376,16 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
             float e[8], total = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][n][i & 3], c[n], -ref[n]));
+                e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][n][i & 3], c[n], -ref[n].r));
                 total += e[i];
             }
-            if (__any(total > kMostSum)) {
-                const bool need = max16(total) > kMostSum;              // a row moves by its own scores alone
+            if (__any(!(total <= kMostSum))) {                           // or NaN: large scores, and what is NaN in earnest
                 float top = s[0][n][0];
 #pragma unroll
                 for (int i = 1; i < 8; ++i) top = __builtin_fmaxf(top, s[i >> 2][n][i & 3]);
                 top = max16(top);
-                const float next = need ? top * c[n] - kBelow : ref[n];
-                const float f = __builtin_amdgcn_exp2f(ref[n] - next);
-                ref[n] = next;
+                float f = 1.0f;
+                if (ref[n].outgrown(top, c[n], max16(total))) f = ref[n].renew(top, c[n]);   // by the row's own scores alone
                 sum[n] *= f;
 #pragma unroll
                 for (int x = 0; x < VT; ++x)
@@ -343,7 +394,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
                 total = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][n][i & 3], c[n], -ref[n]));
+                    e[i] = ref[n].weight(s[i >> 2][n][i & 3], c[n]);
                     total += e[i];
                 }
             }
@@ -416,12 +467,13 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
     // Join the waves: references and sums first, then the rows through LDS.  `finish` turns a row's joined sum into
     // its output; a split leaves its rows as they are, with their reference and sum of weights beside them.
     float (*part)[16][kLd] = reinterpret_cast<float (*)[16][kLd]>(lds);
-    __shared__ float refs[W][16 * NT], sums[W][16 * NT], finish[16 * NT];
+    __shared__ double refs[W][16 * NT];
+    __shared__ float sums[W][16 * NT], finish[16 * NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         sum[n] = sum16(sum[n]);
         if (g == 0) {
-            refs[wave][16 * n + r] = ref[n];
+            refs[wave][16 * n + r] = ref[n].at(c[n]);
             sums[wave][16 * n + r] = sum[n];
         }
     }
@@ -431,28 +483,27 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
     if ((int)threadIdx.x < rows) {
         const int row = threadIdx.x, i = row / group;
         const int64_t at = (sq.q0 + i) * a.q_heads + h * group + (row - i * group);
-        float top = kLowest, total = 0.0f;
+        double top = refs[0][threadIdx.x];
+        float total = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) top = __builtin_fmaxf(top, refs[w][threadIdx.x]);
+        for (int w = 1; w < W; ++w) top = __builtin_fmax(top, refs[w][threadIdx.x]);
 #pragma unroll
         for (int w = 0; w < W; ++w)
-            total = __builtin_fmaf(sums[w][threadIdx.x], __builtin_amdgcn_exp2f(refs[w][threadIdx.x] - top), total);
+            total = __builtin_fmaf(sums[w][threadIdx.x], exp2_of(refs[w][threadIdx.x] - top), total);
         if (splits > 1) {
-            float *pm = po + (int64_t)splits * all * D + 2 * (split * all + at);
-            pm[0] = top;
-            pm[1] = total;
+            reinterpret_cast<PieceRow *>(po + (int64_t)splits * all * D)[split * all + at] = {top, total, 0.0f};
         } else {
             const bool none = visible(a, sq, i) == 0 && !sq.lost;
             finish[threadIdx.x] = sq.lost ? __builtin_nanf("") : none ? 0.0f : *a.c.gv * 4096.0f / total;
-            if (a.lse) a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (top + __builtin_log2f(total)) * kLn2;
+            if (a.lse) a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(top, total);
         }
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        float m = refs[0][16 * n + r];
+        double m = refs[0][16 * n + r];
 #pragma unroll
-        for (int w = 1; w < W; ++w) m = __builtin_fmaxf(m, refs[w][16 * n + r]);
-        const float f = __builtin_amdgcn_exp2f(ref[n] - m);
+        for (int w = 1; w < W; ++w) m = __builtin_fmax(m, refs[w][16 * n + r]);
+        const float f = exp2_of(ref[n].at(c[n]) - m);
         if (n > 0) __syncthreads();
         auto at = [&](int x, int i) -> float & {
             const int rho = 4 * g + i;
@@ -682,7 +733,8 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         fetch(t0 + 64, entries[1], z1);
     }
     h8 qf[C::F];
-    float c, ref = kLowest, sum = 0.0f;
+    float c, sum = 0.0f;
+    Reference ref;
     {
         const uint16_t *src = a.q + (sq.q0 + qi) * a.ldq + (int64_t)hq * D + 8 * up;
         uint4 w[C::F];
@@ -694,6 +746,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
 #pragma unroll
         for (int j = 0; j < C::F; ++j) qf[j] = query_f16(w[j], shift);
         c = score_factor(a, shift);
+        ref.none(c);
     }
     // Operand m of a block: the products with 32 tokens' values (sub) and with the keys of 32 later ones, in turn.
     auto operand = [&](const uint8_t *sub, const uint8_t *keys_at, int m) __attribute__((always_inline)) {
@@ -720,7 +773,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
             return __builtin_bit_cast(uint32_t, z);
         };
         uint32_t w[8];
-        float total = 0.0f, e[2], arg = __builtin_fmaf(s[0], c, -ref);
+        float total = 0.0f, e[2], arg = __builtin_fmaf(s[0], c, -ref.r);
 #pragma unroll
         for (int v = 0; v < 16; ++v) ahead[v] = 0.0f;
         __builtin_amdgcn_sched_barrier(0);
@@ -734,7 +787,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
             for (int y = 0; y < kEach; ++y) {
                 const int v = m * kEach + y;
                 const float now = __builtin_amdgcn_exp2f(arg);           // used one element later: it takes a while
-                if (v < 15) arg = __builtin_fmaf(s[(v + 1) & 15], c, -ref);
+                if (v < 15) arg = __builtin_fmaf(s[(v + 1) & 15], c, -ref.r);
                 if (v > 0) total += e[(v - 1) & 1];
                 if (v > 0 && !(v & 1)) w[(v - 2) >> 1] = pack(e[0], e[1]);
                 e[v & 1] = now;
@@ -743,15 +796,13 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         });
         total += e[1];
         w[7] = pack(e[0], e[1]);
-        if (__any(total > kMostSum)) {
-            const bool need = __builtin_fmaxf(total, __shfl_xor(total, 32, 64)) > kMostSum;   // a row moves by its own scores alone
+        if (__any(!(total <= kMostSum))) {                               // or NaN, as in the kernel above
             float top = s[0];
 #pragma unroll
             for (int v = 1; v < 16; ++v) top = __builtin_fmaxf(top, s[v]);
             top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
-            const float next = need ? top * c - kBelow : ref;
-            const float f = __builtin_amdgcn_exp2f(ref - next);
-            ref = next;
+            float f = 1.0f;
+            if (ref.outgrown(top, c, __builtin_fmaxf(total, __shfl_xor(total, 32, 64)))) f = ref.renew(top, c);   // by the row's own scores alone
             sum *= f;
 #pragma unroll
             for (int x = 0; x < VT; ++x)
@@ -760,8 +811,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
             total = 0.0f;
 #pragma unroll
             for (int v = 0; v < 16; v += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -ref));
-                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v + 1], c, -ref));
+                const float e0 = ref.weight(s[v], c), e1 = ref.weight(s[v + 1], c);
                 total += e0;
                 total += e1;
                 w[v >> 1] = pack(e0, e1);
@@ -844,11 +894,9 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     const float f = splits > 1 ? 1.0f : sq.lost ? __builtin_nanf("") : none ? 0.0f : *a.c.gv * 4096.0f / sum;
     if (up == 0 && there) {
         if (splits > 1) {
-            float *pm = po + (int64_t)splits * all * D + 2 * (split * all + at);
-            pm[0] = ref;
-            pm[1] = sum;
+            reinterpret_cast<PieceRow *>(po + (int64_t)splits * all * D)[split * all + at] = {ref.at(c), sum, 0.0f};
         } else if (a.lse) {
-            a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (ref + __builtin_log2f(sum)) * kLn2;
+            a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(ref.at(c), sum);
         }
     }
 #pragma unroll
@@ -896,48 +944,50 @@ __global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, i
     if (i >= sq.nq) return;
     const int64_t at = (sq.q0 + i) * a.q_heads + hq, all = a.T * a.q_heads;
     const float *po = reinterpret_cast<const float *>(a.workspace);
-    const float *pm = po + (int64_t)splits * all * D;
-    float ref[S], weight[S], y[S][C];
+    const PieceRow *pm = reinterpret_cast<const PieceRow *>(po + (int64_t)splits * all * D);
+    double ref[S];
+    float weight[S], y[S][C];
 #pragma unroll
     for (int k = 0; k < S; ++k) {
         const int s = wave + k * W;
         const int64_t slot = (s < splits ? s : 0) * all + at;
-        ref[k] = pm[2 * slot];
-        weight[k] = pm[2 * slot + 1];
+        ref[k] = pm[slot].at;
+        weight[k] = pm[slot].sum;
 #pragma unroll
         for (int e = 0; e < C; ++e) y[k][e] = po[slot * D + lane * C + e];
     }
     const int n = visible(a, sq, i);
     const int have = sq.lost ? 0 : (n + chunk - 1) / chunk;              // the splits with a token that the row sees
-    float m = kLowest;
+    double m = kNoPiece;
 #pragma unroll
     for (int k = 0; k < S; ++k)
-        if (wave + k * W < have) m = __builtin_fmaxf(m, ref[k]);
+        if (wave + k * W < have) m = __builtin_fmax(m, ref[k]);
     float total = 0.0f, z[C] = {};
 #pragma unroll
     for (int k = 0; k < S; ++k)
         if (wave + k * W < have) {
-            const float f = __builtin_amdgcn_exp2f(ref[k] - m);
+            const float f = exp2_of(ref[k] - m);
             total = __builtin_fmaf(weight[k], f, total);
 #pragma unroll
             for (int e = 0; e < C; ++e) z[e] = __builtin_fmaf(y[k][e], f, z[e]);
         }
     if constexpr (W > 1) {
-        __shared__ float part[W][C + 2][64];
+        __shared__ float part[W][C + 1][64];
+        __shared__ double tops[W];
 #pragma unroll
         for (int e = 0; e < C; ++e) part[wave][e][lane] = z[e];
         part[wave][C][lane] = total;
-        part[wave][C + 1][lane] = m;
+        if (lane == 0) tops[wave] = m;
         __syncthreads();
         if (wave > 0) return;
 #pragma unroll
-        for (int w = 1; w < W; ++w) m = __builtin_fmaxf(m, part[w][C + 1][lane]);
+        for (int w = 1; w < W; ++w) m = __builtin_fmax(m, tops[w]);
         total = 0.0f;
 #pragma unroll
         for (int e = 0; e < C; ++e) z[e] = 0.0f;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const float f = __builtin_amdgcn_exp2f(part[w][C + 1][lane] - m);
+            const float f = exp2_of(tops[w] - m);
             total = __builtin_fmaf(part[w][C][lane], f, total);
 #pragma unroll
             for (int e = 0; e < C; ++e) z[e] = __builtin_fmaf(part[w][e][lane], f, z[e]);
@@ -949,7 +999,7 @@ __global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, i
     if constexpr (C == 2) *reinterpret_cast<uint32_t *>(dst) = bf16_rne_from_float(z[0] * f) | (bf16_rne_from_float(z[1] * f) << 16);
     else dst[0] = (uint16_t)bf16_rne_from_float(z[0] * f);
     if (a.lse && lane == 0)
-        a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : (m + __builtin_log2f(total)) * kLn2;
+        a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(m, total);
 }
 
 template <int D, int NT, int W> void decode(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
@@ -989,7 +1039,7 @@ template <int D> hipError_t attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipSt
 
 size_t kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads, int D) {
     const Kv4Plan p = kv4_plan(B, max_q, max_kv, q_heads, kv_heads);
-    return p.splits > 1 ? (size_t)p.splits * (size_t)T * (size_t)q_heads * (size_t)(D + 2) * 4 : 0;
+    return p.splits > 1 ? (size_t)p.splits * (size_t)T * (size_t)q_heads * ((size_t)D * 4 + sizeof(PieceRow)) : 0;
 }
 
 hipError_t launch_kv4_attention(const Kv4AttnArgs &a, hipStream_t stream) {

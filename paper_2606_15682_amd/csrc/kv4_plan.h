@@ -21,7 +21,7 @@ struct Kv4Plan {
     int tiles, qtiles, waves, splits, chunk;
 };
 constexpr int kKv4MaxSplits = 256;
-constexpr int64_t kKv4MaxPieces = 8192; // in all, where the longest of several sequences asks for them: a workspace of 136 MB at most
+constexpr int64_t kKv4MaxPieces = 8192; // in all, where the longest of several sequences asks for them: a workspace of 138 MB at most
 constexpr int kKv4Prompt = 16;          // tiles of the kernel for prompts: 256 rows
 
 inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads) {
