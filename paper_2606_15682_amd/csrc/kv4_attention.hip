@@ -92,8 +92,11 @@ __device__ __forceinline__ h8 query_f16(const uint4 &w, int shift) {
 
 // From scores of such a row to exponents of two.  A code is half its integer: 2^-13 n s = 2^-12 (n / 2) s.
 // Finite, since a score minus itself is multiplied by it: at the bound any two scores are still worlds apart.
+// Exponents apart: the scales' product may leave the FP32 range where the factor does not.
 __device__ __forceinline__ float score_factor(const Kv4AttnArgs &a, int shift) {
-    const float c = __builtin_ldexpf(a.scale * kLog2e * *a.c.gk * 4096.0f, -shift);
+    const float g = *a.c.gk;
+    const float c = __builtin_ldexpf(__builtin_amdgcn_frexp_mantf(a.scale) * kLog2e * __builtin_amdgcn_frexp_mantf(g),
+                                     __builtin_amdgcn_frexp_expf(a.scale) + __builtin_amdgcn_frexp_expf(g) + 12 - shift);
     return __builtin_fminf(__builtin_fmaxf(c, 0x1p-126f), 0x1p127f);
 }
 
@@ -133,6 +136,12 @@ __device__ __forceinline__ float exp2_of(double below) { return __builtin_amdgcn
 
 __device__ __forceinline__ float log_sum(double at, float sum) {
     return (float)((at + (double)__builtin_log2f(sum)) * kLn2);
+}
+
+// What a row's sum of weights and values is multiplied by; the scale of the values comes last, so that it alone can
+// leave the FP32 range, as the values then do.
+__device__ __forceinline__ float finish_factor(bool lost, bool none, float sum) {
+    return lost ? __builtin_nanf("") : none ? 0.0f : 4096.0f / sum;
 }
 
 // A row's share of a call that is cut into pieces, beside its unfinished output: reference and sum of weights.
@@ -494,7 +503,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
             reinterpret_cast<PieceRow *>(po + (int64_t)splits * all * D)[split * all + at] = {top, total, 0.0f};
         } else {
             const bool none = visible(a, sq, i) == 0 && !sq.lost;
-            finish[threadIdx.x] = sq.lost ? __builtin_nanf("") : none ? 0.0f : *a.c.gv * 4096.0f / total;
+            finish[threadIdx.x] = finish_factor(sq.lost, none, total);
             if (a.lse) a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(top, total);
         }
     }
@@ -532,9 +541,9 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
             if (splits > 1) {
                 *reinterpret_cast<float2 *>(po + (split * all + (sq.q0 + i) * a.q_heads + hq) * D + ch) = make_float2(y0, y1);
             } else {
-                const float f1 = finish[16 * n + rr];
+                const float f1 = finish[16 * n + rr], g1 = *a.c.gv;
                 *reinterpret_cast<uint32_t *>(a.out + (sq.q0 + i) * a.ldo + (int64_t)hq * D + ch) =
-                    bf16_rne_from_float(y0 * f1) | (bf16_rne_from_float(y1 * f1) << 16);
+                    bf16_rne_from_float(y0 * f1 * g1) | (bf16_rne_from_float(y1 * f1 * g1) << 16);
             }
         }
     }
@@ -891,7 +900,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     const int64_t all = a.T * a.q_heads, at = (sq.q0 + qi) * a.q_heads + hq;
     sum += __shfl_xor(sum, 32, 64);
     const bool none = see == 0 && !sq.lost;
-    const float f = splits > 1 ? 1.0f : sq.lost ? __builtin_nanf("") : none ? 0.0f : *a.c.gv * 4096.0f / sum;
+    const float f = splits > 1 ? 1.0f : finish_factor(sq.lost, none, sum), g1 = splits > 1 ? 1.0f : *a.c.gv;
     if (up == 0 && there) {
         if (splits > 1) {
             reinterpret_cast<PieceRow *>(po + (int64_t)splits * all * D)[split * all + at] = {ref.at(c), sum, 0.0f};
@@ -904,7 +913,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int rho = 8 * (v >> 2) + 4 * up + (v & 3);
-            mine[col * kLd + 8 * (rho % WD) + CPT * x + rho / WD] = none ? 0.0f : o[x][v] * f;
+            mine[col * kLd + 8 * (rho % WD) + CPT * x + rho / WD] = none ? 0.0f : o[x][v] * f * g1;
         }
     __builtin_amdgcn_wave_barrier();
     const int64_t my_out = splits > 1 ? (split * all + at) * D : (sq.q0 + qi) * a.ldo + (int64_t)hq * D;
@@ -994,10 +1003,10 @@ __global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, i
         }
     }
     const bool none = n == 0 && !sq.lost;
-    const float f = sq.lost ? __builtin_nanf("") : none ? 0.0f : *a.c.gv * 4096.0f / total;
+    const float f = finish_factor(sq.lost, none, total), g1 = *a.c.gv;
     uint16_t *dst = a.out + (sq.q0 + i) * a.ldo + (int64_t)hq * D + lane * C;
-    if constexpr (C == 2) *reinterpret_cast<uint32_t *>(dst) = bf16_rne_from_float(z[0] * f) | (bf16_rne_from_float(z[1] * f) << 16);
-    else dst[0] = (uint16_t)bf16_rne_from_float(z[0] * f);
+    if constexpr (C == 2) *reinterpret_cast<uint32_t *>(dst) = bf16_rne_from_float(z[0] * f * g1) | (bf16_rne_from_float(z[1] * f * g1) << 16);
+    else dst[0] = (uint16_t)bf16_rne_from_float(z[0] * f * g1);
     if (a.lse && lane == 0)
         a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(m, total);
 }
