@@ -370,8 +370,8 @@ reqat_status reqat_kv4_gather(const reqat_kv4_cache *cache, int64_t T, const int
  *     size the launch).
  *   out [T][ldo] bfloat16; lse NULL or [T][q_heads] FP32, the natural logarithm
  *     of sum_j exp(sm_scale q . k^_j) (of the shifted keys).
- *   workspace: reqat_kv4_attention_workspace_bytes(...) bytes, 16-byte aligned
- *     (may be NULL when that is 0): partial results of long sequences.
+ *   workspace: at least reqat_kv4_attention_workspace_bytes(...) bytes, 16-byte
+ *     aligned (may be NULL when that is 0): partial results of long sequences.
  * A row without a visible token gets zeros and lse -Inf.  What a row does not
  * see does not reach it, NaN included; a NaN or Inf in its query or a NaN among
  * its visible keys or values does.  A visible token whose page entry lies outside the
@@ -391,7 +391,12 @@ reqat_status reqat_kv4_attention(const reqat_kv4_cache *cache, int64_t B, int64_
                                  int64_t max_kv, int causal, float sm_scale, void *out, int64_t ldo, float *lse,
                                  void *workspace, void *stream);
 
-/* Bytes of workspace reqat_kv4_attention needs (0: none; 0 on bad arguments). */
+/*
+ * Bytes of workspace that serve reqat_kv4_attention with these sizes (0: none; 0
+ * on bad arguments), and with any smaller B, T, max_q and max_kv of the same
+ * heads: the size never falls as one of them grows, so one workspace of a loop's
+ * largest sizes serves all its calls.
+ */
 size_t reqat_kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int64_t q_heads,
                                            int64_t kv_heads, int64_t head_dim);
 

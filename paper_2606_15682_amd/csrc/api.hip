@@ -250,7 +250,7 @@ static bool kv4_attention_sizes_ok(int64_t B, int64_t T, int64_t max_q, int64_t 
 size_t reqat_kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int64_t q_heads,
                                            int64_t kv_heads, int64_t head_dim) {
     if (!kv4_attention_sizes_ok(B, T, max_q, max_kv, q_heads, kv_heads) || (head_dim != 64 && head_dim != 128)) return 0;
-    return kv4_attention_workspace_bytes(B, T, max_q < T ? max_q : T, max_kv, (int)q_heads, (int)kv_heads, (int)head_dim);
+    return kv4_attention_workspace_bytes(B, max_q < T ? max_q : T, max_kv, (int)q_heads, (int)kv_heads, (int)head_dim);
 }
 
 reqat_status reqat_kv4_attention(const reqat_kv4_cache *cache, int64_t B, int64_t T, const void *q, int64_t ldq,
@@ -272,9 +272,9 @@ reqat_status reqat_kv4_attention(const reqat_kv4_cache *cache, int64_t B, int64_
          reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(lse)) & 3u)
         return REQAT_E_ALIGN;
     if (max_q > T) max_q = T;
-    if (!kv4_plan_fits(kv4_plan(B, max_q, max_kv, (int)q_heads, view.heads), B, view.heads)) return REQAT_E_SHAPE;
-    const size_t need = kv4_attention_workspace_bytes(B, T, max_q, max_kv, (int)q_heads, view.heads, view.D);
-    if (need > 0 && !workspace) return REQAT_E_NULL;
+    const Kv4Plan plan = kv4_plan(B, max_q, max_kv, (int)q_heads, view.heads);
+    if (!kv4_plan_fits(plan, B, view.heads)) return REQAT_E_SHAPE;
+    if (plan.splits > 1 && !workspace) return REQAT_E_NULL;
     if (!aligned16(workspace)) return REQAT_E_ALIGN;
     if (overlaps(q, span_bf16(T, cols, ldq), out, span_bf16(T, cols, ldo))) return REQAT_E_UNSUPPORTED;
     const Kv4AttnArgs a = {view, reinterpret_cast<const uint16_t *>(q), reinterpret_cast<uint16_t *>(out), lse, q_start,

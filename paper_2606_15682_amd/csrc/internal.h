@@ -91,8 +91,7 @@ struct Kv4AttnArgs {
     float scale;
     void *workspace;
 };
-size_t kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads,
-                                     int D);
+size_t kv4_attention_workspace_bytes(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads, int D);
 hipError_t launch_kv4_attention(const Kv4AttnArgs &a, hipStream_t stream);
 
 // SEM loss: per-row statistics ([T][4]: H, NLL, lse, 0), weights [T], loss[4]

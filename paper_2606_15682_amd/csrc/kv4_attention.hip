@@ -488,10 +488,10 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
     }
     __syncthreads();
     float *po = reinterpret_cast<float *>(a.workspace);
-    const int64_t all = a.T * a.q_heads;
+    const int64_t all = a.B * a.max_q * a.q_heads, first = (int64_t)b * a.max_q;   // partial rows go by sequence, max_q to each
     if ((int)threadIdx.x < rows) {
         const int row = threadIdx.x, i = row / group;
-        const int64_t at = (sq.q0 + i) * a.q_heads + h * group + (row - i * group);
+        const int hq = h * group + (row - i * group);
         double top = refs[0][threadIdx.x];
         float total = 0.0f;
 #pragma unroll
@@ -500,11 +500,11 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
         for (int w = 0; w < W; ++w)
             total = __builtin_fmaf(sums[w][threadIdx.x], exp2_of(refs[w][threadIdx.x] - top), total);
         if (splits > 1) {
-            reinterpret_cast<PieceRow *>(po + (int64_t)splits * all * D)[split * all + at] = {top, total, 0.0f};
+            reinterpret_cast<PieceRow *>(po + (int64_t)splits * all * D)[split * all + (first + i) * a.q_heads + hq] = {top, total, 0.0f};
         } else {
             const bool none = visible(a, sq, i) == 0 && !sq.lost;
             finish[threadIdx.x] = finish_factor(sq.lost, none, total);
-            if (a.lse) a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(top, total);
+            if (a.lse) a.lse[(sq.q0 + i) * a.q_heads + hq] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(top, total);
         }
     }
 #pragma unroll
@@ -539,7 +539,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
             }
             const int row = 16 * n + rr, i = row / group, hq = h * group + (row - i * group);
             if (splits > 1) {
-                *reinterpret_cast<float2 *>(po + (split * all + (sq.q0 + i) * a.q_heads + hq) * D + ch) = make_float2(y0, y1);
+                *reinterpret_cast<float2 *>(po + (split * all + (first + i) * a.q_heads + hq) * D + ch) = make_float2(y0, y1);
             } else {
                 const float f1 = finish[16 * n + rr], g1 = *a.c.gv;
                 *reinterpret_cast<uint32_t *>(a.out + (sq.q0 + i) * a.ldo + (int64_t)hq * D + ch) =
@@ -897,7 +897,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
     constexpr int kLd = D + 1, kPer = D / 8;                             // lanes of a row
     float *mine = reinterpret_cast<float *>(ring) + wave * 32 * kLd;
     float *po = reinterpret_cast<float *>(a.workspace);
-    const int64_t all = a.T * a.q_heads, at = (sq.q0 + qi) * a.q_heads + hq;
+    const int64_t all = a.B * a.max_q * a.q_heads, at = (b * a.max_q + qi) * a.q_heads + hq;   // as in the kernel above
     sum += __shfl_xor(sum, 32, 64);
     const bool none = see == 0 && !sq.lost;
     const float f = splits > 1 ? 1.0f : finish_factor(sq.lost, none, sum), g1 = splits > 1 ? 1.0f : *a.c.gv;
@@ -905,7 +905,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
         if (splits > 1) {
             reinterpret_cast<PieceRow *>(po + (int64_t)splits * all * D)[split * all + at] = {ref.at(c), sum, 0.0f};
         } else if (a.lse) {
-            a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(ref.at(c), sum);
+            a.lse[(sq.q0 + qi) * a.q_heads + hq] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(ref.at(c), sum);
         }
     }
 #pragma unroll
@@ -951,7 +951,7 @@ __global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, i
     const int i = (int)(bi % a.max_q), b = (int)(bi / a.max_q);
     const Seq sq = sequence(a, b);
     if (i >= sq.nq) return;
-    const int64_t at = (sq.q0 + i) * a.q_heads + hq, all = a.T * a.q_heads;
+    const int64_t all = a.B * a.max_q * a.q_heads;
     const float *po = reinterpret_cast<const float *>(a.workspace);
     const PieceRow *pm = reinterpret_cast<const PieceRow *>(po + (int64_t)splits * all * D);
     double ref[S];
@@ -959,7 +959,7 @@ __global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, i
 #pragma unroll
     for (int k = 0; k < S; ++k) {
         const int s = wave + k * W;
-        const int64_t slot = (s < splits ? s : 0) * all + at;
+        const int64_t slot = (s < splits ? s : 0) * all + bi * a.q_heads + hq;
         ref[k] = pm[slot].at;
         weight[k] = pm[slot].sum;
 #pragma unroll
@@ -1008,7 +1008,7 @@ __global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, i
     if constexpr (C == 2) *reinterpret_cast<uint32_t *>(dst) = bf16_rne_from_float(z[0] * f * g1) | (bf16_rne_from_float(z[1] * f * g1) << 16);
     else dst[0] = (uint16_t)bf16_rne_from_float(z[0] * f * g1);
     if (a.lse && lane == 0)
-        a.lse[at] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(m, total);
+        a.lse[(sq.q0 + i) * a.q_heads + hq] = sq.lost ? __builtin_nanf("") : none ? -__builtin_inff() : log_sum(m, total);
 }
 
 template <int D, int NT, int W> void decode(const Kv4AttnArgs &a, const Kv4Plan &p, hipStream_t stream) {
@@ -1046,9 +1046,8 @@ template <int D> hipError_t attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipSt
 
 }  // namespace
 
-size_t kv4_attention_workspace_bytes(int64_t B, int64_t T, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads, int D) {
-    const Kv4Plan p = kv4_plan(B, max_q, max_kv, q_heads, kv_heads);
-    return p.splits > 1 ? (size_t)p.splits * (size_t)T * (size_t)q_heads * ((size_t)D * 4 + sizeof(PieceRow)) : 0;
+size_t kv4_attention_workspace_bytes(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads, int D) {
+    return (size_t)kv4_piece_rows(B, max_q, max_kv, q_heads, kv_heads) * ((size_t)D * 4 + sizeof(PieceRow));
 }
 
 hipError_t launch_kv4_attention(const Kv4AttnArgs &a, hipStream_t stream) {

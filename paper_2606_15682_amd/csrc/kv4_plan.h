@@ -21,7 +21,7 @@ struct Kv4Plan {
     int tiles, qtiles, waves, splits, chunk;
 };
 constexpr int kKv4MaxSplits = 256;
-constexpr int64_t kKv4MaxPieces = 8192; // in all, where the longest of several sequences asks for them: a workspace of 138 MB at most
+constexpr int64_t kKv4MaxPieces = 8192; // in all, where the longest of several sequences asks for them
 constexpr int kKv4Prompt = 16;          // tiles of the kernel for prompts: 256 rows
 
 inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads) {
@@ -53,6 +53,29 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, i
     p.splits = (int)((max_kv + p.chunk - 1) / p.chunk);
     if (p.splits < 1) p.splits = 1;
     return p;
+}
+
+// Rows of partial results (query x head x piece) that a workspace has room for: enough for the plan of a call and of every
+// call with fewer sequences, queries or tokens, since fewer of them can mean more pieces.  Each bound below holds for
+// the plans it names and grows with B, max_q and max_kv.  At most 8192 x 32 rows, 138 MB with heads of 128.
+inline int64_t kv4_piece_rows(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, int kv_heads) {
+    const auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
+    if (max_kv <= 256 || B <= 0 || max_q <= 0) return 0;                 // one piece
+    const int64_t group = q_heads / kv_heads, units = B * kv_heads;      // units of up to 32 rows
+    const int64_t most = least((max_kv + 255) / 256, kKv4MaxSplits);     // pieces of a unit
+    // up to 32 rows: ceil(512 / units) pieces of fewer than 512 units, or pieces of 1536 tokens of several sequences
+    int64_t pieces = least(511 + units, 1022);
+    if (B > 1 && max_kv > 2048) {
+        const int64_t finer = least(units * ((max_kv + 1535) / 1536), kKv4MaxPieces);
+        pieces = pieces > finer ? pieces : finer;
+    }
+    const int64_t rows = group > 32 ? 0 : least(max_q, 32 / group) * group;
+    const int64_t few = least(pieces, units * most) * rows;
+    if (max_q * group <= 32) return few;
+    // prompts: ceil(256 / tiles) pieces of fewer than 256 tiles of 256 rows
+    const int64_t all = max_q * group, tiles = units * ((all + 255) / 256);
+    const int64_t prompts = least(least(255 + tiles, 510) * least(all, 256), units * all * most);
+    return few > prompts ? few : prompts;
 }
 
 // Whether the launch of a plan holds fewer than 2^32 threads (workgroups of up to 512).

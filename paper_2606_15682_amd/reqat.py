@@ -698,8 +698,9 @@ def kv4_attention(q, cache, block_table, kv_len, q_start=None, max_q=None, max_k
     kv_len: int32 [B], cached tokens, the new ones included; q_start: int32 [B + 1], the first query row of each
     sequence, or None: one query each.  max_q and max_kv bound the queries and tokens of every sequence on the host
     (by default T, 1 without q_start, and what the table can hold); closer bounds launch less.  causal: the queries
-    are the last tokens of their sequence.  sm_scale: default head_dim ** -0.5.  ws: uint8 tensor of
-    reqat_kv4_attention_workspace_bytes(B, T, max_q, max_kv, q_heads, kv_heads, head_dim) bytes.
+    are the last tokens of their sequence.  sm_scale: default head_dim ** -0.5.  ws: uint8 tensor of at least
+    reqat_kv4_attention_workspace_bytes(B, T, max_q, max_kv, q_heads, kv_heads, head_dim) bytes; one of the largest
+    sizes serves every smaller call.
     Returns out, bfloat16 like q, or (out, lse) with lse float32 [T, q_heads]."""
     _cache_arg(cache)
     dev, D = cache.device, cache.head_dim
