@@ -550,7 +550,11 @@ class Kv4Cache:
 
     A scale is a number, or a float32 tensor of one element on the device.  The codes and scales (``k_codes``,
     ``k_scales``, ``v_codes``, ``v_scales``) have the layout that include/reqat.h states.  Which pages belong to which
-    sequence is the caller's: a slot is page * page_size + the token's place in the page."""
+    sequence is the caller's: a slot is page * page_size + the token's place in the page.  Scales, shift and arrays
+    may be written in place or assigned; the sizes and the device stay."""
+
+    _ARRAYS = {"k_codes": 2, "k_scales": 16, "v_codes": 2, "v_scales": 16}       # channels to a byte
+    _SIZES = frozenset(("device", "num_pages", "page_size", "kv_heads", "head_dim", "width"))
 
     def __init__(self, num_pages, page_size, kv_heads, head_dim=128, k_scale=1.0, v_scale=1.0, k_shift=None,
                  device="cuda"):
@@ -566,25 +570,38 @@ class Kv4Cache:
         self.num_pages, self.page_size, self.kv_heads, self.head_dim = num_pages, page_size, kv_heads, head_dim
         self.width = kv_heads * head_dim         # channels of a token's keys, and of its values
 
-        def scale(g, name):
-            if isinstance(g, torch.Tensor):
-                return _scale_arg(g, NVFP4, self.device, name)
-            if not 0.0 < float(g) < float("inf"):
-                raise ValueError("%s must be positive and finite" % name)
-            return torch.tensor([float(g)], dtype=torch.float32, device=self.device)
+        self.k_scale, self.v_scale, self.k_shift = k_scale, v_scale, k_shift
+        for name in self._ARRAYS:
+            setattr(self, name, torch.zeros(self._bytes(name), dtype=torch.uint8, device=self.device))
 
-        self.k_scale, self.v_scale = scale(k_scale, "k_scale"), scale(v_scale, "v_scale")
-        self.k_shift, _ = _shift_ptr(k_shift, kv_heads * head_dim, self.device)
-        run = num_pages * kv_heads * page_size
-        u8 = dict(dtype=torch.uint8, device=self.device)
-        self.k_codes = torch.zeros(run * head_dim // 2, **u8)
-        self.k_scales = torch.zeros(run * head_dim // 16, **u8)
-        self.v_codes = torch.zeros(run * head_dim // 2, **u8)
-        self.v_scales = torch.zeros(run * head_dim // 16, **u8)
+    def _bytes(self, name):
+        return self.num_pages * self.page_size * self.width // self._ARRAYS[name]
+
+    def _checked(self, name, value):
+        if name == "k_shift":
+            return _shift_ptr(value, self.width, self.device)[0]
+        if name in self._ARRAYS:
+            return _index_arg(value, (self._bytes(name),), torch.uint8, self.device, name)
+        if isinstance(value, torch.Tensor):
+            return _scale_arg(value, NVFP4, self.device, name)
+        if not 0.0 < float(value) < float("inf"):
+            raise ValueError("%s must be positive and finite" % name)
+        return torch.tensor([float(value)], dtype=torch.float32, device=self.device)
+
+    def __setattr__(self, name, value):
+        if name in self._ARRAYS or name in ("k_scale", "v_scale", "k_shift"):
+            value = self._checked(name, value)
+            self.__dict__.pop("struct", None)            # it has the old tensor's address
+        elif name in self._SIZES and name in self.__dict__:
+            raise AttributeError("%s of a Kv4Cache does not change" % name)
+        object.__setattr__(self, name, value)
+
+    def __getstate__(self):
+        return {name: value for name, value in self.__dict__.items() if name != "struct"}
 
     @functools.cached_property
     def struct(self) -> Kv4CacheStruct:
-        """reqat_kv4_cache of this cache, whose tensors stay the same ones."""
+        """reqat_kv4_cache of this cache, until one of its tensors is replaced."""
         return Kv4CacheStruct(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
                               self.v_scales.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
                               _ptr(self.k_shift), self.num_pages, self.page_size, self.kv_heads, self.head_dim)
