@@ -584,9 +584,10 @@ class Kv4Cache:
             return _index_arg(value, (self._bytes(name),), torch.uint8, self.device, name)
         if isinstance(value, torch.Tensor):
             return _scale_arg(value, NVFP4, self.device, name)
-        if not 0.0 < float(value) < float("inf"):
-            raise ValueError("%s must be positive and finite" % name)
-        return torch.tensor([float(value)], dtype=torch.float32, device=self.device)
+        g = torch.tensor([float(value)], dtype=torch.float32)
+        if not 0.0 < float(g) < float("inf"):
+            raise ValueError("%s must be a positive, finite FP32 number" % name)
+        return g.to(self.device)
 
     def __setattr__(self, name, value):
         if name in self._ARRAYS or name in ("k_scale", "v_scale", "k_shift"):

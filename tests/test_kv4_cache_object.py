@@ -74,3 +74,12 @@ def test_copies_have_their_own_tensors():
     agrees(d)
     agrees(c)
     assert c.k_shift.data_ptr() != d.k_shift.data_ptr()
+
+
+@pytest.mark.parametrize("g", [1e-50, 1e39, 0.0, -1.0, float("inf"), float("nan")])
+def test_scales_are_positive_finite_fp32_numbers(g):
+    """A number that FP32 holds as zero or infinity is no scale either."""
+    for name in ("k_scale", "v_scale"):
+        with pytest.raises(ValueError):
+            reqat.Kv4Cache(1, 16, 1, 64, device="cpu", **{name: g})
+    assert float(reqat.Kv4Cache(1, 16, 1, 64, device="cpu", k_scale=1e-45).k_scale) > 0.0
