@@ -332,7 +332,8 @@ typedef struct reqat_kv4_cache_s {
  *     likewise without rotation and shift.
  *   q [T][ldq] bfloat16, q_heads * D columns: the queries, rotated into q_out
  *     [T][ldq_out] bfloat16, RN_bf16 (padding tokens too).  q_out == q with the
- *     same stride is allowed, any other overlap is not (REQAT_E_UNSUPPORTED).
+ *     same stride is allowed, any other overlap with q, k or v is not
+ *     (REQAT_E_UNSUPPORTED; other columns of the same rows do not overlap).
  *     q_heads == 0: none (q, q_out NULL).  Queries need the tables.
  * Strides are multiples of 8 elements and at least the columns; k, v, q, q_out
  * and the tables 16-byte aligned.  T == 0 is a no-op.

@@ -5,6 +5,7 @@
 
 #include "../../include/reqat.h"
 #include "internal.h"
+#include "row_overlap.h"
 
 namespace {
 
@@ -212,8 +213,10 @@ reqat_status reqat_kv4_append(const reqat_kv4_cache *cache, int64_t T, const int
         return st;
     if (rope && (!aligned16(rope_cos) || !aligned16(rope_sin))) return REQAT_E_ALIGN;
     if ((reinterpret_cast<uintptr_t>(slots) & 7u) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return REQAT_E_ALIGN;
-    if (q_heads > 0 && overlaps(q, span_bf16(T, qcols, ldq), q_out, span_bf16(T, qcols, ldq_out)) &&
-        (q != q_out || ldq != ldq_out))
+    if (q_heads > 0 && (q != q_out || ldq != ldq_out) && rows_overlap(q, T, qcols, ldq, q_out, T, qcols, ldq_out))
+        return REQAT_E_UNSUPPORTED;
+    if (q_heads > 0 && (rows_overlap(k, T, cols, ldk, q_out, T, qcols, ldq_out) ||
+                        rows_overlap(v, T, cols, ldv, q_out, T, qcols, ldq_out)))
         return REQAT_E_UNSUPPORTED;
     hipError_t e = launch_kv4_append(view, T, slots, reinterpret_cast<const uint16_t *>(k), ldk,
                                      reinterpret_cast<const uint16_t *>(v), ldv, reinterpret_cast<const uint16_t *>(q),
