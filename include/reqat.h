@@ -369,7 +369,7 @@ reqat_status reqat_kv4_gather(const reqat_kv4_cache *cache, int64_t T, const int
  *     table_cols entries of a row are used (ld_table >= table_cols).
  *   max_q, max_kv: bounds on every nq and kv_len, at most 2^31 - 1 and 2^30 (they
  *     size the launch).
- *   out [T][ldo] bfloat16; lse NULL or [T][q_heads] FP32, the natural logarithm
+ *   out [T][ldo] bfloat16, no overlap with q (REQAT_E_UNSUPPORTED); lse NULL or [T][q_heads] FP32, the natural logarithm
  *     of sum_j exp(sm_scale q . k^_j) (of the shifted keys).
  *   workspace: at least reqat_kv4_attention_workspace_bytes(...) bytes, 16-byte
  *     aligned (may be NULL when that is 0): partial results of long sequences.

@@ -279,7 +279,7 @@ reqat_status reqat_kv4_attention(const reqat_kv4_cache *cache, int64_t B, int64_
     if (!kv4_plan_fits(plan, B, view.heads)) return REQAT_E_SHAPE;
     if (plan.splits > 1 && !workspace) return REQAT_E_NULL;
     if (!aligned16(workspace)) return REQAT_E_ALIGN;
-    if (overlaps(q, span_bf16(T, cols, ldq), out, span_bf16(T, cols, ldo))) return REQAT_E_UNSUPPORTED;
+    if (rows_overlap(q, T, cols, ldq, out, T, cols, ldo)) return REQAT_E_UNSUPPORTED;
     const Kv4AttnArgs a = {view, reinterpret_cast<const uint16_t *>(q), reinterpret_cast<uint16_t *>(out), lse, q_start,
                            kv_len, block_table, B, T, ldq, ldo, ld_table, table_cols, max_q, max_kv, (int)q_heads,
                            causal != 0, sm_scale, workspace};
