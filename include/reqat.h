@@ -344,7 +344,8 @@ reqat_status reqat_kv4_append(const reqat_kv4_cache *cache, int64_t T, const int
                               int64_t rope_len, void *stream);
 
 /*
- * Read T slots back: k_out, v_out [T][ld] bfloat16 (either may be NULL),
+ * Read T slots back: k_out, v_out [T][ld] bfloat16 (either may be NULL; no
+ * overlap with each other, REQAT_E_UNSUPPORTED),
  * RN_bf16(E1M2(code) * s * g), in the shifted domain, or with add_shift != 0
  * RN_bf16(RN_fp32(RN_fp32(E1M2(code) * s * g) + m)) for the keys.  NaN (0x7FC0)
  * where the scale byte is NaN; zeros for a slot outside the cache.

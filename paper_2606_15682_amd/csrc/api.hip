@@ -237,6 +237,7 @@ reqat_status reqat_kv4_gather(const reqat_kv4_cache *cache, int64_t T, const int
     if (k_out && (st = check_rows(k_out, ldk, cols)) != REQAT_OK) return st;
     if (v_out && (st = check_rows(v_out, ldv, cols)) != REQAT_OK) return st;
     if (reinterpret_cast<uintptr_t>(slots) & 7u) return REQAT_E_ALIGN;
+    if (k_out && v_out && rows_overlap(k_out, T, cols, ldk, v_out, T, cols, ldv)) return REQAT_E_UNSUPPORTED;
     hipError_t e = launch_kv4_gather(view, T, slots, reinterpret_cast<uint16_t *>(k_out), ldk,
                                      reinterpret_cast<uint16_t *>(v_out), ldv, add_shift != 0,
                                      reinterpret_cast<hipStream_t>(stream));

@@ -43,3 +43,13 @@ def test_rotated_queries_beside_their_inputs():
     assert torch.equal(wide[:, Q + 2 * W:], want) and torch.equal(wide[:, :Q + 2 * W], before[:, :Q + 2 * W])
     for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
         assert torch.equal(getattr(caches[0], name), getattr(caches[1], name))
+
+
+def test_keys_and_values_read_back_side_by_side():
+    s = Setup([100], 2, 128, 32, seed=7)
+    slots = torch.from_numpy(s.table[0, :4].astype("int64") * 32).to(DEV).repeat_interleave(25) + torch.arange(100, device=DEV) % 25
+    k, v = reqat.kv4_gather(s.cache, slots)
+    both = torch.empty((100, 512), dtype=torch.bfloat16, device=DEV)
+    reqat.kv4_gather(s.cache, slots, out=(both[:, 256:], both[:, :256]))
+    bits = both.view(torch.int16)                       # slots without a token hold NaN
+    assert torch.equal(bits[:, 256:], k.view(torch.int16)) and torch.equal(bits[:, :256], v.view(torch.int16))

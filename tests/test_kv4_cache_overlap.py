@@ -5,7 +5,7 @@ import os
 import pytest
 
 from paper_2606_15682_amd import reqat
-from tests.test_kv4_cache_abi import E_UNSUP, P, append
+from tests.test_kv4_cache_abi import E_UNSUP, P, append, gather
 
 pytestmark = pytest.mark.skipif(not os.path.exists(reqat.LIB_PATH), reason="libreqat.so not built")
 
@@ -18,3 +18,10 @@ def test_rotated_queries_over_the_keys_or_values(name, ld):
         assert append(**{name: where, other: 32 * P, "q_out": far}) == E_UNSUP, where - far
     # one buffer: the queries' columns 0 .. 1023, keys or values from the last of them
     assert append(**{"q": far, "ldq": 1536, "q_out": far, "ldqo": 1536, name: far + 2 * 1016, ld: 1536}) == E_UNSUP
+
+
+def test_values_read_back_over_the_keys():
+    for where in (P, P + 16, P + 2 * 4 * 256 - 16):
+        assert gather(v=where) == E_UNSUP and gather(k=where, v=P) == E_UNSUP
+    assert gather(ldk=512, ldv=512, v=P + 2 * 248) == E_UNSUP
+    assert gather(ldk=264, ldv=512, v=P + 2 * 600) == E_UNSUP
