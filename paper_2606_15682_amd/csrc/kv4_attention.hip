@@ -1038,7 +1038,7 @@ template <int D> hipError_t attend(const Kv4AttnArgs &a, const Kv4Plan &p, hipSt
         hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kv4_prompt_kernel<D>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, Prompt<D>::kLds);
         if (e != hipSuccess) return e;
-        kv4_prompt_kernel<D><<<(unsigned)n, 512, Prompt<D>::kLds, stream>>>(a, p.qtiles, p.splits, p.chunk);
+        kv4_prompt_kernel<D><<<(unsigned)n, 512, Prompt<D>::kLds, stream>>>(a, (int)p.qtiles, p.splits, p.chunk);
     }
     if (p.splits > 1) join<D>(a, p, stream);
     return hipGetLastError();

@@ -18,7 +18,9 @@ namespace reqat {
 // more: shorter contexts are one piece and need no join; from 257 to 512 tokens eight waves take it (500
 // tokens: 8.1 us, 8.7 in two pieces of four waves and a join; 250 tokens: 6.9 against 6.3).
 struct Kv4Plan {
-    int tiles, qtiles, waves, splits, chunk;
+    int tiles;
+    int64_t qtiles;                     // in an int where the launch fits
+    int waves, splits, chunk;
 };
 constexpr int kKv4MaxSplits = 256;
 constexpr int64_t kKv4MaxPieces = 8192; // in all, where the longest of several sequences asks for them
@@ -28,7 +30,7 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t max_q, int64_t max_kv, int q_heads, i
     Kv4Plan p;
     const int64_t rows = max_q * (q_heads / kv_heads);
     p.tiles = rows > 32 ? kKv4Prompt : rows > 16 ? 2 : 1;
-    p.qtiles = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
+    p.qtiles = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
     const int64_t groups = B * kv_heads * p.qtiles;
     p.waves = 4;
     int64_t splits = 1;
@@ -74,14 +76,14 @@ inline int64_t kv4_piece_rows(int64_t B, int64_t max_q, int64_t max_kv, int q_he
     if (max_q * group <= 32) return few;
     // prompts: ceil(256 / tiles) pieces of fewer than 256 tiles of 256 rows
     const int64_t all = max_q * group, tiles = units * ((all + 255) / 256);
-    const int64_t prompts = least(least(255 + tiles, 510) * least(all, 256), units * all * most);
+    const int64_t prompts = least(least(255 + tiles, 510) * least(all, 256), least(units * all, int64_t(1) << 40) * most);
     return few > prompts ? few : prompts;
 }
 
 // Whether the launch of a plan holds fewer than 2^32 threads (workgroups of up to 512).
 inline bool kv4_plan_fits(const Kv4Plan &p, int64_t B, int kv_heads) {
     const int64_t n = B * kv_heads * p.splits;                           // below 2^40
-    return p.tiles == kKv4Prompt ? n < (int64_t(1) << 23) && n * p.qtiles < (int64_t(1) << 23) : n < (int64_t(1) << 23);
+    return n < (int64_t(1) << 23) && n * p.qtiles < (int64_t(1) << 23);  // qtiles below 2^40; 1 but for prompts
 }
 
 }  // namespace reqat
