@@ -16,8 +16,8 @@ CALLS = [([300, 33, 1, 0], [1] * 4, 2, 5), ([2049], [1], 1, 7), ([300, 40], [5, 
          ([1200], [65], 1, 4)]
 
 
-def run(gk, gv, lens, nqs, H, group, D, scale=None, seed=31):
-    """Random codes, scale bytes 0x20 .. 0x47 (2^-3 to 3.75), queries for scores of a standard deviation of 2."""
+def run(gk, gv, lens, nqs, H, group, D, scale=None, seed=31, least=0x20, most=0x47):
+    """Random codes, scale bytes least .. most (0x20 .. 0x47: 2^-3 to 3.75), queries for scores of a standard deviation of 2."""
     scale = D ** -0.5 if scale is None else scale
     gk, gv, scale = (float(np.float32(x)) for x in (gk, gv, scale))
     print("gk=%g gv=%g scale=%g lens=%s q=%s D=%d" % (gk, gv, scale, lens, nqs, D), flush=True)
@@ -25,7 +25,7 @@ def run(gk, gv, lens, nqs, H, group, D, scale=None, seed=31):
     for i, (g, values) in enumerate(((gk, s.k), (gv, s.v))):
         for b, n in enumerate(lens):
             c = s.rng.integers(0, 16, (n, H, D)).astype(np.uint8)
-            t = s.rng.integers(0x20, 0x48, (n, H, D // 16)).astype(np.uint8)
+            t = s.rng.integers(least, most + 1, (n, H, D // 16)).astype(np.uint8)
             if n:
                 j = np.arange(n)
                 at = (s.table[b, j // s.P], j % s.P)
@@ -78,3 +78,11 @@ def test_narrow_heads():
     for gk, gv in ((2.0 ** 118, 2.0 ** -126), (2.0 ** -120, 2.0 ** 120)):
         run(gk, gv, [2049, 7], [1, 1], 2, 4, 64)
         run(gk, gv, [700], [65], 1, 4, 64)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens,nqs,H,group", CALLS)
+@pytest.mark.parametrize("least,most", [(1, 7), (1, 20), (0x70, 0x7E)])
+def test_block_scales_at_the_ends(least, most, lens, nqs, H, group, D):
+    """E4M3 subnormals (2^-9 to 7 2^-9) and the numbers next to them, and the largest."""
+    run(2.0 ** -3, 2.0 ** -4, lens, nqs, H, group, D, seed=32, least=least, most=most)
