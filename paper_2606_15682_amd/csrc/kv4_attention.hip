@@ -193,11 +193,12 @@ __device__ __forceinline__ int visible(const Kv4AttnArgs &a, const Seq &s, int i
 // to a tile and 5 to 8 heads a group the matrix cores do two to three times the work there is, and have time for it.
 //
 // Bound by memory where the call is large, with the VALU's unpacking not far behind it: 728 MB (64 sequences
-// of up to 16384 tokens, 8 KV heads of 128) in 136 us, 5.4 TB/s with the join's 6 us, reads alone running at 6.0 to 6.4;
-// counters: VALU issue on 0.74 of the SIMD cycles, matrix pipe busy on 0.15.  131072 tokens of one sequence: 151 MB in
-// 34.4 us, 28 without the join.  Below some 50 MB by the steps in a row: first codes, queries, the join of the waves, then
-// the other launch (1021 tokens of 2 heads: 8.5 us, 7.0 and 2.2 to 2.9 by kernel).  Up to 32 rows (25: 52 MB in 27.6 us) twice the
-// products and exponentials stand beside the same codes.
+// of up to 16384 tokens, 8 KV heads of 128) in 137 to 140 us, 5.3 TB/s with the join's 6 us, reads alone running at 6.0 to
+// 6.4; counters: VALU issue on 0.75 of the SIMD cycles, matrix pipe busy on 0.15.  131072 tokens of one sequence: 151 MB in
+// 34.9 us, 29 without the join.  Below some 50 MB by the steps in a row: first codes, queries, the join of the waves, then
+// the other launch (1021 tokens of 2 heads: 8.7 us, 7.1 and 2.9 by kernel).  Up to 32 rows (25: 52 MB in 27.8 us) twice the
+// products and exponentials stand beside the same codes.  Heads of 64: half the bytes, and the same steps, whose loads fetch
+// every operand twice (lanes g and g + 2 the same keys, r and r + 8 the same values): the full batch 88.8 us, 4.1 TB/s.
 template <int D> struct Step {
     uint32_t k[2][D / 32], ks[2];
     uint32_t v[2][4], vs[2];
@@ -561,11 +562,12 @@ __global__ __launch_bounds__(64 * W, 2) void kv4_decode_kernel(const Kv4AttnArgs
 //
 // 256 rows to a workgroup, since unpacking a token costs the same for any number of rows; 32 x 32 products, since each
 // operand read feeds twice the work of a 16 x 16 one.  Bound by issue and by power: 8192 queries of 8192 tokens, 40 + 8 heads
-// of 128 (687 GFLOP of visible pairs) in 649 us, 1.06 PFLOP/s (a large library FP16 product: 1.15; MFMA with the operand read
+// of 128 (687 GFLOP of visible pairs) in 642 to 659 us, 1.04 to 1.07 PFLOP/s (a large library FP16 product, both operands
+// along K: 1.39 to 1.49 by the box, its operands being FP16 in memory; MFMA with the operand read
 // and the exponential beside it and nothing else: 1.33, at a clock that power holds near 1.56 GHz); counters: matrix
-// pipe busy on 0.55 of the cycles, 7.7 VALU instructions to an MFMA (with it), of which unpacking and weights.
-// 5 sequences of up to 777 queries and 9001 tokens, 28 + 4 heads: 240 GFLOP in 265 us, 0.91 PFLOP/s, 440 workgroups of unequal
-// length on 256 CUs.
+// pipe busy on 0.54 of the cycles, 7.8 VALU instructions to an MFMA (with it), of which unpacking and weights.
+// 5 sequences of up to 777 queries and 9001 tokens, 28 + 4 heads: 240 GFLOP in 262 us, 0.92 PFLOP/s, 440 workgroups of unequal
+// length on 256 CUs.  Heads of 64 (half the operands, as many exponentials): the prompt in 448 us, 0.77 PFLOP/s.
 template <int D> struct Prompt {
     static constexpr int F = D / 16;                     // operands of 1 KB: of 32 tokens' keys; of their values
     static constexpr int kSub = 2 * F * 1024;            // 32 tokens: keys, then values
@@ -941,7 +943,7 @@ __global__ __launch_bounds__(512, 2) void kv4_prompt_kernel(const Kv4AttnArgs a,
 
 // Joins the splits of a row: one workgroup of W waves per query and head, a wave up to S of the splits.  Every load
 // is on its way before the first is waited for; what was not written is not used.  A few rows: bound by the launch and
-// one trip to memory (4.5 us for 40 rows of 64 splits); many: 18 MB in 6 us (2560 rows of up to 11).
+// one trip to memory (4.1 us for 40 rows of 64 splits); many: 18 MB in 6.4 us (2560 rows of up to 11).
 template <int D, int W, int S>
 __global__ __launch_bounds__(64 * W) void kv4_join_kernel(const Kv4AttnArgs a, int splits, int chunk) {
     constexpr int C = D / 64;

@@ -86,8 +86,9 @@ __device__ __forceinline__ void put_block(const AppendArgs &a, const float (&x)[
 // workgroups take the keys, the next the values, the last the queries: a wave does one of the three (with heads of
 // all kinds in a wave, 5003 tokens of 28 + 4 + 4 heads took 32 us; rounding by bit arithmetic in FP32 was part of that).
 // Two 16-byte loads at each half of a head give a lane whole blocks of 16 channels and both members of its pairs.
-// Bound by memory: those 5003 tokens move 87 MB in 21.8 us, 4.0 TB/s (a copy: 5.2; waves wait on 0.71 of their cycles, VALU
-// issue on 0.40).  64 tokens of 40 + 8 + 8 heads: 5.3 us, a launch and one trip to memory and back.
+// Bound by memory: those 5003 tokens move 87 MB in 21.8 us, 4.0 TB/s (a copy: 5.2; waves wait on 0.72 of their cycles, VALU
+// issue on 0.38).  64 tokens of 40 + 8 + 8 heads: 5.3 us, a launch and, for a key, five trips to memory in turn, each behind a
+// branch: the row, its position, cos and sin, the slot, the scale and the shift.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv4_append_kernel(const AppendArgs a) {
     constexpr int kPairs = D / 32;
@@ -208,8 +209,8 @@ __device__ __forceinline__ void stream16(uint16_t *__restrict__ p, const uint4 &
 // Workgroups are dealt to the eight XCDs in turn; each XCD takes a contiguous run of items, since four adjacent tokens share
 // the 16-byte pieces of their value codes and sixteen a line of their scales, which two and eight XCDs then fetched
 // (32768 tokens of 8 heads: 86 MB read for 38, 34.5 us against 31.8; 5003 of 4 heads: 4.5 against 4.1).  172 MB in
-// 31.8 us call after call (5.4 TB/s) and 26.6 among other work: bound by memory, where a copy runs at 5.2 TB/s; VALU issue
-// takes 0.91 of the SIMD cycles by then.
+// 30.8 us call after call (5.6 TB/s) and 27.1 among other work: bound by memory, where a copy runs at 5.0 to 5.2 TB/s; VALU issue
+// takes 0.89 of the SIMD cycles by then.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv4_gather_kernel(const Kv4View c, const int64_t *__restrict__ slots, int T,
                                                               uint16_t *__restrict__ ky, int64_t ldk,

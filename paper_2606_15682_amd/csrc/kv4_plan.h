@@ -9,14 +9,15 @@ namespace reqat {
 // a sequence to `splits` pieces of `chunk`, a workgroup each, whose results a second kernel joins (splits > 1).
 //
 // Up to 32 rows (tiles 1, 2) a wave does all by itself, 32 tokens a step; beyond, the kernel for prompts, in which waves
-// without rows only unpack (16 sequences of up to 4000 tokens, 8 KV heads: 28.6 us with 25 rows, 47 with 35 to 60).
+// without rows only unpack (16 sequences of up to 4000 tokens, 8 KV heads: 28.5 us with 25 rows, 48 to 53 with 35 to 80, 69 with 160, where the
+// bytes take 11: no kernel here is made for 33 to 255 rows).
 //
-// Pieces: 512 workgroups of four waves, two per CU, where there are fewer units (sequence x KV head): 131072 tokens of one
-// sequence with 8 KV heads take 34.4 us in 512 pieces, 37.5 in 1024, whose results the join reads too.  Several
+// Pieces: 512 workgroups of four waves, two per CU, where there are fewer units (sequence x KV head): 30000 tokens of one
+// sequence with 8 KV heads take 16.4 us in 472 pieces, 20.5 in 944, whose results the join reads too.  Several
 // sequences differ in length and max_kv is the longest's: pieces of at most 1536 tokens (64 sequences of up to
-// 16384 tokens, 8 KV heads: 142 us, 169 in one piece each, 151 in pieces of 1024 or 2048).  At most 256 pieces, of 256 tokens or
+// 16384 tokens, 8 KV heads: 139 us, 170 in one piece each, 148 in pieces of 1024, 145 of 2048).  At most 256 pieces, of 256 tokens or
 // more: shorter contexts are one piece and need no join; from 257 to 512 tokens eight waves take it (500
-// tokens: 8.1 us, 8.7 in two pieces of four waves and a join; 250 tokens: 6.9 against 6.3).
+// tokens: 8.1 us, 8.6 in two pieces of four waves and a join; 250 tokens: 6.9 against 6.3).
 struct Kv4Plan {
     int tiles;
     int64_t qtiles;                     // in an int where the launch fits

@@ -1,6 +1,6 @@
 // The queue in LDS through which a wave of the decode attention (kv4_attention.hip) takes its codes and scales: direct
-// loads, each lane's where the lane finds them again, so that what is on its way takes no registers (102 instead of 166:
-// sixteen waves a CU rather than twelve).
+// loads, each lane's where the lane finds them again, so that what is on its way takes no registers (106 of the up to 128 that
+// sixteen waves a CU may have; 64 more with loads into registers).
 #pragma once
 
 #include "g2l.h"
@@ -8,7 +8,7 @@
 namespace reqat {
 
 // g2l16 past the caches: codes are read once.  64 sequences of up to 16384 tokens (8 KV heads) 153 -> 137 us, 131072
-// tokens of one 37.5 -> 34.9; with the scales' loads, several to a line, so too: no further gain.
+// tokens of one 37.5 -> 34.9, when it was changed; with the scales' loads, several to a line, so too: no further gain.
 __device__ __forceinline__ void g2l16_once(const uint8_t *base, uint32_t voff, uint8_t *l) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(base), "{m0}"((uint32_t)(uintptr_t)l));
 }
