@@ -437,6 +437,152 @@ reqat_status reqat_sem_loss_backward(const void *logits, int64_t T, int64_t V, i
                                      void *grad, reqat_dtype grad_dtype, int64_t ldg, void *stream);
 
 /*
+ * Training side: the operators around the quantized linear layers of a training
+ * step (embedding, norm, loss over the logits, optimizer).  Values are bfloat16 or
+ * FP32 as their reqat_dtype says, rows of any length and leading dimension,
+ * pointers aligned to their elements; sums, statistics and states are FP32 or
+ * wider, and every sum has a fixed order, so results are deterministic.
+ *
+ * Clipped policy loss with a KL term, of T tokens (rows of logits z over the
+ * vocabulary, p the softmax of z / temperature):
+ *     lp = log p_y,  r = exp(lp - old_logp),  x = ref_logp - lp,
+ *     l  = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(x) - x - 1),
+ *     L  = sum_t w_t l_t,   dL/dlp = w (-A r [inside] - kl_coef (exp(x) - 1)),
+ * inside: neither A > 0 with r > 1 + clip_high nor A < 0 with r < 1 - clip_low.
+ *   logits [T][ld] of dtype; targets [T] int32 in [0, V) (outside: NaN, no read);
+ *   old_logp, advantages [T] FP32;  ref_logp [T] FP32, or NULL without a KL term
+ *     (kl_coef 0);  weights [T] FP32, mask and normaliser in one, or NULL: 1 / T.
+ *     A row of weight 0 is not read: its statistics and gradient are zeros,
+ *     whatever its logits, advantage or target are.
+ *   stats [T][4] FP32 out (16-byte aligned): lp, log-sum-exp of z / temperature,
+ *     dL/dlp, r (kept for the backward pass);
+ *   loss [4] FP32 out: L, sum w (-min(..)), sum w (exp(x) - x - 1), sum w [not inside];
+ *   grad: NULL, or [T][ldg] of dtype out, dL/dz_j = (dL/dlp) ([j = y] - p_j) / temperature
+ *     in the same call, the row read once more from the caches.  grad == logits with
+ *     the same stride is allowed, any other overlap is not (REQAT_E_UNSUPPORTED).
+ * A logit of -Inf has probability 0; NaN or +Inf gives NaN for its row.
+ * 0 <= clip_low <= 1, clip_high >= 0, temperature > 0 and finite
+ * (REQAT_E_UNSUPPORTED); T at most 2^22.  T == 0 writes a loss of zeros.
+ */
+reqat_status reqat_policy_loss(const void *logits, reqat_dtype dtype, int64_t T, int64_t V, int64_t ld, const int32_t *targets,
+                               const float *old_logp, const float *advantages, const float *ref_logp, const float *weights,
+                               float clip_low, float clip_high, float kl_coef, float temperature, float *stats, float *loss,
+                               void *grad, int64_t ldg, void *stream);
+
+/*
+ * The gradient of the policy loss from logits and stats, times *grad_loss (a device
+ * float; NULL: 1).  Rows whose dL/dlp is 0 are not read.  grad as above.
+ */
+reqat_status reqat_policy_loss_backward(const void *logits, reqat_dtype dtype, int64_t T, int64_t V, int64_t ld,
+                                        const int32_t *targets, const float *stats, float temperature, const float *grad_loss,
+                                        void *grad, int64_t ldg, void *stream);
+
+/*
+ * Layer norm (center != 0) or root-mean-square norm (center == 0) of the rows of
+ * x [rows][ldx], cols <= 32768 (REQAT_E_UNSUPPORTED beyond):
+ *     mu = mean x (0 without center), rstd = 1 / sqrt(mean (x - mu)^2 + eps),
+ *     y = (x - mu) rstd weight + bias.
+ *   weight, bias [cols] of w_dtype, bias may be NULL;  y [rows][ldy] of dtype (y == x
+ *   with the same stride is allowed, any other overlap is not: REQAT_E_UNSUPPORTED);
+ *   stats [rows][2] FP32 out: mu, rstd.  eps >= 0.  rows == 0 is a no-op.
+ */
+reqat_status reqat_layer_norm(const void *x, reqat_dtype dtype, int64_t rows, int64_t cols, int64_t ldx, const void *weight,
+                              const void *bias, reqat_dtype w_dtype, float eps, int center, void *y, int64_t ldy, float *stats,
+                              void *stream);
+
+/*
+ * Backward pass, from x and stats: with h = (x - mu) rstd and g = dy weight,
+ *     dx = rstd (g - [center] mean g - h mean(g h)),
+ *     dweight = sum over rows of dy h,   dbias = sum over rows of dy (NULL: not computed).
+ * dx may be dy or x with the same stride; any other overlap is not allowed.
+ * workspace: reqat_layer_norm_workspace_bytes(dtype, rows, cols, dbias != NULL) bytes,
+ * 4-byte aligned.  rows == 0 writes zeros into dweight and dbias.
+ */
+reqat_status reqat_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, reqat_dtype dtype, int64_t rows,
+                                       int64_t cols, const void *weight, reqat_dtype w_dtype, const float *stats, int center,
+                                       void *dx, int64_t lddx, void *dweight, void *dbias, void *workspace, void *stream);
+
+/* Bytes of workspace of reqat_layer_norm_backward; never falls as rows grow (0 on bad arguments). */
+size_t reqat_layer_norm_workspace_bytes(reqat_dtype dtype, int64_t rows, int64_t cols, int bias);
+
+/*
+ * Embedding lookup: out[t] = scale * table[ids[t]], rounded once (exact for scale 1);
+ * an id outside [0, V) is padding and gives a row of zeros.
+ *   ids [T] int32, T at most 2^22; table [V][ld_table], V at most 2^23; out [T][ldo] of
+ *   dtype, D columns, at most 2^20; out must not overlap table (REQAT_E_UNSUPPORTED).
+ */
+reqat_status reqat_embedding(const int32_t *ids, int64_t T, const void *table, reqat_dtype dtype, int64_t V, int64_t D,
+                             int64_t ld_table, float scale, void *out, int64_t ldo, void *stream);
+
+/*
+ * Its gradient: dtable[v] = scale * (sum of dy[t] over the t with ids[t] == v, in
+ * rising order of t within pieces of 64), added to what dtable holds when accumulate != 0
+ * (rows without a token are not touched then), else written, zeros included; summed in
+ * FP32 and rounded once to table_dtype.  Padding has no gradient.
+ *   dy [T][lddy] of dtype; dtable [V][ld_table] of table_dtype, no overlap with dy;
+ *   workspace: reqat_embedding_workspace_bytes(T, V, D) bytes, 16-byte aligned.
+ */
+reqat_status reqat_embedding_backward(const void *dy, reqat_dtype dtype, int64_t lddy, const int32_t *ids, int64_t T, int64_t V,
+                                      int64_t D, float scale, void *dtable, reqat_dtype table_dtype, int64_t ld_table,
+                                      int accumulate, void *workspace, void *stream);
+
+/* Bytes of workspace of reqat_embedding_backward (0 on bad arguments); never falls as a size grows. */
+size_t reqat_embedding_workspace_bytes(int64_t T, int64_t V, int64_t D);
+
+/*
+ * AdamW step over many tensors, each of n elements without gaps:
+ *     g = grad * *grad_scale (NULL: 1),  m' = b1 m + (1 - b1) g,  v' = b2 v + (1 - b2) g^2,
+ *     p' = (1 - lr weight_decay) p - lr / (1 - b1^step) * m' / (sqrt(v') / sqrt(1 - b2^step) + eps),
+ * every product, sum and root rounded to FP32 (b1, 1 - b1, b2 and 1 - b2 are FP32 numbers,
+ * taken from the doubles).
+ *   p [n] of p_dtype, in place; copy: NULL, or [n] bfloat16 out, RN_bf16(p') (the weights
+ *   that the quantizers read, beside FP32 master weights);  g [n] of g_dtype.
+ *   state_bits 32: m, v [n] FP32, in place; m_scale, v_scale unused.
+ *   state_bits 8: m, v [n] uint8 and FP32 scales [ceil(n / 128)], one for each 128 elements:
+ *     m = E4M3(code) s,  s = RN(max |m'| / 448), code of RN(m' / s) to nearest, ties to even;
+ *     v = RN(u u), u = RN(q(code) s), q(0) = 0, q(c) the FP32 number of bit pattern
+ *     (c + 1792) << 19: 2^-15 (1 + 1/16) to 1.9375, four bits behind the binary point,
+ *     s = RN(max u' / 1.9375), u' = RN(sqrt(v')), code of RN(u' / s) to nearest, ties to
+ *     even, and never 0 for u' / s > 0.  All bytes zero is the state at the start.
+ *     A block with a NaN or Inf has scale NaN and codes 0, a block of zeros scale 0.
+ * Tensors of n == 0 are skipped.  No two tensors may overlap; the tensors and the struct
+ * array are checked on the host, which reads the array during the call.  count tensors
+ * take ceil(count / 56) launches.
+ *   hyper: host memory; step counts from 1 (REQAT_E_UNSUPPORTED for less, for a beta outside
+ *     [0, 1), a negative eps or values that are not finite).
+ *   coef: NULL, or three device floats from reqat_adamw_coefficients, which take the
+ *     place of lr, weight_decay and step.
+ */
+typedef struct reqat_adamw_tensor_s {
+    void *p;
+    const void *g;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    void *copy;
+    int64_t n;
+} reqat_adamw_tensor;
+
+typedef struct reqat_adamw_hyper_s {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;
+} reqat_adamw_hyper;
+
+reqat_status reqat_adamw_step(const reqat_adamw_tensor *tensors, int64_t count, reqat_dtype p_dtype, reqat_dtype g_dtype,
+                              int state_bits, const reqat_adamw_hyper *hyper, const float *grad_scale, const float *coef,
+                              void *stream);
+
+/*
+ * For steps captured in a graph: adds one to *step (device) and writes the step's three
+ * factors into coef[0..2], with *lr (device; NULL: hyper's lr) as the rate.  hyper->step
+ * is not used.
+ */
+reqat_status reqat_adamw_coefficients(const reqat_adamw_hyper *hyper, const float *lr, int32_t *step, float *coef, void *stream);
+
+/* The values of 8-bit states: m_out, v_out [n] FP32 from codes [n] and scales [ceil(n / 128)]. */
+reqat_status reqat_adamw_moments(const uint8_t *m, const float *m_scale, const uint8_t *v, const float *v_scale, int64_t n,
+                                 float *m_out, float *v_out, void *stream);
+
+/*
  * Block-scaled FP4 x FP4 product (the W4A4 GEMM of Sec. 5.3):
  *   Y[m][n] = g_a * g_b * sum_k A^[m][k] * B^[n][k]
  * with A^ = E2M1(a_codes) * block scale (and likewise B^), FP32 accumulation.

@@ -14,7 +14,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libreqat.so")
 SOURCES = ["api.hip", "quantize.hip", "gemm.hip", "gemm_skinny.hip", "gemm_tile256.hip", "gemm_ksplit.hip", "gemm_w4a16.hip", "gemm_w4a16_tile.hip",
-           "kv4.hip", "kv4_cache.hip", "kv4_attention.hip", "sem.hip"]
+           "kv4.hip", "kv4_cache.hip", "kv4_attention.hip", "sem.hip", "api_train.hip", "policy.hip", "norm.hip",
+           "embedding.hip", "adamw.hip"]
 PROBE_LIB = os.path.join(HERE, "libreqat_probe.so")
 PROBE_SOURCE = "probe_mfma.hip"
 

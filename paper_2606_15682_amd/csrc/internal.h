@@ -8,6 +8,7 @@
 #include "dispatch.h"
 #include "kv4_cache.h"
 #include "kv4_plan.h"
+#include "norm_plan.h"
 
 namespace reqat {
 
@@ -102,6 +103,78 @@ hipError_t launch_sem_forward(const uint16_t *logits, int64_t T, int64_t V, int6
 hipError_t launch_sem_backward(const uint16_t *logits, int64_t T, int64_t V, int64_t ld, const int32_t *targets,
                                const float *stats, const float *weights, float lambda, float scale, void *grad,
                                bool grad_bf16, int64_t ldg, hipStream_t stream);
+
+// Policy loss (policy.hip).  stats [T][4]: lp, log-sum-exp, dL/dlp, ratio; loss [4].
+struct PolicyArgs {
+    const void *logits;                    // [T][ld] bfloat16 or FP32
+    const int32_t *targets;
+    const float *old_logp, *adv, *ref;     // ref null: no KL term
+    const float *weights;                  // null: default_weight for every token
+    float *stats, *loss;
+    void *grad;                            // [T][ldg] of the logits' type, or null
+    const float *grad_loss;                // backward: dL's factor on the device, or null
+    int64_t T, V, ld, ldg;
+    float default_weight, low, high;       // low, high: bounds of the ratio
+    float kl, c, inv_temp;                 // c: log2(e) / temperature
+};
+// The statistics and the loss, and the gradient where a.grad is not null.
+hipError_t launch_policy_loss(const PolicyArgs &a, bool bf16, hipStream_t stream);
+// The gradient from logits, targets and stats.
+hipError_t launch_policy_backward(const PolicyArgs &a, bool bf16, hipStream_t stream);
+
+// Layer norm (norm.hip), K <= kNormMaxCols.  stats [M][2]: mean, 1 / standard deviation.
+struct NormArgs {
+    const void *x, *dy, *w, *b;            // x, dy, y, dx of one type; w, b, dw, db of another; b, db may be null
+    void *y, *dx, *dw, *db;
+    float *stats, *partials;               // partials: norm_plan's groups x K sums of dw, then of db
+    int64_t M, K, ldx, lddy, ldy, lddx;
+    float eps;
+    bool center, w_bf16;
+};
+hipError_t launch_norm(const NormArgs &a, bool bf16, bool backward, hipStream_t stream);
+
+// Embedding (embedding.hip).
+constexpr int kEmbedPiece = 64;            // tokens of one id that one workgroup adds up
+struct EmbedArgs {
+    const int32_t *ids;
+    const void *table;
+    void *out;
+    int64_t T, V, D, ld_table, ld_out;
+    float scale;
+};
+hipError_t launch_embedding(const EmbedArgs &a, bool bf16, hipStream_t stream);
+struct EmbedGradArgs {
+    const void *dy;
+    void *dtable;
+    int32_t *row_start, *order, *sorted;   // workspace: [V + 1], [T], [T]
+    float *partials;
+    int64_t T, V, D, ld_dy, ld_table;
+    float scale;
+    bool accumulate;
+};
+size_t embedding_workspace_bytes(int64_t T, int64_t V, int64_t D);
+size_t embedding_workspace_head(int64_t T, int64_t V);          // bytes before the partial sums
+hipError_t launch_embedding_backward(const EmbedGradArgs &a, const int32_t *ids, bool bf16, bool table_bf16, hipStream_t stream);
+
+// AdamW (adamw.hip).
+constexpr int kAdamBlock = 128;            // elements to a scale of the 8-bit states
+struct AdamTensor {
+    void *p;
+    const void *g;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    void *copy;
+    int64_t n;
+};
+struct AdamCoef {
+    float b1, c1, b2, c2, decay, step, root, eps;
+};
+hipError_t launch_adamw(const AdamTensor *tensors, int64_t count, bool p_bf16, bool g_bf16, int bits, const AdamCoef &c,
+                        const float *dev_coef, const float *grad_scale, hipStream_t stream);
+hipError_t launch_adamw_coef(double lr, double beta1, double beta2, double decay, const float *lr_dev, int32_t *step,
+                             float *coef, hipStream_t stream);
+hipError_t launch_adamw_moments(const uint8_t *mc, const float *ms, const uint8_t *vc, const float *vs, int64_t n, float *m,
+                                float *v, hipStream_t stream);
 
 bool gemm_tile256_supported(Fmt fmt, int64_t M, int64_t N, int64_t K, int64_t ldy);
 // Skinny product for M <= 64 (K % 128 == 0, K > 0).  packed: b_codes / b_scales

@@ -37,6 +37,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libreqat.so
 _VP = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _INT = ctypes.c_int
+_F32 = ctypes.c_float
 SIGNATURES = {
     "reqat_quantize_fp4": (_INT, [_INT, _VP, _I64, _I64, _I64, _VP, _VP, _VP, _INT, _VP, _VP]),
     "reqat_fakequant_fp4": (_INT, [_INT, _VP, _I64, _I64, _I64, _VP, _I64, _VP, _INT, _VP, _VP]),
@@ -72,6 +73,19 @@ SIGNATURES = {
     "reqat_gemm_w4a16_packed": (_INT, [_I64, _I64, _I64, _VP, _I64, _VP, _VP, _INT, _I64, _VP, _VP]),
     "reqat_quantize_mxfp4_rht": (_INT, [_VP, _I64, _I64, _I64, ctypes.c_uint32, _VP, _VP, _VP]),
     "reqat_fakequant_mxfp4_rht": (_INT, [_VP, _I64, _I64, _I64, ctypes.c_uint32, _VP, _I64, _VP]),
+    "reqat_policy_loss": (_INT, [_VP, _INT, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP, _F32, _F32, _F32, _F32, _VP, _VP, _VP,
+                                 _I64, _VP]),
+    "reqat_policy_loss_backward": (_INT, [_VP, _INT, _I64, _I64, _I64, _VP, _VP, _F32, _VP, _VP, _I64, _VP]),
+    "reqat_layer_norm": (_INT, [_VP, _INT, _I64, _I64, _I64, _VP, _VP, _INT, _F32, _INT, _VP, _I64, _VP, _VP]),
+    "reqat_layer_norm_workspace_bytes": (ctypes.c_size_t, [_INT, _I64, _I64, _INT]),
+    "reqat_layer_norm_backward": (_INT, [_VP, _I64, _VP, _I64, _INT, _I64, _I64, _VP, _INT, _VP, _INT, _VP, _I64, _VP, _VP,
+                                         _VP, _VP]),
+    "reqat_embedding": (_INT, [_VP, _I64, _VP, _INT, _I64, _I64, _I64, _F32, _VP, _I64, _VP]),
+    "reqat_embedding_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _I64]),
+    "reqat_embedding_backward": (_INT, [_VP, _INT, _I64, _VP, _I64, _I64, _I64, _F32, _VP, _INT, _I64, _INT, _VP, _VP]),
+    "reqat_adamw_step": (_INT, [_VP, _I64, _INT, _INT, _INT, _VP, _VP, _VP, _VP]),
+    "reqat_adamw_coefficients": (_INT, [_VP, _VP, _VP, _VP, _VP]),
+    "reqat_adamw_moments": (_INT, [_VP, _VP, _VP, _VP, _I64, _VP, _VP, _VP]),
     "reqat_workspace_bytes": (ctypes.c_size_t, []),
     "reqat_status_str": (ctypes.c_char_p, [_INT]),
     "reqat_abi_version": (_INT, []),
@@ -208,6 +222,71 @@ def reqat_quantize_mxfp4_rht(x, rows, cols, ldx, signs, codes, scales, stream):
 
 def reqat_fakequant_mxfp4_rht(x, rows, cols, ldx, signs, y, ldy, stream):
     return load().reqat_fakequant_mxfp4_rht(x, rows, cols, ldx, signs, y, ldy, stream)
+
+
+def reqat_policy_loss(logits, dtype, T, V, ld, targets, old_logp, advantages, ref_logp, weights, clip_low, clip_high,
+                      kl_coef, temperature, stats, loss, grad, ldg, stream):
+    return load().reqat_policy_loss(logits, dtype, T, V, ld, targets, old_logp, advantages, ref_logp, weights, clip_low,
+                                    clip_high, kl_coef, temperature, stats, loss, grad, ldg, stream)
+
+
+def reqat_policy_loss_backward(logits, dtype, T, V, ld, targets, stats, temperature, grad_loss, grad, ldg, stream):
+    return load().reqat_policy_loss_backward(logits, dtype, T, V, ld, targets, stats, temperature, grad_loss, grad, ldg,
+                                             stream)
+
+
+def reqat_layer_norm(x, dtype, rows, cols, ldx, weight, bias, w_dtype, eps, center, y, ldy, stats, stream):
+    return load().reqat_layer_norm(x, dtype, rows, cols, ldx, weight, bias, w_dtype, eps, center, y, ldy, stats, stream)
+
+
+def reqat_layer_norm_workspace_bytes(dtype, rows, cols, bias) -> int:
+    return load().reqat_layer_norm_workspace_bytes(dtype, rows, cols, bias)
+
+
+def reqat_layer_norm_backward(dy, lddy, x, ldx, dtype, rows, cols, weight, w_dtype, stats, center, dx, lddx, dweight,
+                              dbias, workspace, stream):
+    return load().reqat_layer_norm_backward(dy, lddy, x, ldx, dtype, rows, cols, weight, w_dtype, stats, center, dx, lddx,
+                                            dweight, dbias, workspace, stream)
+
+
+def reqat_embedding(ids, T, table, dtype, V, D, ld_table, scale, out, ldo, stream):
+    return load().reqat_embedding(ids, T, table, dtype, V, D, ld_table, scale, out, ldo, stream)
+
+
+def reqat_embedding_workspace_bytes(T, V, D) -> int:
+    return load().reqat_embedding_workspace_bytes(T, V, D)
+
+
+def reqat_embedding_backward(dy, dtype, lddy, ids, T, V, D, scale, dtable, table_dtype, ld_table, accumulate, workspace,
+                             stream):
+    return load().reqat_embedding_backward(dy, dtype, lddy, ids, T, V, D, scale, dtable, table_dtype, ld_table, accumulate,
+                                           workspace, stream)
+
+
+class AdamwTensor(ctypes.Structure):
+    """reqat_adamw_tensor of the C ABI."""
+    _fields_ = [("p", _VP), ("g", _VP), ("m", _VP), ("v", _VP), ("m_scale", _VP), ("v_scale", _VP), ("copy", _VP),
+                ("n", _I64)]
+
+
+class AdamwHyper(ctypes.Structure):
+    """reqat_adamw_hyper of the C ABI."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", _I64)]
+
+
+def reqat_adamw_step(tensors, count, p_dtype, g_dtype, state_bits, hyper, grad_scale, coef, stream):
+    """tensors: an array of AdamwTensor (or None), hyper: an AdamwHyper (or None)."""
+    return load().reqat_adamw_step(_cache_ref(tensors), count, p_dtype, g_dtype, state_bits, _cache_ref(hyper), grad_scale,
+                                   coef, stream)
+
+
+def reqat_adamw_coefficients(hyper, lr, step, coef, stream):
+    return load().reqat_adamw_coefficients(_cache_ref(hyper), lr, step, coef, stream)
+
+
+def reqat_adamw_moments(m, m_scale, v, v_scale, n, m_out, v_out, stream):
+    return load().reqat_adamw_moments(m, m_scale, v, v_scale, n, m_out, v_out, stream)
 
 
 def reqat_w4a4_packed_bytes(fmt, N, K) -> int:
@@ -1027,3 +1106,356 @@ class SemLoss(torch.autograd.Function):
         logits, targets, stats, weights = ctx.saved_tensors
         grad = sem_loss_backward(logits, targets, stats, weights, ctx.lam, scale=float(g), out_dtype=logits.dtype)
         return grad, None, None, None
+
+
+# ------------------------------------------------------------------ the operators around the quantized layers
+
+def _call(fn, device, *args):
+    """The C call with the device current, on its current stream."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(device)), fn.__name__)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(device)), fn.__name__)
+
+
+def _float_rows(x, name):
+    """Rows, columns, row stride and C dtype of a 2-D bfloat16 or float32 tensor with contiguous rows."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("%s must be a 2-D bfloat16 or float32 tensor" % name)
+    rows, cols = x.shape
+    if cols > 1 and x.stride(1) != 1 or rows > 1 and x.stride(0) < cols:
+        raise ValueError("%s must have contiguous rows that do not overlap" % name)
+    return rows, cols, x.stride(0) if rows > 1 else max(cols, 1), _dtype_arg(x.dtype)
+
+
+def _float_out(t, rows, cols, dtype, device, name):
+    """A given output [rows, cols], or a new one; returns it and its row stride."""
+    if t is None:
+        return torch.empty((rows, cols), dtype=dtype, device=device), max(cols, 1)
+    ld = _out2d(t, rows, cols, dtype, device, name)
+    if ld < cols:
+        raise ValueError("%s must have rows that do not overlap" % name)
+    return t, ld
+
+
+def _vector(t, n, device, name, dtypes=(torch.float32,)):
+    """A contiguous vector of n numbers."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise TypeError("%s must be a tensor of %s" % (name, " or ".join(str(d) for d in dtypes)))
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError("%s must be contiguous, of shape (%d,), got %s" % (name, n, tuple(t.shape)))
+    _same_device(t, device, name)
+    return t
+
+
+def _policy_loss(logits, targets, old_logp, advantages, ref_logp, weights, clip_low, clip_high, kl_coef, temperature, grad,
+                 out):
+    T, V, ld, dt = _float_rows(logits, "logits")
+    dev = logits.device
+    _vector(targets, T, dev, "targets", (torch.int32,))
+    _vector(old_logp, T, dev, "old_logp")
+    _vector(advantages, T, dev, "advantages")
+    if ref_logp is not None:
+        _vector(ref_logp, T, dev, "ref_logp")
+    elif kl_coef != 0.0:
+        raise ValueError("kl_coef without ref_logp")
+    if weights is not None:
+        _vector(weights, T, dev, "weights")
+    ldg = 0
+    if grad:
+        out, ldg = _float_out(out, T, V, logits.dtype, dev, "out")
+    stats = torch.empty((T, 4), dtype=torch.float32, device=dev)
+    loss = torch.empty(4, dtype=torch.float32, device=dev)
+    _require_cuda(logits, "logits")
+    _call(reqat_policy_loss, dev, logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), old_logp.data_ptr(),
+          advantages.data_ptr(), _ptr(ref_logp), _ptr(weights), clip_low, clip_high, kl_coef, temperature, stats.data_ptr(),
+          loss.data_ptr(), _ptr(out) if grad else None, ldg)
+    return loss, stats, out
+
+
+def policy_loss(logits, targets, old_logp, advantages, ref_logp=None, weights=None, clip_low=0.2, clip_high=0.2,
+                kl_coef=0.0, temperature=1.0):
+    """Clipped policy loss with a KL term, of bfloat16 or float32 logits [T, V] (rows may be strided) and int32 targets,
+    float32 old_logp, advantages, ref_logp and weights [T].
+
+    With r = exp(log p - old_logp) and x = ref_logp - log p a token's loss is
+    -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(x) - x - 1); the loss is their sum under ``weights``
+    (mask and normaliser in one, default 1 / T).  Rows of weight 0 are not read.  Returns (loss[4] = the loss, its
+    surrogate part, the KL term's weighted sum, the clipped share; stats [T, 4] = log p of the target, log-sum-exp,
+    dL / d log p, r)."""
+    return _policy_loss(logits, targets, old_logp, advantages, ref_logp, weights, clip_low, clip_high, kl_coef, temperature,
+                        False, None)[:2]
+
+
+def policy_loss_grad(logits, targets, old_logp, advantages, ref_logp=None, weights=None, clip_low=0.2, clip_high=0.2,
+                     kl_coef=0.0, temperature=1.0, out=None):
+    """policy_loss() and dL/dlogits in one pass.  Returns (loss, stats, grad), grad like the logits; out: where it goes,
+    the logits themselves allowed."""
+    return _policy_loss(logits, targets, old_logp, advantages, ref_logp, weights, clip_low, clip_high, kl_coef, temperature,
+                        True, out)
+
+
+def policy_loss_backward(logits, targets, stats, temperature=1.0, grad_loss=None, out=None):
+    """dL/dlogits from the logits and the statistics of policy_loss(), times grad_loss (a float32 tensor of one element).
+    out may be the logits."""
+    T, V, ld, dt = _float_rows(logits, "logits")
+    dev = logits.device
+    _vector(targets, T, dev, "targets", (torch.int32,))
+    _index_arg(stats, (T, 4), torch.float32, dev, "stats")
+    if grad_loss is not None:
+        _scale_arg(grad_loss, NVFP4, dev, "grad_loss")
+    out, ldg = _float_out(out, T, V, logits.dtype, dev, "out")
+    _require_cuda(logits, "logits")
+    _call(reqat_policy_loss_backward, dev, logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), stats.data_ptr(),
+          temperature, _ptr(grad_loss), out.data_ptr(), ldg)
+    return out
+
+
+_FLOATS = (torch.bfloat16, torch.float32)
+
+
+def layer_norm(x, weight, bias=None, eps=1e-6, center=True, out=None):
+    """Layer norm of the rows of x (bfloat16 or float32 [rows, cols], rows may be strided), or with center=False the
+    root-mean-square norm, with weight and bias [cols] (bfloat16 or float32, both alike).  Returns (y like x; stats
+    [rows, 2] = mean, 1 / standard deviation).  out may be x."""
+    rows, cols, ldx, dt = _float_rows(x, "x")
+    dev = x.device
+    _vector(weight, cols, dev, "weight", _FLOATS)
+    if bias is not None:
+        _vector(bias, cols, dev, "bias", (weight.dtype,))
+    y, ldy = _float_out(out, rows, cols, x.dtype, dev, "out")
+    stats = torch.empty((rows, 2), dtype=torch.float32, device=dev)
+    _require_cuda(x, "x")
+    _call(reqat_layer_norm, dev, x.data_ptr(), dt, rows, cols, ldx, weight.data_ptr(), _ptr(bias), _dtype_arg(weight.dtype),
+          eps, 1 if center else 0, y.data_ptr(), ldy, stats.data_ptr())
+    return y, stats
+
+
+def layer_norm_backward(dy, x, weight, stats, center=True, bias=False, out=None, ws=None):
+    """Gradients of layer_norm() from its input and statistics.  Returns (dx like x, dweight like weight, dbias or None).
+    out (where dx goes) may be dy or x; ws: uint8 tensor of at least
+    reqat_layer_norm_workspace_bytes(dtype, rows, cols, bias) bytes."""
+    rows, cols, ldx, dt = _float_rows(x, "x")
+    dev = x.device
+    if not isinstance(dy, torch.Tensor) or dy.dtype != x.dtype or dy.shape != x.shape:
+        raise ValueError("dy must have x's type and shape")
+    lddy = _float_rows(dy, "dy")[2]
+    _same_device(dy, dev, "dy")
+    _vector(weight, cols, dev, "weight", _FLOATS)
+    _index_arg(stats, (rows, 2), torch.float32, dev, "stats")
+    dx, lddx = _float_out(out, rows, cols, x.dtype, dev, "out")
+    need = reqat_layer_norm_workspace_bytes(dt, rows, cols, 1 if bias else 0)
+    if ws is not None:
+        _workspace_arg(ws, need, dev)
+    _require_cuda(x, "x")
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    dw = torch.empty(cols, dtype=weight.dtype, device=dev)
+    db = torch.empty(cols, dtype=weight.dtype, device=dev) if bias else None
+    _call(reqat_layer_norm_backward, dev, dy.data_ptr(), lddy, x.data_ptr(), ldx, dt, rows, cols, weight.data_ptr(),
+          _dtype_arg(weight.dtype), stats.data_ptr(), 1 if center else 0, dx.data_ptr(), lddx, dw.data_ptr(), _ptr(db),
+          ws.data_ptr())
+    return dx, dw, db
+
+
+def embedding(ids, table, scale=1.0, out=None):
+    """Rows of the table (bfloat16 or float32 [V, D]) times scale, for int32 ids [T]: [T, D] like the table.  An id outside
+    the table is padding and gives zeros."""
+    V, D, ld, dt = _float_rows(table, "table")
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        raise TypeError("ids must be a 1-D int32 tensor")
+    T, dev = ids.shape[0], table.device
+    _vector(ids, T, dev, "ids", (torch.int32,))
+    out, ldo = _float_out(out, T, D, table.dtype, dev, "out")
+    _require_cuda(table, "table")
+    _call(reqat_embedding, dev, ids.data_ptr(), T, table.data_ptr(), dt, V, D, ld, scale, out.data_ptr(), ldo)
+    return out
+
+
+def embedding_backward(dy, ids, rows, scale=1.0, out=None, accumulate=False, out_dtype=None, ws=None):
+    """Gradient of the table [rows, D] of embedding() from dy [T, D]: every id's rows of dy summed in float32, in a fixed
+    order, times scale.  With accumulate it is added to ``out``, whose other rows stay untouched (a table that has a
+    gradient already, as one that is the output layer's too).  out_dtype: default dy's, or out's.  ws: uint8 tensor of at
+    least reqat_embedding_workspace_bytes(T, rows, D) bytes."""
+    T, D, lddy, dt = _float_rows(dy, "dy")
+    dev = dy.device
+    _vector(ids, T, dev, "ids", (torch.int32,))
+    if out is None and accumulate:
+        raise ValueError("accumulate needs out")
+    if out_dtype is None:
+        out_dtype = dy.dtype if out is None else out.dtype
+    out_dt = _dtype_arg(out_dtype)
+    out, ld = _float_out(out, rows, D, out_dtype, dev, "out")
+    need = reqat_embedding_workspace_bytes(T, rows, D)
+    if ws is not None:
+        _workspace_arg(ws, need, dev)
+    _require_cuda(dy, "dy")
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _call(reqat_embedding_backward, dev, dy.data_ptr(), dt, lddy, ids.data_ptr(), T, rows, D, scale, out.data_ptr(), out_dt,
+          ld, 1 if accumulate else 0, ws.data_ptr())
+    return out
+
+
+class AdamW:
+    """AdamW over many tensors in few launches, with states in 32 or 8 bits.
+
+    params: contiguous tensors of one type, bfloat16 or float32, on one device, updated in place; copies: for each of them
+    a bfloat16 tensor of the same shape that receives the new values rounded (the weights that the quantizers read, beside
+    float32 master weights), or None.  The states of all tensors lie in one buffer each: ``m`` and ``v``, float32, or uint8
+    codes with the float32 scales ``m_scale`` and ``v_scale`` of every 128 elements (the formats are stated in
+    include/reqat.h); tensor i has the elements ``offsets[i]`` .. ``offsets[i]`` + its size.  All zeros at the start, they
+    may be written in place.  ``steps`` counts the steps taken; ``lr``, ``betas``, ``eps`` and ``weight_decay`` may be
+    assigned between steps.
+
+    captured=True is for steps in a HIP graph: the count is ``step_tensor`` (int32) and the rate ``lr_tensor`` (float32),
+    on the device, the count rising with every replay.  Parameters, copies, states and gradients of a captured step stay
+    where they are."""
+
+    def __init__(self, params, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, copies=None,
+                 captured=False):
+        self.params = list(params)
+        self.copies = None if copies is None else list(copies)
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        if not self.params:
+            raise ValueError("no parameters")
+        if self.copies is not None and len(self.copies) != len(self.params):
+            raise ValueError("copies must have one tensor (or None) for each parameter")
+        first = self.params[0]
+        if not isinstance(first, torch.Tensor) or first.dtype not in _FLOATS:
+            raise TypeError("parameters must be bfloat16 or float32 tensors")
+        self.device, self.dtype, self.state_bits = first.device, first.dtype, state_bits
+        spans = []
+        for i, p in enumerate(self.params):
+            self._tensor_arg(p, p, (self.dtype,), "params[%d]" % i)
+            spans.append((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()))
+            c = None if self.copies is None else self.copies[i]
+            if c is not None:
+                self._tensor_arg(c, p, (torch.bfloat16,), "copies[%d]" % i)
+                spans.append((c.data_ptr(), c.data_ptr() + c.numel() * 2))
+        spans = sorted(s for s in spans if s[1] > s[0])
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("parameters and copies must not overlap")
+        self.lr, self.betas, self.eps, self.weight_decay, self.steps = lr, betas, eps, weight_decay, 0
+        self.offsets, size = [], 0
+        for p in self.params:
+            self.offsets.append(size)
+            size += -(-p.numel() // 128) * 128
+        kind = torch.float32 if state_bits == 32 else torch.uint8
+        self.m, self.v = (torch.zeros(size, dtype=kind, device=self.device) for _ in range(2))
+        self.m_scale = self.v_scale = None
+        if state_bits == 8:
+            self.m_scale, self.v_scale = (torch.zeros(size // 128, dtype=torch.float32, device=self.device) for _ in range(2))
+        self.step_tensor = self.lr_tensor = self._coef = None
+        if captured:
+            self.step_tensor = torch.zeros(1, dtype=torch.int32, device=self.device)
+            self.lr_tensor = torch.full((1,), lr, dtype=torch.float32, device=self.device)
+            self._coef = torch.zeros(3, dtype=torch.float32, device=self.device)
+
+    def _tensor_arg(self, t, like, dtypes, name):
+        if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+            raise TypeError("%s must be a tensor of %s" % (name, " or ".join(str(d) for d in dtypes)))
+        if t.shape != like.shape:
+            raise ValueError("%s must have shape %s, got %s" % (name, tuple(like.shape), tuple(t.shape)))
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+        _same_device(t, self.device, name)
+
+    def step(self, grads, grad_scale=None):
+        """One step with the gradients of all parameters (tensors of their shapes, all bfloat16 or all float32; None: the
+        parameter is left out of this step), each times grad_scale (a float32 tensor of one element, as of a clipped
+        norm) first."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError("grads must have one tensor (or None) for each parameter")
+        if grad_scale is not None:
+            _scale_arg(grad_scale, NVFP4, self.device, "grad_scale")
+        kind = next((g.dtype for g in grads if isinstance(g, torch.Tensor)), torch.float32)
+        m, v, wide = self.m.data_ptr(), self.v.data_ptr(), self.m.element_size()
+        ms, vs = _ptr(self.m_scale), _ptr(self.v_scale)
+        tensors, count = (AdamwTensor * len(grads))(), 0
+        for i, (g, p, at) in enumerate(zip(grads, self.params, self.offsets)):
+            if g is None:
+                continue
+            self._tensor_arg(g, p, (kind,) if kind in _FLOATS else _FLOATS, "grads[%d]" % i)
+            c = None if self.copies is None else self.copies[i]
+            scales = (None, None) if ms is None else (ms + at // 32, vs + at // 32)
+            tensors[count] = AdamwTensor(p.data_ptr(), g.data_ptr(), m + at * wide, v + at * wide, *scales, _ptr(c), p.numel())
+            count += 1
+        hyper = AdamwHyper(self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1)
+        _require_cuda(self.params[0], "params[0]")
+        if self._coef is not None:
+            _call(reqat_adamw_coefficients, self.device, hyper, self.lr_tensor.data_ptr(), self.step_tensor.data_ptr(),
+                  self._coef.data_ptr())
+        _call(reqat_adamw_step, self.device, tensors, count, _dtype_arg(self.dtype), _dtype_arg(kind), self.state_bits, hyper,
+              _ptr(grad_scale), _ptr(self._coef))
+        self.steps += 1
+
+    def moments(self):
+        """The values of m and v as float32 buffers laid out like them (the states themselves when they have 32 bits)."""
+        if self.state_bits == 32:
+            return self.m, self.v
+        _require_cuda(self.m, "m")
+        n = self.m.numel()
+        m, v = (torch.empty(n, dtype=torch.float32, device=self.device) for _ in range(2))
+        _call(reqat_adamw_moments, self.device, self.m.data_ptr(), self.m_scale.data_ptr(), self.v.data_ptr(),
+              self.v_scale.data_ptr(), n, m.data_ptr(), v.data_ptr())
+        return m, v
+
+
+class PolicyLoss(torch.autograd.Function):
+    """The policy loss as an autograd function over the logits; the arguments of policy_loss() in order."""
+
+    @staticmethod
+    def forward(ctx, logits, targets, old_logp, advantages, ref_logp=None, weights=None, clip_low=0.2, clip_high=0.2,
+                kl_coef=0.0, temperature=1.0):
+        loss, stats = policy_loss(logits, targets, old_logp, advantages, ref_logp, weights, clip_low, clip_high, kl_coef,
+                                  temperature)
+        ctx.save_for_backward(logits, targets, stats)
+        ctx.temperature = temperature
+        return loss[0]
+
+    @staticmethod
+    def backward(ctx, g):
+        logits, targets, stats = ctx.saved_tensors
+        grad = policy_loss_backward(logits, targets, stats, ctx.temperature, g.reshape(1).to(torch.float32))
+        return (grad,) + (None,) * 9
+
+
+class LayerNorm(torch.autograd.Function):
+    """layer_norm() as an autograd function of x, weight and bias."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias=None, eps=1e-6, center=True):
+        y, stats = layer_norm(x, weight, bias, eps, center)
+        ctx.save_for_backward(x, weight, stats)
+        ctx.center, ctx.bias = center, bias is not None
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, stats = ctx.saved_tensors
+        dx, dw, db = layer_norm_backward(_dense_rows(dy), x, weight, stats, ctx.center, ctx.bias)
+        return dx, dw, db, None, None
+
+
+class Embedding(torch.autograd.Function):
+    """embedding() as an autograd function of the table (ids come first, as in embedding())."""
+
+    @staticmethod
+    def forward(ctx, ids, table, scale=1.0):
+        ctx.save_for_backward(ids)
+        ctx.rows, ctx.scale = table.shape[0], scale
+        return embedding(ids, table, scale)
+
+    @staticmethod
+    def backward(ctx, dy):
+        ids, = ctx.saved_tensors
+        return None, embedding_backward(_dense_rows(dy), ids, ctx.rows, ctx.scale), None
+
+
+def _dense_rows(g):
+    """A gradient as the kernels take it: one that autograd expanded has rows without an extent of their own."""
+    return g if g.stride(1) == 1 and g.stride(0) >= g.shape[1] else g.contiguous()
