@@ -458,16 +458,21 @@ reqat_status reqat_sem_loss_backward(const void *logits, int64_t T, int64_t V, i
  *     dL/dlp, r (kept for the backward pass);
  *   loss [4] FP32 out: L, sum w (-min(..)), sum w (exp(x) - x - 1), sum w [not inside];
  *   grad: NULL, or [T][ldg] of dtype out, dL/dz_j = (dL/dlp) ([j = y] - p_j) / temperature
- *     in the same call, the row read once more from the caches.  grad == logits with
- *     the same stride is allowed, any other overlap is not (REQAT_E_UNSUPPORTED).
+ *     in the same call.  grad == logits with the same stride is allowed, any other
+ *     overlap is not (REQAT_E_UNSUPPORTED);
+ *   workspace: reqat_policy_loss_workspace_bytes(dtype, T, V) bytes, 16-byte aligned
+ *     (may be NULL when that is 0): statistics of the slices that few rows are cut into.
  * A logit of -Inf has probability 0; NaN or +Inf gives NaN for its row.
  * 0 <= clip_low <= 1, clip_high >= 0, temperature > 0 and finite
- * (REQAT_E_UNSUPPORTED); T at most 2^22.  T == 0 writes a loss of zeros.
+ * (REQAT_E_UNSUPPORTED); T at most 2^22, V at most 2^30.  T == 0 writes a loss of zeros.
  */
 reqat_status reqat_policy_loss(const void *logits, reqat_dtype dtype, int64_t T, int64_t V, int64_t ld, const int32_t *targets,
                                const float *old_logp, const float *advantages, const float *ref_logp, const float *weights,
                                float clip_low, float clip_high, float kl_coef, float temperature, float *stats, float *loss,
-                               void *grad, int64_t ldg, void *stream);
+                               void *grad, int64_t ldg, void *workspace, void *stream);
+
+/* Bytes of workspace of reqat_policy_loss (0: none; 0 on bad arguments), for these sizes. */
+size_t reqat_policy_loss_workspace_bytes(reqat_dtype dtype, int64_t T, int64_t V);
 
 /*
  * The gradient of the policy loss from logits and stats, times *grad_loss (a device

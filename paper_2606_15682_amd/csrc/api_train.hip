@@ -39,7 +39,7 @@ extern "C" {
 static reqat_status check_policy(const void *logits, reqat_dtype dtype, int64_t T, int64_t V, int64_t ld, const int32_t *targets,
                                  float temperature, const float *stats, const void *grad, int64_t ldg, bool need_grad) {
     if (!dtype_ok(dtype)) return REQAT_E_ENUM;
-    if (T < 0 || T > kMaxTokens || V <= 0 || V > 0x7FFFFFFF || ld < V || !span_ok(T, ld)) return REQAT_E_SHAPE;
+    if (T < 0 || T > kMaxTokens || V <= 0 || V > (1 << 30) || ld < V || !span_ok(T, ld)) return REQAT_E_SHAPE;
     if (need_grad && (ldg < V || !span_ok(T, ldg))) return REQAT_E_SHAPE;
     if (!(temperature > 0.0f) || isinf(temperature)) return REQAT_E_UNSUPPORTED;
     if (T == 0) return REQAT_OK;
@@ -58,19 +58,27 @@ static void set_temperature(PolicyArgs &a, float temperature) {
     a.inv_temp = (float)(1.0 / (double)temperature);
 }
 
+size_t reqat_policy_loss_workspace_bytes(reqat_dtype dtype, int64_t T, int64_t V) {
+    if (!dtype_ok(dtype) || T < 0 || T > kMaxTokens || V <= 0 || V > (1 << 30)) return 0;
+    const PolicyPlan p = policy_plan(T, V, dtype == REQAT_DT_BF16);
+    return p.slices > 1 ? (size_t)(T * p.slices) * 16 : 0;
+}
+
 reqat_status reqat_policy_loss(const void *logits, reqat_dtype dtype, int64_t T, int64_t V, int64_t ld, const int32_t *targets,
                                const float *old_logp, const float *advantages, const float *ref_logp, const float *weights,
                                float clip_low, float clip_high, float kl_coef, float temperature, float *stats, float *loss,
-                               void *grad, int64_t ldg, void *stream) {
+                               void *grad, int64_t ldg, void *workspace, void *stream) {
     const reqat_status st = check_policy(logits, dtype, T, V, ld, targets, temperature, stats, grad, ldg, grad != nullptr);
     if (st != REQAT_OK) return st;
+    if (!workspace && reqat_policy_loss_workspace_bytes(dtype, T, V) > 0) return REQAT_E_NULL;
+    if (!aligned(workspace, 16)) return REQAT_E_ALIGN;
     if (!(clip_low >= 0.0f) || !(clip_low <= 1.0f) || !(clip_high >= 0.0f)) return REQAT_E_UNSUPPORTED;
     if (!loss || (T > 0 && (!old_logp || !advantages || (kl_coef != 0.0f && !ref_logp)))) return REQAT_E_NULL;
     if (!aligned(loss, 4) || !aligned(old_logp, 4) || !aligned(advantages, 4) || !aligned(ref_logp, 4) || !aligned(weights, 4))
         return REQAT_E_ALIGN;
     PolicyArgs a = {};
     a.logits = logits; a.targets = targets; a.old_logp = old_logp; a.adv = advantages; a.weights = weights;
-    a.ref = ref_logp; a.stats = stats; a.loss = loss; a.grad = grad;
+    a.ref = ref_logp; a.stats = stats; a.loss = loss; a.grad = grad; a.parts = reinterpret_cast<float4 *>(workspace);
     a.T = T; a.V = V; a.ld = ld; a.ldg = ldg;
     a.default_weight = T > 0 ? (float)(1.0 / (double)T) : 0.0f;
     a.low = (float)(1.0 - (double)clip_low);

@@ -9,6 +9,7 @@
 #include "kv4_cache.h"
 #include "kv4_plan.h"
 #include "norm_plan.h"
+#include "policy_plan.h"
 
 namespace reqat {
 
@@ -113,6 +114,7 @@ struct PolicyArgs {
     float *stats, *loss;
     void *grad;                            // [T][ldg] of the logits' type, or null
     const float *grad_loss;                // backward: dL's factor on the device, or null
+    float4 *parts;                         // workspace: the statistics of policy_plan's slices
     int64_t T, V, ld, ldg;
     float default_weight, low, high;       // low, high: bounds of the ratio
     float kl, c, inv_temp;                 // c: log2(e) / temperature

@@ -4,9 +4,10 @@
 //   dL/dlp = w_t (-A r [inside] - kl (exp(x) - 1)),  inside: neither A > 0, r > 1 + high nor A < 0, r < 1 - low,
 //   dL/dz_j = (dL/dlp) ([j = y] - p_j) / temperature.
 //
-// Softmax statistics in base-2 units: c = log2(e) / temperature, mb = c max z, t = c z - mb in one fused multiply-add,
-// S = sum 2^t; then lp = ln 2 (t_y - log2 S) and p_j = 2^t_j / S.  The rounding of mb is in every t alike and leaves lp and
-// p as they are.
+// Softmax statistics relative to a reference: the largest logit, scaled.  bfloat16 rows: in base-2 units, c = log2(e) /
+// temperature, reference c max z, t = c z - reference in one fused multiply-add (8 half steps of c z at most, beside a
+// rounding to bfloat16).  FP32 rows: z / temperature is rounded, the reference taken off it, and the difference brought to
+// base 2, so that the likely tokens, whose 1 - p is small, keep FP32's digits.  S = sum 2^t in both.
 #include "internal.h"
 #include "row_io.h"
 
@@ -15,36 +16,56 @@ namespace reqat {
 namespace {
 
 constexpr int kThreads = 512;
+constexpr int kMaxHeld = 18;
 
-// Running maximum and sum of a slice of a row; empty: m = -Inf, mb = 0, S = 0, and so for a slice of -Inf logits alone.
-struct Online {
-    float m, mb, S;
-};
-
-__device__ __forceinline__ void grow(Online &o, float mx, float c) {
-    if (mx > o.m) {
-        const float mxb = mx * c;
-        if (o.S != 0.0f) o.S *= __builtin_amdgcn_exp2f(o.mb - mxb);
-        o.m = mx;
-        o.mb = mxb;
-    }
+// The scaled logit that references are measured in, and the base-2 exponent of a logit.
+template <typename T> __device__ __forceinline__ float scaled(const PolicyArgs &a, float z) { return z * (sizeof(T) == 4 ? a.inv_temp : a.c); }
+template <typename T> __device__ __forceinline__ float base2(float d) { return sizeof(T) == 4 ? d * kLog2e : d; }
+template <typename T> __device__ __forceinline__ float exponent(const PolicyArgs &a, float z, float ref) {
+    return sizeof(T) == 4 ? (z * a.inv_temp - ref) * kLog2e : __builtin_fmaf(z, a.c, -ref);
 }
 
+// Running maximum and sum of a slice of a row; empty: m = -Inf, ref = 0, S = 0, and so for a slice of -Inf logits alone.
+struct Online {
+    float m, ref, S;
+};
+
 // A NaN logit makes S NaN, and so does +Inf (Inf - Inf): the row's statistics are NaN then.
-template <int N> __device__ __forceinline__ void add(Online &o, const float (&z)[N], float c) {
+template <typename T> __device__ __forceinline__ void add(Online &o, const PolicyArgs &a, uint4 v) {
+    constexpr int N = kVec<T>;
+    float z[N];
+    unpack<T>(v, z);
     float mx = z[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) mx = __builtin_fmaxf(mx, z[i]);
-    grow(o, mx, c);
+    if (mx > o.m) {
+        const float ref = scaled<T>(a, mx);
+        if (o.S != 0.0f) o.S *= __builtin_amdgcn_exp2f(base2<T>(o.ref - ref));
+        o.m = mx;
+        o.ref = ref;
+    }
 #pragma unroll
-    for (int i = 0; i < N; ++i) o.S += __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], c, -o.mb));
+    for (int i = 0; i < N; ++i) o.S += __builtin_amdgcn_exp2f(exponent<T>(a, z[i], o.ref));
 }
 
-__device__ __forceinline__ Online merge(Online a, Online b) {
+template <typename T> __device__ __forceinline__ Online merge(Online a, Online b) {
     if (b.m > a.m) { const Online t = a; a = b; b = t; }
     if (b.S == 0.0f) return a;
-    a.S += b.S * __builtin_amdgcn_exp2f(b.mb - a.mb);
+    a.S += b.S * __builtin_amdgcn_exp2f(base2<T>(b.ref - a.ref));
     return a;
+}
+
+// The workgroup's TH slices in a fixed order: within the wave, then wave by wave.
+template <typename T, int TH> __device__ __forceinline__ Online join(Online o, Online (&red)[TH / 64]) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1)
+        o = merge<T>(o, Online{__shfl_xor(o.m, off, 64), __shfl_xor(o.ref, off, 64), __shfl_xor(o.S, off, 64)});
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = o;
+    __syncthreads();
+    o = red[0];
+#pragma unroll
+    for (int k = 1; k < TH / 64; ++k) o = merge<T>(o, red[k]);
+    return o;
 }
 
 // exp(x) - x - 1 >= 0.  Near zero the difference of close numbers is summed as its series (to x^8 / 8!: 2e-8 of it at 1/2).
@@ -66,108 +87,211 @@ __device__ __forceinline__ bool outside(const PolicyArgs &a, float r, float adv)
     return (adv > 0.0f && r > a.high) || (adv < 0.0f && r < a.low);
 }
 
+// What a row brings besides its logits, asked for before they are summed.
+struct RowInputs {
+    float w, old, adv, ref, zy;
+    int32_t y;
+};
+
+// A number at an address that is the same in every lane, read through the scalar cache: no vector register, and no wait for
+// the vector loads in flight.  Nothing that this kernel writes is read so.
+template <typename T> __device__ __forceinline__ T load_scalar(const T *p) {
+    static_assert(sizeof(T) == 4, "a word");
+    return *(const __attribute__((address_space(4))) T *)reinterpret_cast<uintptr_t>(p);
+}
+
+// An element of a row, by the word that holds it.
+__device__ __forceinline__ float scalar_element(const float *p) { return load_scalar(p); }
+__device__ __forceinline__ float scalar_element(const uint16_t *p) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    const uint32_t w = load_scalar(reinterpret_cast<const uint32_t *>(at & ~(uintptr_t)3));
+    return __uint_as_float(at & 2 ? w & 0xFFFF0000u : w << 16);
+}
+
 __device__ __forceinline__ float weight_of(const PolicyArgs &a, int64_t t) {
-    return a.weights ? a.weights[t] : a.default_weight;
+    return a.weights ? load_scalar(a.weights + t) : a.default_weight;
 }
 
-// lp, log-sum-exp, dL/dlp and r of a row with weight w != 0.
-__device__ __forceinline__ float4 row_stats(const PolicyArgs &a, int64_t t, float w, Online o, float zy) {
+// A number that is the same in every lane, in a scalar register.
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
+// All but the target's logit.
+__device__ __forceinline__ RowInputs row_inputs(const PolicyArgs &a, int64_t t) {
+    RowInputs in;
+    in.zy = __builtin_nanf("");
+    in.y = load_scalar(a.targets + t);
+    in.w = weight_of(a, t);
+    in.old = load_scalar(a.old_logp + t);
+    in.adv = load_scalar(a.adv + t);
+    in.ref = a.ref ? load_scalar(a.ref + t) : 0.0f;
+    return in;
+}
+
+// A target outside [0, V) gives a NaN logit; what is read for it is the row's first one.  (With grad in the logits' memory
+// this is still before the row is written, by this workgroup.)
+template <typename T> __device__ __forceinline__ RowInputs row_inputs(const PolicyArgs &a, int64_t t, const T *row) {
+    RowInputs in = row_inputs(a, t);
+    const bool known = in.y >= 0 && (int64_t)in.y < a.V;
+    const float zy = scalar_element(row + (known ? in.y : 0));
+    if (known) in.zy = zy;
+    return in;
+}
+
+// lp, log-sum-exp, dL/dlp and r of a row.
+template <typename T> __device__ __forceinline__ float4 row_stats(const PolicyArgs &a, const RowInputs &in, Online o) {
     const float log2S = __builtin_amdgcn_logf(o.S);
-    const float lp = (__builtin_fmaf(zy, a.c, -o.mb) - log2S) * kLn2;
-    const float r = expf(lp - a.old_logp[t]), adv = a.adv[t];
-    float slope = outside(a, r, adv) ? 0.0f : -adv * r;
-    if (a.ref) slope -= a.kl * expm1f(a.ref[t] - lp);
-    return make_float4(lp, (o.mb + log2S) * kLn2, w * slope, r);
+    float lp, lse;
+    if (sizeof(T) == 4) {
+        lp = (in.zy * a.inv_temp - o.ref) - log2S * kLn2;
+        lse = o.ref + log2S * kLn2;
+    } else {
+        lp = (__builtin_fmaf(in.zy, a.c, -o.ref) - log2S) * kLn2;
+        lse = (o.ref + log2S) * kLn2;
+    }
+    const float r = expf(lp - in.old);
+    float slope = outside(a, r, in.adv) ? 0.0f : -in.adv * r;
+    if (a.ref) slope -= a.kl * expm1f(in.ref - lp);
+    return make_float4(lp, lse, in.w * slope, r);
 }
 
-// 0 <= y < V, else NaN without a read.
-template <typename T> __device__ __forceinline__ float target_logit(const PolicyArgs &a, const T *row, int32_t y) {
-    return y >= 0 && (int64_t)y < a.V ? to_f32(row[y]) : __builtin_nanf("");
-}
-
-// dL/dz of one vector: f ([j = y] - s 2^(c z - b)).
+// dL/dz of a vector whose first element is j: f [j = y] - fs 2^t.
 template <typename T>
-__device__ __forceinline__ uint4 grad_vec(uint4 v, float c, float b, float fs, float f, int64_t j0, int64_t y) {
-    float z[kVec<T>], g[kVec<T>];
+__device__ __forceinline__ uint4 grad_vec(const PolicyArgs &a, uint4 v, float ref, float fs, float f, int32_t j, int32_t y) {
+    constexpr int N = kVec<T>;
+    float z[N];
     unpack<T>(v, z);
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) {
-        g[i] = -fs * __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], c, -b));
-        if (j0 + i == y) g[i] += f;
+    for (int i = 0; i < N; ++i) z[i] = -fs * __builtin_amdgcn_exp2f(exponent<T>(a, z[i], ref));
+    if ((uint32_t)(y - j) < (uint32_t)N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] += j + i == y ? f : 0.0f;
     }
-    return pack<T>(g);
+    return pack<T>(z);
 }
 
-// The gradient of elements [begin, end) of a row (begin a multiple of the vector), by the threads tid of `step`.
-template <typename T>
-__device__ __forceinline__ void write_grad(const T *row, T *out, int64_t begin, int64_t end, int tid, int step, float c,
-                                           float b, float fs, float f, int64_t y) {
-    for (int64_t j = begin + (int64_t)tid * kVec<T>; j < end; j += (int64_t)step * kVec<T>) {
-        const int n = (int)(end - j < kVec<T> ? end - j : kVec<T>);
-        if (n == kVec<T>) store_vec(out + j, grad_vec<T>(load_vec(row + j), c, b, fs, f, j, y));
-        else store_part(out + j, grad_vec<T>(load_part(row + j, n), c, b, fs, f, j, y), n);
-    }
-}
-
-template <typename T> __device__ __forceinline__ void write_zeros(T *out, int64_t begin, int64_t end, int tid, int step) {
-    for (int64_t j = begin + (int64_t)tid * kVec<T>; j < end; j += (int64_t)step * kVec<T>) {
-        const int n = (int)(end - j < kVec<T> ? end - j : kVec<T>);
-        if (n == kVec<T>) store_vec(out + j, make_uint4(0, 0, 0, 0));
-        else store_part(out + j, make_uint4(0, 0, 0, 0), n);
-    }
-}
-
-// One workgroup per row.  logits and grad may be the same memory: a thread writes the elements that it has read.
-template <typename T, bool GRAD> __global__ __launch_bounds__(kThreads) void policy_rows_kernel(PolicyArgs a) {
+// Vector j of a row of V elements; -Inf, whose exponential is 0, behind its end.
+template <typename T> __device__ __forceinline__ uint4 load_at(const T *row, int32_t V, int32_t j) {
     constexpr int N = kVec<T>;
+    if (V - j >= N) return load_vec(row + j);
+    T e[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) e[i] = j + i < V ? row[j + i] : from_f32<T>(-__builtin_inff());
+    return __builtin_bit_cast(uint4, e);
+}
+
+template <typename T> __device__ __forceinline__ void store_at(T *row, int32_t V, int32_t j, uint4 v) {
+    if (V - j >= kVec<T>) store_vec(row + j, v);
+    else store_part(row + j, v, V - j);
+}
+
+// The gradient of the elements [begin, end) of a row (begin a multiple of the vector), by TH threads.
+template <typename T, int TH>
+__device__ __forceinline__ void write_grad(const PolicyArgs &a, const T *row, T *out, int32_t begin, int32_t end, float ref,
+                                           float fs, float f, int32_t y) {
+    for (int32_t j = begin + (int32_t)threadIdx.x * kVec<T>; j < end; j += TH * kVec<T>)
+        store_at(out, end, j, grad_vec<T>(a, load_at(row, end, j), ref, fs, f, j, y));
+}
+
+template <typename T, int TH> __device__ __forceinline__ void write_zeros(T *out, int32_t begin, int32_t end) {
+    for (int32_t j = begin + (int32_t)threadIdx.x * kVec<T>; j < end; j += TH * kVec<T>) store_at(out, end, j, make_uint4(0, 0, 0, 0));
+}
+
+// Loss alone: a workgroup per row, which is read once.
+template <typename T> __global__ __launch_bounds__(kThreads) void policy_rows_kernel(PolicyArgs a) {
+    constexpr int N = kVec<T>, kStep = kThreads * N;
     const int64_t t = blockIdx.x;
-    const T *row = reinterpret_cast<const T *>(a.logits) + t * a.ld;
-    T *out = GRAD ? reinterpret_cast<T *>(a.grad) + t * a.ldg : nullptr;
     const float w = weight_of(a, t);
     if (w == 0.0f) {
         if (threadIdx.x == 0) reinterpret_cast<float4 *>(a.stats)[t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (GRAD) write_zeros(out, 0, a.V, threadIdx.x, kThreads);
         return;
     }
-    const int32_t y = a.targets[t];
-    const float zy = target_logit(a, row, y);
+    const T *row = reinterpret_cast<const T *>(a.logits) + t * a.ld;
+    const RowInputs in = row_inputs(a, t, row);
     Online o{-__builtin_inff(), 0.0f, 0.0f};
-    const int64_t full = a.V / N;
-    int64_t i = threadIdx.x;
-    for (; i + 3 * kThreads < full; i += 4 * kThreads) {
+    const int64_t V = a.V;
+    int64_t j = (int64_t)threadIdx.x * N;
+    for (; j + 3 * kStep + N <= V; j += 4 * kStep) {
         uint4 v[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v[u] = load_vec(row + (i + u * kThreads) * N);
+        for (int u = 0; u < 4; ++u) v[u] = load_vec(row + j + u * kStep);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            float z[N];
-            unpack<T>(v[u], z);
-            add(o, z, a.c);
-        }
+        for (int u = 0; u < 4; ++u) add<T>(o, a, v[u]);
     }
-    for (; i < full; i += kThreads) {
-        float z[N];
-        unpack<T>(load_vec(row + i * N), z);
-        add(o, z, a.c);
-    }
-    if (threadIdx.x < (unsigned)(a.V - full * N)) {
-        const float z[1] = {to_f32(row[full * N + threadIdx.x])};
-        add(o, z, a.c);
-    }
-    // fixed order: within the wave, then wave by wave
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
-        o = merge(o, Online{__shfl_xor(o.m, off, 64), __shfl_xor(o.mb, off, 64), __shfl_xor(o.S, off, 64)});
+    for (; j < V; j += kStep) add<T>(o, a, load_at(row, (int32_t)V, (int32_t)j));
     __shared__ Online red[kThreads / 64];
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = o;
-    __syncthreads();
-    o = red[0];
-    for (int k = 1; k < kThreads / 64; ++k) o = merge(o, red[k]);
-    const float4 s = row_stats(a, t, w, o, zy);
-    if (threadIdx.x == 0) reinterpret_cast<float4 *>(a.stats)[t] = s;
-    if (GRAD) {
-        const float f = s.z * a.inv_temp;
-        write_grad(row, out, 0, a.V, threadIdx.x, kThreads, a.c, o.mb, f / o.S, f, y);
+    o = join<T, kThreads>(o, red);
+    if (threadIdx.x == 0) reinterpret_cast<float4 *>(a.stats)[t] = row_stats<T>(a, in, o);
+}
+
+// Vector v as it came, after x is known: without this the compiler unpacks all vectors of a row first, or keeps the unpacked
+// ones from the sums to the gradients, in two or four times the registers.
+__device__ __forceinline__ void pin(uint4 &v, float x) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w) : "v"(x)); }
+
+// Loss and gradient.  Workgroups of TH threads walk over the rows in steps of the grid and keep a row's first TH x NV
+// whole vectors in registers, so that most rows are read once; as the gradient of a vector is written, the next row's is
+// asked for in its place.  What does not fit, and a last partial vector, is read again, from the caches.  logits and grad
+// may be the same memory: a row's vectors are read before they are written, and the next row is another one's memory.
+//
+// The row has more than (NV - 1) TH whole vectors (or NV is 0), so that all but the last step's accesses are without a
+// condition: behind a branch the compiler cannot count the accesses in flight, and waits for all of them.
+template <typename T, int TH, int NV> __global__ __launch_bounds__(TH) void policy_grad_kernel(PolicyArgs a) {
+    constexpr int N = kVec<T>, kStep = TH * N, kHeld = kStep * NV, kBytes = TH * 16;
+    const int32_t V = (int32_t)a.V, j0 = threadIdx.x * N, full = V / N * N, rest = full < kHeld ? full : kHeld;
+    const uint32_t lane = threadIdx.x * 16;             // bytes from a step's begin, which is the same in every lane
+    const bool last = j0 < full - (NV - 1) * kStep;     // whether the last step has a vector of this thread
+    const T *logits = reinterpret_cast<const T *>(a.logits);
+    T *grad = reinterpret_cast<T *>(a.grad);
+    __shared__ Online red[2][TH / 64];
+    int half = 0;
+    uint4 buf[NV > 0 ? NV : 1];
+    // the next row with a weight from t on; those without get their zeros
+    const auto seek = [&](int64_t t) {
+        for (; t < a.T; t += gridDim.x) {
+            if (weight_of(a, t) != 0.0f) break;
+            if (threadIdx.x == 0) reinterpret_cast<float4 *>(a.stats)[t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            write_zeros<T, TH>(grad + t * a.ldg, 0, V);
+        }
+        return t;
+    };
+    int64_t t = seek(blockIdx.x);
+    if (t >= a.T) return;
+    const T *row = logits + t * a.ld;
+    RowInputs in = row_inputs(a, t, row);
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+        if (v < NV - 1 || last) buf[v] = load_vec(reinterpret_cast<const char *>(row) + v * kBytes + lane);
+    while (true) {
+        const int32_t y = in.y;
+        Online o{-__builtin_inff(), 0.0f, 0.0f};
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            pin(buf[v], o.S);
+            if (v < NV - 1 || last) add<T>(o, a, buf[v]);
+        }
+        for (int32_t j = j0 + rest; j < V; j += kStep) add<T>(o, a, load_at(row, V, j));
+        o = join<T, TH>(o, red[half]);
+        half ^= 1;                                      // the other half is written before this one is again
+        o.ref = uniform(o.ref);
+        const float4 s = row_stats<T>(a, in, o);
+        if (threadIdx.x == 0) reinterpret_cast<float4 *>(a.stats)[t] = s;
+        const float f = uniform(s.z * a.inv_temp), fs = uniform(f / o.S);
+        T *out = grad + t * a.ldg;
+        const int64_t next = seek(t + gridDim.x);
+        const bool more = next < a.T;
+        const T *ahead = logits + (more ? next : t) * a.ld;      // no further row: this one's first vectors once more
+        in = row_inputs(a, more ? next : t, ahead);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            pin(buf[v], o.ref);
+            if (v < NV - 1 || last) {
+                store_vec_once(reinterpret_cast<char *>(out) + v * kBytes + lane, grad_vec<T>(a, buf[v], o.ref, fs, f, j0 + v * kStep, y));
+                buf[v] = load_vec(reinterpret_cast<const char *>(ahead) + v * kBytes + lane);
+            }
+        }
+        write_grad<T, TH>(a, row, out, rest, V, o.ref, fs, f, y);
+        if (!more) return;
+        t = next;
+        row = ahead;
     }
 }
 
@@ -178,33 +302,33 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_backwar
     T *out = reinterpret_cast<T *>(a.grad) + t * a.ldg;
     const float lse = a.stats[4 * t + 1], slope = a.stats[4 * t + 2];
     if (slope == 0.0f) {                                   // no weight, or clipped without a KL term: nothing to read
-        write_zeros(out, begin, end, threadIdx.x, kThreads);
+        write_zeros<T, kThreads>(out, (int32_t)begin, (int32_t)end);
         return;
     }
     const float f = slope * a.inv_temp * (a.grad_loss ? a.grad_loss[0] : 1.0f);
-    // lse log2(e) as a rounded number and what it leaves, which joins the factor
-    const float b = lse * kLog2e;
-    const float rest = __builtin_fmaf(lse, kLog2e, -b) + lse * 1.925963033500e-8f;
-    write_grad(row, out, begin, end, threadIdx.x, kThreads, a.c, b, f * __builtin_amdgcn_exp2f(-rest), f, a.targets[t]);
+    float ref = lse, fs = f;
+    if (sizeof(T) == 2) {
+        // lse log2(e) as a rounded number and what it leaves, which joins the factor
+        ref = lse * kLog2e;
+        fs *= __builtin_amdgcn_exp2f(-(__builtin_fmaf(lse, kLog2e, -ref) + lse * 1.925963033500e-8f));
+    }
+    write_grad<T, kThreads>(a, row, out, (int32_t)begin, (int32_t)end, ref, fs, f, a.targets[t]);
 }
 
 constexpr int kSumThreads = 1024;
 
-// loss = sum w (surrogate + kl KL), sum w surrogate, sum w KL, sum w [outside]; FP64, fixed order.
-__global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(PolicyArgs a) {
-    double s[3] = {0.0, 0.0, 0.0};
-    for (int64_t t = threadIdx.x; t < a.T; t += kSumThreads) {
-        const float w = weight_of(a, t);
-        if (w == 0.0f) continue;
-        const float4 st = reinterpret_cast<const float4 *>(a.stats)[t];
-        const float adv = a.adv[t], r = st.w;
-        const float held = r < a.low ? a.low : (r > a.high ? a.high : r);
-        const float x = r * adv, y = held * adv;
-        s[0] += (double)w * -(double)(y < x ? y : x);
-        if (a.ref) s[1] += (double)w * (double)kl_term(a.ref[t] - st.x);
-        s[2] += outside(a, r, adv) ? (double)w : 0.0;
-    }
-    __shared__ double red[3][kSumThreads / 64];
+// Adds w surrogate, w KL and w [outside] of a row.
+__device__ __forceinline__ void add_terms(const PolicyArgs &a, float w, float adv, float ref, float lp, float r, double (&s)[3]) {
+    const float held = r < a.low ? a.low : (r > a.high ? a.high : r);
+    const float x = r * adv, y = held * adv;
+    s[0] += (double)w * -(double)(y < x ? y : x);
+    if (a.ref) s[1] += (double)w * (double)kl_term(ref - lp);
+    s[2] += outside(a, r, adv) ? (double)w : 0.0;
+}
+
+// loss = sum w (surrogate + kl KL), sum w surrogate, sum w KL, sum w [outside]; FP64, the threads' sums in a fixed order.
+template <int TH> __device__ __forceinline__ void write_loss(const PolicyArgs &a, double (&s)[3]) {
+    __shared__ double red[3][TH / 64];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
 #pragma unroll
@@ -215,7 +339,7 @@ __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(PolicyArgs a) {
     if (threadIdx.x == 0) {
         for (int k = 0; k < 3; ++k) {
             s[k] = 0.0;
-            for (int i = 0; i < kSumThreads / 64; ++i) s[k] += red[k][i];
+            for (int i = 0; i < TH / 64; ++i) s[k] += red[k][i];
         }
         a.loss[0] = (float)(s[0] + (double)a.kl * s[1]);
         a.loss[1] = (float)s[0];
@@ -224,15 +348,125 @@ __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(PolicyArgs a) {
     }
 }
 
+__global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(PolicyArgs a) {
+    double s[3] = {0.0, 0.0, 0.0};
+    for (int64_t t = threadIdx.x; t < a.T; t += kSumThreads) {
+        const float w = a.weights ? a.weights[t] : a.default_weight;
+        if (w == 0.0f) continue;
+        const float4 st = reinterpret_cast<const float4 *>(a.stats)[t];
+        add_terms(a, w, a.adv[t], a.ref ? a.ref[t] : 0.0f, st.x, st.w, s);
+    }
+    write_loss<kSumThreads>(a, s);
+}
+
+// ------------------------------------------------------------------ few rows: several workgroups to a row
+
+// Statistics of slice blockIdx.y of row blockIdx.x, and the target's logit where it is in the slice: the gradient may be
+// written over the logits by then.
+template <typename T> __global__ __launch_bounds__(kThreads) void policy_part_kernel(PolicyArgs a, int32_t slice) {
+    const int64_t t = blockIdx.x;
+    if (weight_of(a, t) == 0.0f) return;
+    const int32_t V = (int32_t)a.V, begin = (int32_t)blockIdx.y * slice, end = V - begin < slice ? V : begin + slice;
+    const T *row = reinterpret_cast<const T *>(a.logits) + t * a.ld;
+    Online o{-__builtin_inff(), 0.0f, 0.0f};
+#pragma unroll 4
+    for (int32_t j = begin + (int32_t)threadIdx.x * kVec<T>; j < end; j += kThreads * kVec<T>) add<T>(o, a, load_at(row, end, j));
+    __shared__ Online red[kThreads / 64];
+    o = join<T, kThreads>(o, red);
+    if (threadIdx.x == 0) {
+        const int32_t y = a.targets[t];
+        a.parts[t * gridDim.y + blockIdx.y] = make_float4(o.m, o.ref, o.S, y >= begin && y < end ? to_f32(row[y]) : __builtin_nanf(""));
+    }
+}
+
+// A row's slices in their order, and its target's logit.
+template <typename T>
+__device__ __forceinline__ Online merge_parts(const PolicyArgs &a, int64_t t, int32_t slice, int slices, RowInputs &in) {
+    Online o{-__builtin_inff(), 0.0f, 0.0f};
+    for (int k = 0; k < slices; ++k) {
+        const float4 p = a.parts[t * slices + k];
+        o = merge<T>(o, Online{p.x, p.y, p.z});
+        if (in.y >= 0 && in.y / slice == k) in.zy = p.w;      // NaN for a target behind the row's end
+    }
+    return o;
+}
+
+// Workgroup 0: every row's statistics, a thread each, and the loss.  Workgroup 1 + t slices + k: the gradient of slice k of
+// row t.
+template <typename T> __global__ __launch_bounds__(kThreads) void policy_finish_kernel(PolicyArgs a, int32_t slice, int slices) {
+    if (blockIdx.x == 0) {
+        double s[3] = {0.0, 0.0, 0.0};
+        for (int64_t t = threadIdx.x; t < a.T; t += kThreads) {
+            const float w = a.weights ? a.weights[t] : a.default_weight;
+            float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (w != 0.0f) {
+                RowInputs in = {w, a.old_logp[t], a.adv[t], a.ref ? a.ref[t] : 0.0f, __builtin_nanf(""), a.targets[t]};
+                const Online o = merge_parts<T>(a, t, slice, slices, in);
+                st = row_stats<T>(a, in, o);
+                add_terms(a, w, in.adv, in.ref, st.x, st.w, s);
+            }
+            reinterpret_cast<float4 *>(a.stats)[t] = st;
+        }
+        write_loss<kThreads>(a, s);
+        return;
+    }
+    const int64_t t = (blockIdx.x - 1) / slices;
+    const int32_t V = (int32_t)a.V, begin = (int32_t)((blockIdx.x - 1) % slices) * slice, end = V - begin < slice ? V : begin + slice;
+    const T *row = reinterpret_cast<const T *>(a.logits) + t * a.ld;
+    T *out = reinterpret_cast<T *>(a.grad) + t * a.ldg;
+    if (weight_of(a, t) == 0.0f) {
+        write_zeros<T, kThreads>(out, begin, end);
+        return;
+    }
+    RowInputs in = row_inputs(a, t);
+    const Online o = merge_parts<T>(a, t, slice, slices, in);
+    const float f = row_stats<T>(a, in, o).z * a.inv_temp;
+    write_grad<T, kThreads>(a, row, out, begin, end, o.ref, f / o.S, f, in.y);
+}
+
+}  // namespace
+
+namespace {
+
+// Workgroups of 256 threads for rows of up to 4096 bytes a wave, else of 1024, with as many vectors as the row has and the
+// registers hold (128 a thread).  They are persistent: as many as the card's 256 compute units hold at once.
+template <typename T, int TH, int NV> void launch_grad_of(const PolicyArgs &a, int64_t steps, hipStream_t stream) {
+    if (steps == NV) {
+        const int64_t most = TH == 256 ? 4 * 256 : 256;
+        hipLaunchKernelGGL((policy_grad_kernel<T, TH, NV>), dim3((unsigned)(a.T < most ? a.T : most)), dim3(TH), 0, stream, a);
+    } else if constexpr (NV > 0) {
+        launch_grad_of<T, TH, NV - 1>(a, steps, stream);
+    }
+}
+
+template <typename T> void launch_grad(const PolicyArgs &a, hipStream_t stream) {
+    const int64_t full = a.V / kVec<T>, steps = (full + 1023) / 1024;
+    if (full <= 4 * 256) launch_grad_of<T, 256, 4>(a, (full + 255) / 256, stream);
+    else launch_grad_of<T, 1024, kMaxHeld>(a, steps < kMaxHeld ? steps : kMaxHeld, stream);
+}
+
 }  // namespace
 
 hipError_t launch_policy_loss(const PolicyArgs &a, bool bf16, hipStream_t stream) {
     const dim3 grid((unsigned)a.T), block(kThreads);
+    const PolicyPlan plan = policy_plan(a.T, a.V, bf16);
+    if (plan.slices > 1) {
+        const int32_t slice = (int32_t)plan.slice;
+        const int slices = (int)plan.slices;
+        const dim3 parts((unsigned)a.T, (unsigned)slices), finish(a.grad ? (unsigned)(1 + a.T * slices) : 1);
+        if (bf16) {
+            hipLaunchKernelGGL(policy_part_kernel<uint16_t>, parts, block, 0, stream, a, slice);
+            hipLaunchKernelGGL(policy_finish_kernel<uint16_t>, finish, block, 0, stream, a, slice, slices);
+        } else {
+            hipLaunchKernelGGL(policy_part_kernel<float>, parts, block, 0, stream, a, slice);
+            hipLaunchKernelGGL(policy_finish_kernel<float>, finish, block, 0, stream, a, slice, slices);
+        }
+        return hipGetLastError();
+    }
     if (a.T > 0) {
-        if (bf16 && a.grad) hipLaunchKernelGGL((policy_rows_kernel<uint16_t, true>), grid, block, 0, stream, a);
-        else if (bf16) hipLaunchKernelGGL((policy_rows_kernel<uint16_t, false>), grid, block, 0, stream, a);
-        else if (a.grad) hipLaunchKernelGGL((policy_rows_kernel<float, true>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((policy_rows_kernel<float, false>), grid, block, 0, stream, a);
+        if (a.grad) bf16 ? launch_grad<uint16_t>(a, stream) : launch_grad<float>(a, stream);
+        else if (bf16) hipLaunchKernelGGL(policy_rows_kernel<uint16_t>, grid, block, 0, stream, a);
+        else hipLaunchKernelGGL(policy_rows_kernel<float>, grid, block, 0, stream, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -74,7 +74,8 @@ SIGNATURES = {
     "reqat_quantize_mxfp4_rht": (_INT, [_VP, _I64, _I64, _I64, ctypes.c_uint32, _VP, _VP, _VP]),
     "reqat_fakequant_mxfp4_rht": (_INT, [_VP, _I64, _I64, _I64, ctypes.c_uint32, _VP, _I64, _VP]),
     "reqat_policy_loss": (_INT, [_VP, _INT, _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP, _F32, _F32, _F32, _F32, _VP, _VP, _VP,
-                                 _I64, _VP]),
+                                 _I64, _VP, _VP]),
+    "reqat_policy_loss_workspace_bytes": (ctypes.c_size_t, [_INT, _I64, _I64]),
     "reqat_policy_loss_backward": (_INT, [_VP, _INT, _I64, _I64, _I64, _VP, _VP, _F32, _VP, _VP, _I64, _VP]),
     "reqat_layer_norm": (_INT, [_VP, _INT, _I64, _I64, _I64, _VP, _VP, _INT, _F32, _INT, _VP, _I64, _VP, _VP]),
     "reqat_layer_norm_workspace_bytes": (ctypes.c_size_t, [_INT, _I64, _I64, _INT]),
@@ -225,9 +226,13 @@ def reqat_fakequant_mxfp4_rht(x, rows, cols, ldx, signs, y, ldy, stream):
 
 
 def reqat_policy_loss(logits, dtype, T, V, ld, targets, old_logp, advantages, ref_logp, weights, clip_low, clip_high,
-                      kl_coef, temperature, stats, loss, grad, ldg, stream):
+                      kl_coef, temperature, stats, loss, grad, ldg, workspace, stream):
     return load().reqat_policy_loss(logits, dtype, T, V, ld, targets, old_logp, advantages, ref_logp, weights, clip_low,
-                                    clip_high, kl_coef, temperature, stats, loss, grad, ldg, stream)
+                                    clip_high, kl_coef, temperature, stats, loss, grad, ldg, workspace, stream)
+
+
+def reqat_policy_loss_workspace_bytes(dtype, T, V) -> int:
+    return load().reqat_policy_loss_workspace_bytes(dtype, T, V)
 
 
 def reqat_policy_loss_backward(logits, dtype, T, V, ld, targets, stats, temperature, grad_loss, grad, ldg, stream):
@@ -1165,12 +1170,13 @@ def _policy_loss(logits, targets, old_logp, advantages, ref_logp, weights, clip_
     ldg = 0
     if grad:
         out, ldg = _float_out(out, T, V, logits.dtype, dev, "out")
-    stats = torch.empty((T, 4), dtype=torch.float32, device=dev)
-    loss = torch.empty(4, dtype=torch.float32, device=dev)
     _require_cuda(logits, "logits")
+    # one allocation: statistics, loss and workspace
+    held = torch.empty(4 * T + 4 + reqat_policy_loss_workspace_bytes(dt, T, V) // 4, dtype=torch.float32, device=dev)
+    stats, loss = held[:4 * T].view(T, 4), held[4 * T:4 * T + 4]
     _call(reqat_policy_loss, dev, logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), old_logp.data_ptr(),
           advantages.data_ptr(), _ptr(ref_logp), _ptr(weights), clip_low, clip_high, kl_coef, temperature, stats.data_ptr(),
-          loss.data_ptr(), _ptr(out) if grad else None, ldg)
+          loss.data_ptr(), _ptr(out) if grad else None, ldg, held.data_ptr() + 16 * T + 16)
     return loss, stats, out
 
 

@@ -224,7 +224,11 @@ def test_backward_from_statistics(T, V, dtype):
                                     kl_coef=0.05, temperature=0.7)
     both = reqat.policy_loss_grad(c["logits"], c["targets"], c["old"], c["adv"], ref_logp=c["ref"], weights=c["weights"],
                                   kl_coef=0.05, temperature=0.7)
-    assert torch.equal(loss, both[0]) and torch.equal(stats, both[1])
+    # two workgroup sizes add the same terms in two orders: each is within its bound
+    d = _bounds(c, 0.7)
+    assert torch.all((stats[:, :2] - both[1][:, :2]).abs() <= 2 * d + 2 * ref.EPS32 * stats[:, :2].abs())
+    assert torch.all((stats[:, 3] - both[1][:, 3]).abs() <= stats[:, 3] * (4 * d + 16 * ref.EPS32))
+    assert torch.allclose(loss, both[0], rtol=1e-4, atol=1e-6)
     up = torch.tensor([3.0], device=DEV)
     grad = reqat.policy_loss_backward(c["logits"], c["targets"], stats, temperature=0.7, grad_loss=up)
     lse, slope = stats[:, 1:2].double(), stats[:, 2:3].double()

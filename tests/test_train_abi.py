@@ -29,11 +29,11 @@ def refused(call, base, want, **change):
 
 def test_policy_loss():
     base = dict(logits=P, dtype=BF16, T=4, V=100, ld=104, targets=P, old=P, adv=P, ref=P, weights=None, low=0.2, high=0.2,
-                kl=0.1, temp=1.0, stats=P, loss=P, grad=None, ldg=0, stream=None)
+                kl=0.1, temp=1.0, stats=P, loss=P, grad=None, ldg=0, ws=P, stream=None)
     no = lambda want, **c: refused(reqat.reqat_policy_loss, base, want, **c)
     no(ENUM, dtype=2)
     no(ENUM, dtype=-1)
-    for c in (dict(T=-1), dict(T=(1 << 22) + 1), dict(V=0), dict(V=-3), dict(V=1 << 31, ld=1 << 31), dict(ld=99),
+    for c in (dict(T=-1), dict(T=(1 << 22) + 1), dict(V=0), dict(V=-3), dict(V=(1 << 30) + 1, ld=1 << 31), dict(ld=99),
               dict(ld=1 << 62), dict(grad=2 * P, ldg=99), dict(grad=2 * P, ldg=1 << 62)):
         no(SHAPE, **c)
     for name in ("logits", "targets", "old", "adv", "ref", "stats", "loss"):
@@ -42,6 +42,12 @@ def test_policy_loss():
                       ("loss", 2)):
         no(ALIGN, **{name: P + off})
     no(ALIGN, dtype=F32, logits=P + 2)
+    no(ALIGN, ws=P + 4)
+    no(NULL, V=100000, ld=100000, ws=None)
+    assert reqat.reqat_policy_loss_workspace_bytes(BF16, 4, 100) == 0
+    assert reqat.reqat_policy_loss_workspace_bytes(BF16, 4, 100000) >= 4 * 16
+    assert reqat.reqat_policy_loss_workspace_bytes(BF16, 100000, 100000) == 0
+    assert reqat.reqat_policy_loss_workspace_bytes(5, 4, 100000) == reqat.reqat_policy_loss_workspace_bytes(F32, -1, 9) == 0
     no(ALIGN, grad=2 * P + 1, ldg=104)
     for c in (dict(low=-0.1), dict(low=1.5), dict(high=-0.1), dict(low=math.nan), dict(high=math.nan), dict(temp=0.0),
               dict(temp=-1.0), dict(temp=math.inf), dict(temp=math.nan), dict(grad=P + 2, ldg=104), dict(grad=P, ldg=100)):
