@@ -514,24 +514,26 @@ size_t reqat_layer_norm_workspace_bytes(reqat_dtype dtype, int64_t rows, int64_t
  * Embedding lookup: out[t] = scale * table[ids[t]], rounded once (exact for scale 1);
  * an id outside [0, V) is padding and gives a row of zeros.
  *   ids [T] int32, T at most 2^22; table [V][ld_table], V at most 2^23; out [T][ldo] of
- *   dtype, D columns, at most 2^20; out must not overlap table (REQAT_E_UNSUPPORTED).
+ *   dtype, D columns, at most 2^20 and T D at most 2^37; out must not overlap table
+ *   (REQAT_E_UNSUPPORTED).
  */
 reqat_status reqat_embedding(const int32_t *ids, int64_t T, const void *table, reqat_dtype dtype, int64_t V, int64_t D,
                              int64_t ld_table, float scale, void *out, int64_t ldo, void *stream);
 
 /*
- * Its gradient: dtable[v] = scale * (sum of dy[t] over the t with ids[t] == v, in
- * rising order of t within pieces of 64), added to what dtable holds when accumulate != 0
+ * Its gradient: dtable[v] = scale * (sum of dy[t] over the t with ids[t] == v, in an
+ * order that the ids alone decide), added to what dtable holds when accumulate != 0
  * (rows without a token are not touched then), else written, zeros included; summed in
  * FP32 and rounded once to table_dtype.  Padding has no gradient.
  *   dy [T][lddy] of dtype; dtable [V][ld_table] of table_dtype, no overlap with dy;
- *   workspace: reqat_embedding_workspace_bytes(T, V, D) bytes, 16-byte aligned.
+ *   workspace: reqat_embedding_workspace_bytes(T, V, D) bytes, 16-byte aligned (may be
+ *     NULL when that is 0).
  */
 reqat_status reqat_embedding_backward(const void *dy, reqat_dtype dtype, int64_t lddy, const int32_t *ids, int64_t T, int64_t V,
                                       int64_t D, float scale, void *dtable, reqat_dtype table_dtype, int64_t ld_table,
                                       int accumulate, void *workspace, void *stream);
 
-/* Bytes of workspace of reqat_embedding_backward (0 on bad arguments); never falls as a size grows. */
+/* Bytes of workspace of reqat_embedding_backward (0: none; 0 on bad arguments); never falls as a size grows. */
 size_t reqat_embedding_workspace_bytes(int64_t T, int64_t V, int64_t D);
 
 /*

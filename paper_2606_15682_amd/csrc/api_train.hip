@@ -155,7 +155,7 @@ reqat_status reqat_layer_norm_backward(const void *dy, int64_t lddy, const void 
 }
 
 static reqat_status check_embedding(int64_t T, int64_t V, int64_t D) {
-    return T < 0 || T > kMaxTokens || V < 0 || V > kMaxVocab || D <= 0 || D > (1 << 20) ? REQAT_E_SHAPE : REQAT_OK;
+    return T < 0 || T > kMaxTokens || V < 0 || V > kMaxVocab || D <= 0 || D > (1 << 20) || T > (int64_t(1) << 37) / D ? REQAT_E_SHAPE : REQAT_OK;
 }
 
 reqat_status reqat_embedding(const int32_t *ids, int64_t T, const void *table, reqat_dtype dtype, int64_t V, int64_t D,
@@ -181,16 +181,17 @@ reqat_status reqat_embedding_backward(const void *dy, reqat_dtype dtype, int64_t
     if (!dtype_ok(dtype) || !dtype_ok(table_dtype)) return REQAT_E_ENUM;
     if (check_embedding(T, V, D) != REQAT_OK || lddy < D || ld_table < D || !span_ok(T, lddy) || !span_ok(V, ld_table)) return REQAT_E_SHAPE;
     if (V == 0 || (T == 0 && accumulate)) return REQAT_OK;
-    if (!dtable || !workspace || (T > 0 && (!dy || !ids))) return REQAT_E_NULL;
+    if (!dtable || (T > 0 && (!dy || !ids)) || (!workspace && embedding_workspace_bytes(T, V, D) > 0)) return REQAT_E_NULL;
     const int64_t e = size_of(dtype), g = size_of(table_dtype);
     if (!aligned(dy, e) || !aligned(ids, 4) || !aligned(dtable, g) || !aligned(workspace, 16)) return REQAT_E_ALIGN;
     if (overlap({dy, T, D, lddy, e}, {dtable, V, D, ld_table, g})) return REQAT_E_UNSUPPORTED;
     EmbedGradArgs a = {};
     a.dy = dy; a.dtable = dtable;
-    a.row_start = reinterpret_cast<int32_t *>(workspace);
-    a.order = a.row_start + V + 1;
-    a.sorted = a.order + T;
-    a.partials = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(workspace) + embedding_workspace_head(T, V));
+    if (workspace) {
+        a.valid = reinterpret_cast<int32_t *>(workspace);
+        a.places = reinterpret_cast<int4 *>(reinterpret_cast<uint8_t *>(workspace) + 16);
+        a.partials = reinterpret_cast<float *>(a.places + T);
+    }
     a.T = T; a.V = V; a.D = D; a.ld_dy = lddy; a.ld_table = ld_table;
     a.scale = scale; a.accumulate = accumulate != 0;
     return launch_embedding_backward(a, ids, dtype == REQAT_DT_BF16, table_dtype == REQAT_DT_BF16,

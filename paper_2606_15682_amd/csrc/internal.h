@@ -136,7 +136,7 @@ struct NormArgs {
 hipError_t launch_norm(const NormArgs &a, bool bf16, bool backward, hipStream_t stream);
 
 // Embedding (embedding.hip).
-constexpr int kEmbedPiece = 64;            // tokens of one id that one workgroup adds up
+constexpr int kEmbedPiece = 16;            // sorted tokens whose rows one wave adds up
 struct EmbedArgs {
     const int32_t *ids;
     const void *table;
@@ -148,14 +148,14 @@ hipError_t launch_embedding(const EmbedArgs &a, bool bf16, hipStream_t stream);
 struct EmbedGradArgs {
     const void *dy;
     void *dtable;
-    int32_t *row_start, *order, *sorted;   // workspace: [V + 1], [T], [T]
+    int32_t *valid;                        // workspace (null where none is needed)
+    int4 *places;
     float *partials;
     int64_t T, V, D, ld_dy, ld_table;
     float scale;
     bool accumulate;
 };
 size_t embedding_workspace_bytes(int64_t T, int64_t V, int64_t D);
-size_t embedding_workspace_head(int64_t T, int64_t V);          // bytes before the partial sums
 hipError_t launch_embedding_backward(const EmbedGradArgs &a, const int32_t *ids, bool bf16, bool table_bf16, hipStream_t stream);
 
 // AdamW (adamw.hip).

@@ -13,6 +13,7 @@ marshals arguments.  It raises at load time when the library is missing.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import os
@@ -281,8 +282,10 @@ class AdamwHyper(ctypes.Structure):
 
 
 def reqat_adamw_step(tensors, count, p_dtype, g_dtype, state_bits, hyper, grad_scale, coef, stream):
-    """tensors: an array of AdamwTensor (or None), hyper: an AdamwHyper (or None)."""
-    return load().reqat_adamw_step(_cache_ref(tensors), count, p_dtype, g_dtype, state_bits, _cache_ref(hyper), grad_scale,
+    """tensors: an array of AdamwTensor, or its 8 words a tensor in an array.array (or None), hyper: an AdamwHyper (or
+    None)."""
+    at = tensors.buffer_info()[0] if isinstance(tensors, array.array) else _cache_ref(tensors)
+    return load().reqat_adamw_step(at, count, p_dtype, g_dtype, state_bits, _cache_ref(hyper), grad_scale,
                                    coef, stream)
 
 
@@ -1117,21 +1120,27 @@ class SemLoss(torch.autograd.Function):
 
 def _call(fn, device, *args):
     """The C call with the device current, on its current stream."""
-    if device.index is None or device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream(device)), fn.__name__)
+    current = torch.cuda.current_device()
+    if device.index is None or device.index == current:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(current))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, _stream(device)), fn.__name__)
+            st = fn(*args, _stream(device))
+    _check(st, fn.__name__)
+
+
+_FLOATS = {torch.bfloat16: DT_BF16, torch.float32: DT_F32}
 
 
 def _float_rows(x, name):
     """Rows, columns, row stride and C dtype of a 2-D bfloat16 or float32 tensor with contiguous rows."""
-    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32):
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in _FLOATS:
         raise TypeError("%s must be a 2-D bfloat16 or float32 tensor" % name)
     rows, cols = x.shape
-    if cols > 1 and x.stride(1) != 1 or rows > 1 and x.stride(0) < cols:
+    ld, one = x.stride()
+    if cols > 1 and one != 1 or rows > 1 and ld < cols:
         raise ValueError("%s must have contiguous rows that do not overlap" % name)
-    return rows, cols, x.stride(0) if rows > 1 else max(cols, 1), _dtype_arg(x.dtype)
+    return rows, cols, ld if rows > 1 else max(cols, 1), _FLOATS[x.dtype]
 
 
 def _float_out(t, rows, cols, dtype, device, name):
@@ -1145,13 +1154,30 @@ def _float_out(t, rows, cols, dtype, device, name):
 
 
 def _vector(t, n, device, name, dtypes=(torch.float32,)):
-    """A contiguous vector of n numbers."""
+    """A contiguous vector of n numbers (the whole check first: small calls are short)."""
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == (n,) and t.device == device and t.is_contiguous():
+        return t
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
         raise TypeError("%s must be a tensor of %s" % (name, " or ".join(str(d) for d in dtypes)))
     if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         raise ValueError("%s must be contiguous, of shape (%d,), got %s" % (name, n, tuple(t.shape)))
     _same_device(t, device, name)
     return t
+
+
+@functools.lru_cache(maxsize=1024)
+def _policy_workspace(dtype, T, V) -> int:
+    return reqat_policy_loss_workspace_bytes(dtype, T, V)
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_workspace(dtype, rows, cols, bias) -> int:
+    return reqat_layer_norm_workspace_bytes(dtype, rows, cols, bias)
+
+
+@functools.lru_cache(maxsize=1024)
+def _embedding_workspace(T, V, D) -> int:
+    return reqat_embedding_workspace_bytes(T, V, D)
 
 
 def _policy_loss(logits, targets, old_logp, advantages, ref_logp, weights, clip_low, clip_high, kl_coef, temperature, grad,
@@ -1171,12 +1197,13 @@ def _policy_loss(logits, targets, old_logp, advantages, ref_logp, weights, clip_
     if grad:
         out, ldg = _float_out(out, T, V, logits.dtype, dev, "out")
     _require_cuda(logits, "logits")
-    # one allocation: statistics, loss and workspace
-    held = torch.empty(4 * T + 4 + reqat_policy_loss_workspace_bytes(dt, T, V) // 4, dtype=torch.float32, device=dev)
-    stats, loss = held[:4 * T].view(T, 4), held[4 * T:4 * T + 4]
+    stats = torch.empty((T, 4), dtype=torch.float32, device=dev)
+    loss = torch.empty(4, dtype=torch.float32, device=dev)
+    need = _policy_workspace(dt, T, V)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _call(reqat_policy_loss, dev, logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), old_logp.data_ptr(),
           advantages.data_ptr(), _ptr(ref_logp), _ptr(weights), clip_low, clip_high, kl_coef, temperature, stats.data_ptr(),
-          loss.data_ptr(), _ptr(out) if grad else None, ldg, held.data_ptr() + 16 * T + 16)
+          loss.data_ptr(), _ptr(out) if grad else None, ldg, _ptr(ws))
     return loss, stats, out
 
 
@@ -1218,9 +1245,6 @@ def policy_loss_backward(logits, targets, stats, temperature=1.0, grad_loss=None
     return out
 
 
-_FLOATS = (torch.bfloat16, torch.float32)
-
-
 def layer_norm(x, weight, bias=None, eps=1e-6, center=True, out=None):
     """Layer norm of the rows of x (bfloat16 or float32 [rows, cols], rows may be strided), or with center=False the
     root-mean-square norm, with weight and bias [cols] (bfloat16 or float32, both alike).  Returns (y like x; stats
@@ -1251,7 +1275,7 @@ def layer_norm_backward(dy, x, weight, stats, center=True, bias=False, out=None,
     _vector(weight, cols, dev, "weight", _FLOATS)
     _index_arg(stats, (rows, 2), torch.float32, dev, "stats")
     dx, lddx = _float_out(out, rows, cols, x.dtype, dev, "out")
-    need = reqat_layer_norm_workspace_bytes(dt, rows, cols, 1 if bias else 0)
+    need = _norm_workspace(dt, rows, cols, 1 if bias else 0)
     if ws is not None:
         _workspace_arg(ws, need, dev)
     _require_cuda(x, "x")
@@ -1293,14 +1317,14 @@ def embedding_backward(dy, ids, rows, scale=1.0, out=None, accumulate=False, out
         out_dtype = dy.dtype if out is None else out.dtype
     out_dt = _dtype_arg(out_dtype)
     out, ld = _float_out(out, rows, D, out_dtype, dev, "out")
-    need = reqat_embedding_workspace_bytes(T, rows, D)
+    need = _embedding_workspace(T, rows, D)
     if ws is not None:
         _workspace_arg(ws, need, dev)
     _require_cuda(dy, "dy")
-    if ws is None:
+    if ws is None and need > 0:
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
     _call(reqat_embedding_backward, dev, dy.data_ptr(), dt, lddy, ids.data_ptr(), T, rows, D, scale, out.data_ptr(), out_dt,
-          ld, 1 if accumulate else 0, ws.data_ptr())
+          ld, 1 if accumulate else 0, _ptr(ws))
     return out
 
 
@@ -1333,17 +1357,8 @@ class AdamW:
         if not isinstance(first, torch.Tensor) or first.dtype not in _FLOATS:
             raise TypeError("parameters must be bfloat16 or float32 tensors")
         self.device, self.dtype, self.state_bits = first.device, first.dtype, state_bits
-        spans = []
-        for i, p in enumerate(self.params):
-            self._tensor_arg(p, p, (self.dtype,), "params[%d]" % i)
-            spans.append((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()))
-            c = None if self.copies is None else self.copies[i]
-            if c is not None:
-                self._tensor_arg(c, p, (torch.bfloat16,), "copies[%d]" % i)
-                spans.append((c.data_ptr(), c.data_ptr() + c.numel() * 2))
-        spans = sorted(s for s in spans if s[1] > s[0])
-        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
-            raise ValueError("parameters and copies must not overlap")
+        self._shapes = [p.shape if isinstance(p, torch.Tensor) else None for p in self.params]
+        self._adopt()
         self.lr, self.betas, self.eps, self.weight_decay, self.steps = lr, betas, eps, weight_decay, 0
         self.offsets, size = [], 0
         for p in self.params:
@@ -1354,17 +1369,50 @@ class AdamW:
         self.m_scale = self.v_scale = None
         if state_bits == 8:
             self.m_scale, self.v_scale = (torch.zeros(size // 128, dtype=torch.float32, device=self.device) for _ in range(2))
+        # an array of reqat_adamw_tensor; a step fills in the addresses of parameters, copies and gradients
+        self._sizes = array.array("q", [p.numel() for p in self.params])
+        self._tensors = array.array("q", bytes(64 * len(self.params)))
+        base = [t if t is None else t.data_ptr() for t in (self.m, self.v, self.m_scale, self.v_scale)]
+        for i, at in enumerate(self.offsets):
+            self._tensors[8 * i + 2] = base[0] + at * self.m.element_size()
+            self._tensors[8 * i + 3] = base[1] + at * self.v.element_size()
+            if state_bits == 8:
+                self._tensors[8 * i + 4] = base[2] + at // 32
+                self._tensors[8 * i + 5] = base[3] + at // 32
         self.step_tensor = self.lr_tensor = self._coef = None
         if captured:
             self.step_tensor = torch.zeros(1, dtype=torch.int32, device=self.device)
             self.lr_tensor = torch.full((1,), lr, dtype=torch.float32, device=self.device)
             self._coef = torch.zeros(3, dtype=torch.float32, device=self.device)
 
-    def _tensor_arg(self, t, like, dtypes, name):
+    def _addresses_now(self):
+        at = [p.data_ptr() for p in self.params]
+        if self.copies is not None:
+            at += [0 if c is None else c.data_ptr() for c in self.copies]
+        return array.array("q", at)
+
+    def _adopt(self):
+        """Checks parameters and copies and holds on to their memory, so that an address that stays is theirs."""
+        spans, held = [], []
+        for i, (p, shape) in enumerate(zip(self.params, self._shapes)):
+            self._tensor_arg(p, shape, (self.dtype,), "params[%d]" % i)
+            c = None if self.copies is None else self.copies[i]
+            if c is not None:
+                self._tensor_arg(c, shape, (torch.bfloat16,), "copies[%d]" % i)
+            for t in (p, c):
+                if t is not None and t.numel():
+                    spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()))
+                    held.append(t.detach())
+        spans.sort()
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("parameters and copies must not overlap")
+        self._held, self._addresses = held, self._addresses_now()
+
+    def _tensor_arg(self, t, shape, dtypes, name):
         if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
             raise TypeError("%s must be a tensor of %s" % (name, " or ".join(str(d) for d in dtypes)))
-        if t.shape != like.shape:
-            raise ValueError("%s must have shape %s, got %s" % (name, tuple(like.shape), tuple(t.shape)))
+        if t.shape != shape:
+            raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
         if not t.is_contiguous():
             raise ValueError("%s must be contiguous" % name)
         _same_device(t, self.device, name)
@@ -1379,23 +1427,32 @@ class AdamW:
         if grad_scale is not None:
             _scale_arg(grad_scale, NVFP4, self.device, "grad_scale")
         kind = next((g.dtype for g in grads if isinstance(g, torch.Tensor)), torch.float32)
-        m, v, wide = self.m.data_ptr(), self.v.data_ptr(), self.m.element_size()
-        ms, vs = _ptr(self.m_scale), _ptr(self.v_scale)
-        tensors, count = (AdamwTensor * len(grads))(), 0
-        for i, (g, p, at) in enumerate(zip(grads, self.params, self.offsets)):
+        at, sizes, dev = [], self._sizes, self.device
+        for i, (g, shape) in enumerate(zip(grads, self._shapes)):
             if g is None:
+                if sizes is self._sizes:
+                    sizes = self._sizes[:]
+                sizes[i] = 0                             # left out
+                at.append(0)
                 continue
-            self._tensor_arg(g, p, (kind,) if kind in _FLOATS else _FLOATS, "grads[%d]" % i)
-            c = None if self.copies is None else self.copies[i]
-            scales = (None, None) if ms is None else (ms + at // 32, vs + at // 32)
-            tensors[count] = AdamwTensor(p.data_ptr(), g.data_ptr(), m + at * wide, v + at * wide, *scales, _ptr(c), p.numel())
-            count += 1
+            if not (isinstance(g, torch.Tensor) and g.dtype is kind and kind in _FLOATS and g.shape == shape
+                    and g.device == dev and g.is_contiguous()):
+                self._tensor_arg(g, shape, (kind,) if kind in _FLOATS else tuple(_FLOATS), "grads[%d]" % i)
+            at.append(g.data_ptr())
+        if self._addresses_now() != self._addresses:     # a tensor that was given other memory
+            self._adopt()
+        tensors, count = self._tensors, len(at)
+        tensors[0::8] = self._addresses[:count]
+        tensors[1::8] = array.array("q", at)
+        if self.copies is not None:
+            tensors[6::8] = self._addresses[count:]
+        tensors[7::8] = sizes
         hyper = AdamwHyper(self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1)
         _require_cuda(self.params[0], "params[0]")
         if self._coef is not None:
             _call(reqat_adamw_coefficients, self.device, hyper, self.lr_tensor.data_ptr(), self.step_tensor.data_ptr(),
                   self._coef.data_ptr())
-        _call(reqat_adamw_step, self.device, tensors, count, _dtype_arg(self.dtype), _dtype_arg(kind), self.state_bits, hyper,
+        _call(reqat_adamw_step, dev, tensors, count, _FLOATS[self.dtype], _FLOATS[kind], self.state_bits, hyper,
               _ptr(grad_scale), _ptr(self._coef))
         self.steps += 1
 

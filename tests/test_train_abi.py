@@ -138,8 +138,9 @@ def test_embedding_backward():
     no(ENUM, tdtype=4)
     for c in (dict(T=-1), dict(V=-1), dict(D=0), dict(lddy=7), dict(ldt=7)):
         no(SHAPE, **c)
-    for name in ("dy", "ids", "dtable", "ws"):
+    for name in ("dy", "ids", "dtable"):
         no(NULL, **{name: None})
+    no(NULL, T=1000, ws=None, dtable=4 * P)
     for name, off in (("dy", 1), ("ids", 2), ("dtable", 2), ("ws", 8)):
         no(ALIGN, **{name: 4 * P + off})
     no(UNSUPPORTED, dtable=P + 16)
@@ -153,7 +154,7 @@ def test_embedding_workspace_never_falls():
         for V in (0, 1, 9, 152064):
             for D in (1, 7, 5120):
                 n = size(T, V, D)
-                assert n >= 4 * (V + 1 + 2 * T)
+                assert n >= 16 * T if T > 512 else n == 0
                 assert size(min(T + 1, 1 << 22), V, D) >= n and size(T, V + 1, D) >= n and size(T, V, D + 1) >= n
     assert size(-1, 5, 5) == 0 and size(5, -1, 5) == 0 and size(5, 5, 0) == 0
 
@@ -274,7 +275,8 @@ def test_binding_embedding():
     no(ValueError, reqat.embedding_backward, dy, ids, 5, accumulate=True)
     no(ValueError, reqat.embedding_backward, dy, ids, 5, out=torch.zeros(4, 8))
     no(TypeError, reqat.embedding_backward, dy, ids, 5, out_dtype=torch.float16)
-    no(ValueError, reqat.embedding_backward, dy, ids, 5, ws=torch.zeros(1, dtype=torch.uint8))
+    no(ValueError, reqat.embedding_backward, torch.zeros(600, 8), torch.zeros(600, dtype=torch.int32), 5,
+       ws=torch.zeros(9, dtype=torch.uint8))
     no(TypeError, reqat.embedding_backward, dy, ids, 5)
 
 
