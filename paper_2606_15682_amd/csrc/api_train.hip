@@ -129,7 +129,7 @@ reqat_status reqat_layer_norm(const void *x, reqat_dtype dtype, int64_t rows, in
 
 size_t reqat_layer_norm_workspace_bytes(reqat_dtype dtype, int64_t rows, int64_t cols, int bias) {
     if (check_norm(dtype, REQAT_DT_F32, rows, cols) != REQAT_OK) return 0;
-    return (size_t)norm_plan(rows, cols, dtype == REQAT_DT_BF16).groups * (size_t)cols * (bias ? 8 : 4);
+    return (size_t)norm_plan(rows, cols, dtype == REQAT_DT_BF16).sums * (size_t)cols * (bias ? 8 : 4);
 }
 
 reqat_status reqat_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, reqat_dtype dtype, int64_t rows,

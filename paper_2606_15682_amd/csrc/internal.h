@@ -128,7 +128,7 @@ hipError_t launch_policy_backward(const PolicyArgs &a, bool bf16, hipStream_t st
 struct NormArgs {
     const void *x, *dy, *w, *b;            // x, dy, y, dx of one type; w, b, dw, db of another; b, db may be null
     void *y, *dx, *dw, *db;
-    float *stats, *partials;               // partials: norm_plan's groups x K sums of dw, then of db
+    float *stats, *partials;               // partials: norm_plan's sums x K of dw, then of db
     int64_t M, K, ldx, lddy, ldy, lddx;
     float eps;
     bool center, w_bf16;

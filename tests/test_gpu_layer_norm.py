@@ -115,6 +115,17 @@ def test_strides_and_in_place(pad, dtype):
     assert torch.equal(reqat.layer_norm(z, w, b, out=z)[0], y)
 
 
+@pytest.mark.parametrize("K,dtype", [(20000, BF), (20001, BF), (9001, F32), (20000, F32)])
+def test_wide_rows_in_place(K, dtype):
+    x, dy, w, b = _inputs(7, K, dtype, F32)
+    stats = reqat.layer_norm(x, w, b)[1]
+    want = reqat.layer_norm_backward(dy, x, w, stats, bias=True)
+    for target in ("dy", "x"):
+        a, c = dy.clone(), x.clone()
+        got = reqat.layer_norm_backward(a, c, w, stats, bias=True, out=a if target == "dy" else c)
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
 def test_constant_and_far_rows():
     """A constant row has variance 0; far means do not cost the variance its digits, for the mean is taken off first."""
     for center in (True, False):
