@@ -204,3 +204,44 @@ def test_against_plain_recurrence():
         x = x * (1 - 0.1 * 0.05) - 0.1 * (m / (1 - 0.9 ** t)) / (math.sqrt(v / (1 - 0.99 ** t)) + 1e-6)
         # each step: 3 half steps of x and some 20 of its move of at most 0.3, over ten steps
         assert abs(float(p) - x) <= t * ref.EPS32 * (3 + 20 * 0.3)
+
+
+def test_replaced_memory_is_the_one_used():
+    """A parameter that was given other memory is stepped there; one that no longer fits is refused."""
+    p = [torch.nn.Parameter(torch.ones(300, device=DEV)), torch.nn.Parameter(torch.ones(50, device=DEV))]
+    copies = [torch.empty(300, dtype=BF, device=DEV), None]
+    opt = reqat.AdamW(p, 1e-2, weight_decay=0.0, copies=copies)
+    g = [torch.ones(300, device=DEV), torch.ones(50, device=DEV)]
+    opt.step(g)
+    old = p[0].data
+    kept = old.clone()
+    p[0].data = torch.full((300,), 5.0, device=DEV)
+    opt.copies[0] = other = torch.zeros(300, dtype=BF, device=DEV)
+    opt.step(g)
+    assert torch.equal(old, kept) and torch.allclose(p[0].data, torch.full((300,), 4.99, device=DEV), atol=1e-6)
+    assert torch.equal(other, p[0].data.to(BF))
+    p[0].data = torch.ones(299, device=DEV)
+    with pytest.raises(ValueError):
+        opt.step(g)
+    p[0].data = p[1].data
+    with pytest.raises(ValueError):
+        opt.step(g)
+    assert opt.steps == 2
+
+
+def test_gradients_in_odd_places():
+    """States lie at multiples of 128; parameters, gradients and copies anywhere: every alignment of them, both state widths."""
+    n = 1000
+    for bits in (32, 8):
+        for off in range(1, 8):
+            wide = torch.randn(n + 8, generator=torch.Generator().manual_seed(off)).to(DEV)
+            grad = torch.randn(n + 8, generator=torch.Generator().manual_seed(9 + off)).to(BF).to(DEV)
+            copy = torch.zeros(n + 8, dtype=BF, device=DEV)
+            a, b = wide.clone(), wide[off:off + n].clone()
+            one = reqat.AdamW([a[off:off + n]], 1e-2, state_bits=bits, copies=[copy[off:off + n]])
+            two = reqat.AdamW([b], 1e-2, state_bits=bits)
+            one.step([grad[off:off + n]])
+            two.step([grad[off:off + n].clone()])
+            assert torch.equal(a[off:off + n], b) and torch.equal(a[:off], wide[:off]) and torch.equal(a[off + n:], wide[off + n:])
+            assert torch.equal(copy[off:off + n], b.to(BF)) and not copy[:off].any() and not copy[off + n:].any()
+            assert torch.equal(one.m, two.m) and torch.equal(one.v, two.v)
