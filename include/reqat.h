@@ -537,7 +537,7 @@ reqat_status reqat_embedding_backward(const void *dy, reqat_dtype dtype, int64_t
 size_t reqat_embedding_workspace_bytes(int64_t T, int64_t V, int64_t D);
 
 /*
- * AdamW step over many tensors, each of n elements without gaps:
+ * AdamW step over many tensors, each of n elements without gaps, at most 2^34:
  *     g = grad * *grad_scale (NULL: 1),  m' = b1 m + (1 - b1) g,  v' = b2 v + (1 - b2) g^2,
  *     p' = (1 - lr weight_decay) p - lr / (1 - b1^step) * m' / (sqrt(v') / sqrt(1 - b2^step) + eps),
  * every product, sum and root rounded to FP32 (b1, 1 - b1, b2 and 1 - b2 are FP32 numbers,

@@ -219,7 +219,7 @@ reqat_status reqat_adamw_step(const reqat_adamw_tensor *tensors, int64_t count, 
     const int64_t state = state_bits == 32 ? 4 : 1;
     for (int64_t i = 0; i < count; ++i) {
         const reqat_adamw_tensor &t = tensors[i];
-        if (t.n < 0 || t.n > (int64_t(1) << 35)) return REQAT_E_SHAPE;
+        if (t.n < 0 || t.n > (int64_t(1) << 34)) return REQAT_E_SHAPE;
         if (t.n == 0) continue;
         if (!t.p || !t.g || !t.m || !t.v || (state_bits == 8 && (!t.m_scale || !t.v_scale))) return REQAT_E_NULL;
         if (!aligned(t.p, size_of(p_dtype)) || !aligned(t.g, size_of(g_dtype)) || !aligned(t.m, state) || !aligned(t.v, state) ||
