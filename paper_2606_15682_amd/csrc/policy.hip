@@ -150,7 +150,7 @@ template <typename T> __device__ __forceinline__ float4 row_stats(const PolicyAr
     }
     const float r = expf(lp - in.old);
     float slope = outside(a, r, in.adv) ? 0.0f : -in.adv * r;
-    if (a.ref) slope -= a.kl * expm1f(in.ref - lp);
+    if (a.ref && a.kl != 0.0f) slope -= a.kl * expm1f(in.ref - lp);      // not 0 times Inf
     return make_float4(lp, lse, in.w * slope, r);
 }
 
@@ -347,7 +347,7 @@ template <int TH> __device__ __forceinline__ void write_loss(const PolicyArgs &a
             s[k] = 0.0;
             for (int i = 0; i < TH / 64; ++i) s[k] += red[k][i];
         }
-        a.loss[0] = (float)(s[0] + (double)a.kl * s[1]);
+        a.loss[0] = (float)(a.kl != 0.0f ? s[0] + (double)a.kl * s[1] : s[0]);
         a.loss[1] = (float)s[0];
         a.loss[2] = (float)s[1];
         a.loss[3] = (float)s[2];

@@ -267,3 +267,14 @@ def test_deterministic_and_empty():
     e = {k: v[:0] for k, v in c.items()}
     loss, stats, grad = _run(e)
     assert not loss.any() and stats.shape == (0, 4) and grad.shape == (0, 5001)
+
+
+def test_reference_without_weight():
+    """With kl_coef 0 a reference, however far, is reported and reaches neither loss nor gradient."""
+    for T in (3, 200):                                     # cut into slices, whole rows
+        c = _case(T, 9000, torch.float32)
+        want = reqat.policy_loss_grad(c["logits"], c["targets"], c["old"], c["adv"])
+        far = torch.full((T,), 300.0, device=DEV)
+        loss, stats, grad = reqat.policy_loss_grad(c["logits"], c["targets"], c["old"], c["adv"], ref_logp=far)
+        assert torch.equal(loss[:2], want[0][:2]) and torch.equal(stats, want[1]) and torch.equal(grad, want[2])
+        assert torch.isinf(loss[2])
