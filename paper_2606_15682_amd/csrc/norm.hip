@@ -78,19 +78,40 @@ template <int N> __device__ __forceinline__ void load_params_at(const void *w, b
     else load_params_of(reinterpret_cast<const float *>(w) + j, n, out);
 }
 
-// Those of the thread's elements.  WHOLE: the row has whole vectors only; a vector without an element of it reads the first.
+// Where a thread's vectors of a row of K >= kVec elements lie, so that every access is a whole vector and none stands
+// behind a branch, where the compiler waits for all loads in flight.  The last vector of a row whose length is no multiple of
+// it ends with the row: its first `skip` elements are the vector's before it once more, get the same results in both
+// places, and count in the sums once.  A thread without elements there reads the row's first vector; all its elements are
+// skipped and nothing of it is written.  (All vectors but a thread's last are whole: the group's last step is not full only
+// there.)
+template <typename T, int G, int VPT> struct Places {
+    int i, at_last, skip;
+    bool last;
+    __device__ __forceinline__ Places(int i, int K) : i(i) {
+        constexpr int N = kVec<T>;
+        const int start = ((VPT - 1) * G + i) * N;
+        last = start < K;
+        at_last = last ? (start < K - N ? start : K - N) : 0;
+        skip = last ? start - at_last : N;
+    }
+    __device__ __forceinline__ int at(int v) const { return v < VPT - 1 ? (v * G + i) * kVec<T> : at_last; }
+    __device__ __forceinline__ bool mine(int v) const { return v < VPT - 1 || last; }
+    __device__ __forceinline__ bool counts(int v, int e) const { return v < VPT - 1 || e >= skip; }
+};
+
+// The thread's parameters.  WHOLE: the row has at least a vector.
 template <typename T, int G, int VPT, bool WHOLE>
-__device__ __forceinline__ void load_params(const void *w, bool bf16, int K, int i, float (&out)[VPT][kVec<T>]) {
+__device__ __forceinline__ void load_params(const void *w, bool bf16, int K, const Places<T, G, VPT> &p, float (&out)[VPT][kVec<T>]) {
     constexpr int N = kVec<T>;
     if (!WHOLE || !w) {
 #pragma unroll
-        for (int v = 0; v < VPT; ++v) load_params_at(w, bf16, K, (v * G + i) * N, out[v]);
+        for (int v = 0; v < VPT; ++v) load_params_at(w, bf16, K, (v * G + p.i) * N, out[v]);
     } else if (bf16) {
 #pragma unroll
-        for (int v = 0; v < VPT; ++v) load_params_of(reinterpret_cast<const uint16_t *>(w) + ((v * G + i) * N < K ? (v * G + i) * N : 0), N, out[v]);
+        for (int v = 0; v < VPT; ++v) load_params_of(reinterpret_cast<const uint16_t *>(w) + p.at(v), N, out[v]);
     } else {
 #pragma unroll
-        for (int v = 0; v < VPT; ++v) load_params_of(reinterpret_cast<const float *>(w) + ((v * G + i) * N < K ? (v * G + i) * N : 0), N, out[v]);
+        for (int v = 0; v < VPT; ++v) load_params_of(reinterpret_cast<const float *>(w) + p.at(v), N, out[v]);
     }
 }
 
@@ -116,18 +137,16 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_forward_kernel(NormArg
     const int i = threadIdx.x % G;
     const int K = (int)a.K;
     const float inv = 1.0f / (float)K;
-    const bool last = ((VPT - 1) * G + i) * N < K;      // whether the thread's last vector has elements
+    const Places<T, G, VPT> p(i, K);
     float w[VPT][N], b[VPT][N];
-    load_params<T, G, VPT, WHOLE>(a.w, a.w_bf16, K, i, w);
-    load_params<T, G, VPT, WHOLE>(a.b, a.w_bf16, K, i, b);
+    load_params<T, G, VPT, WHOLE>(a.w, a.w_bf16, K, p, w);
+    load_params<T, G, VPT, WHOLE>(a.b, a.w_bf16, K, p, b);
     for (int64_t r = (int64_t)blockIdx.x * kRows + (G == 64 ? threadIdx.x >> 6 : 0); r < a.M; r += (int64_t)gridDim.x * kRows) {
         uint4 raw[VPT];
         const T *row = reinterpret_cast<const T *>(a.x) + r * a.ldx;
         if constexpr (WHOLE) {
 #pragma unroll
-            for (int v = 0; v < VPT; ++v) raw[v] = load_vec(row + (v < VPT - 1 || last ? (v * G + i) * N : 0));
-#pragma unroll
-            for (int v = 0; v < VPT; ++v) raw[v] = where(v < VPT - 1 || last, raw[v]);
+            for (int v = 0; v < VPT; ++v) raw[v] = load_vec(row + p.at(v));
         } else {
             load_row<T, G, VPT>(row, K, i, raw);
         }
@@ -138,7 +157,7 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_forward_kernel(NormArg
 #pragma unroll
             for (int v = 0; v < VPT; ++v)
 #pragma unroll
-                for (int e = 0; e < N; ++e) s[0] += x[v][e];
+                for (int e = 0; e < N; ++e) s[0] += !WHOLE || p.counts(v, e) ? x[v][e] : 0.0f;
             sum(s);
             mu = s[0] * inv;
         }
@@ -148,7 +167,7 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_forward_kernel(NormArg
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 x[v][e] -= mu;
-                const bool in = (v * G + i) * N + e < K;
+                const bool in = WHOLE ? p.counts(v, e) : (v * G + i) * N + e < K;
                 s[0] = __builtin_fmaf(in ? x[v][e] : 0.0f, x[v][e], s[0]);
             }
         sum(s);
@@ -158,7 +177,11 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_forward_kernel(NormArg
         for (int v = 0; v < VPT; ++v) {
 #pragma unroll
             for (int e = 0; e < N; ++e) x[v][e] = __builtin_fmaf(x[v][e] * rstd, w[v][e], b[v][e]);
-            store_at(y, K, (v * G + i) * N, x[v]);
+            if constexpr (WHOLE) {
+                if (p.mine(v)) store_vec(y + p.at(v), pack<T>(x[v]));
+            } else {
+                store_at(y, K, (v * G + i) * N, x[v]);
+            }
         }
         if (i == 0) {
             a.stats[2 * r] = mu;
@@ -171,9 +194,7 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_forward_kernel(NormArg
 // from the sums to dx, in two or four times the registers.
 __device__ __forceinline__ void pin(uint4 &v, float x) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w) : "v"(x)); }
 
-// WHOLE: K is a multiple of the vector, so that every load is a whole vector, and those without an element of the row read
-// its first one instead of standing behind a branch: behind one the compiler waits for all loads in flight, the next row's
-// too.  Their elements are made zeros when they are used.
+// WHOLE: the row has at least a vector, and Places says where the thread's are.
 template <typename T, int G, int VPT, bool WHOLE>
 __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormArgs a) {
     constexpr int N = kVec<T>, P = norm_groups(G);
@@ -186,10 +207,10 @@ __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormAr
     const float inv = 1.0f / (float)K;
     constexpr int kSums = kHold ? VPT : 1;
     float held[kSums][N], dw[kSums][N] = {}, db[kSums][N] = {};
-    if constexpr (kHold) load_params<T, G, VPT, WHOLE>(a.w, a.w_bf16, K, i, held);
+    const Places<T, G, VPT> p(i, K);
+    if constexpr (kHold) load_params<T, G, VPT, WHOLE>(a.w, a.w_bf16, K, p, held);
     uint4 xr[VPT], yr[VPT];
     float2 sr;                                          // mean and 1 / deviation of the row in xr
-    const bool last = ((VPT - 1) * G + i) * N < K;      // whether the thread's last vector has elements
     const auto load = [&](int64_t r) {                  // a row behind the last one: zeros, which add nothing
         const bool in = r < a.M;
         __builtin_memcpy(&sr, a.stats + 2 * (in ? r : 0), 8);
@@ -198,9 +219,8 @@ __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormAr
         if constexpr (WHOLE) {
 #pragma unroll
             for (int v = 0; v < VPT; ++v) {
-                const int j = v < VPT - 1 || last ? (v * G + i) * N : 0;
-                xr[v] = load_vec(x + j);
-                yr[v] = load_vec(dy + j);
+                xr[v] = load_vec(x + p.at(v));
+                yr[v] = load_vec(dy + p.at(v));
             }
         } else {
             load_row<T, G, VPT>(x, in ? K : 0, i, xr);
@@ -217,9 +237,8 @@ __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormAr
         uint4 x0[VPT], y0[VPT];
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
-            const bool real = in && (v < VPT - 1 || last);
-            x0[v] = WHOLE ? where(real, xr[v]) : xr[v];
-            y0[v] = WHOLE ? where(real, yr[v]) : yr[v];
+            x0[v] = WHOLE && P > 1 ? where(in, xr[v]) : xr[v];      // with one group a workgroup, every row is one
+            y0[v] = WHOLE && P > 1 ? where(in, yr[v]) : yr[v];
         }
         if (kHold) load(r + step);
         float s[2] = {0.0f, 0.0f};                      // sum g, sum g h; zeros beyond K: dy and w are zero there
@@ -229,13 +248,14 @@ __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormAr
             if (!kHold) pin(x0[v], s[1]);
             unpack<T>(x0[v], x);
             unpack<T>(y0[v], dy);
-            if constexpr (!kHold) load_params_at(a.w, a.w_bf16, K, (v * G + i) * N, w);
+            if constexpr (!kHold) load_params_at(a.w, a.w_bf16, K, WHOLE ? p.at(v) : (v * G + i) * N, w);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 if constexpr (kHold) w[e] = held[v][e];
-                const float h = (x[e] - mu) * rstd, gr = dy[e] * w[e];
+                const bool counts = !WHOLE || p.counts(v, e);
+                const float h = (x[e] - mu) * rstd, gr = counts ? dy[e] * w[e] : 0.0f;
                 s[0] += gr;
-                s[1] = __builtin_fmaf(gr, h, s[1]);
+                s[1] = __builtin_fmaf(gr, counts ? h : 0.0f, s[1]);
                 if constexpr (kHold) {
                     dw[v][e] = __builtin_fmaf(dy[e], h, dw[v][e]);
                     db[v][e] += dy[e];
@@ -252,7 +272,7 @@ __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormAr
             float x[N], dy[N], w[N];
             unpack<T>(x0[v], x);
             unpack<T>(y0[v], dy);
-            if constexpr (!kHold) load_params_at(a.w, a.w_bf16, K, (v * G + i) * N, w);
+            if constexpr (!kHold) load_params_at(a.w, a.w_bf16, K, WHOLE ? p.at(v) : (v * G + i) * N, w);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 if constexpr (kHold) w[e] = held[v][e];
@@ -260,7 +280,7 @@ __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormAr
                 x[e] = rstd * (__builtin_fmaf(dy[e], w[e], -c0) - h * c1);
             }
             if constexpr (WHOLE) {
-                if (in && (v < VPT - 1 || last)) store_vec(dx + (v * G + i) * N, pack<T>(x));
+                if (in && p.mine(v)) store_vec(dx + p.at(v), pack<T>(x));
             } else {
                 store_at(dx, in ? K : 0, (v * G + i) * N, x);
             }
@@ -276,8 +296,8 @@ __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormAr
         if (g == from) {
 #pragma unroll
             for (int v = 0; v < kSums; ++v) {
-                const int j = (v * G + i) * N;
-                if (j < K) {
+                const int j = WHOLE ? p.at(v) : (v * G + i) * N;
+                if (WHOLE ? p.mine(v) : j < K) {
                     put_sums(others + j, K - j, dw[v]);
                     put_sums(others + K + j, K - j, db[v]);
                 }
@@ -287,8 +307,8 @@ __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormAr
         if (g == 0) {
 #pragma unroll
             for (int v = 0; v < kSums; ++v) {
-                const int j = (v * G + i) * N;
-                if (j < K) {
+                const int j = WHOLE ? p.at(v) : (v * G + i) * N;
+                if (WHOLE ? p.mine(v) : j < K) {
                     float x[N], y[N];
                     load_params_of(others + j, K - j, x);
                     load_params_of(others + K + j, K - j, y);
@@ -305,8 +325,8 @@ __global__ __launch_bounds__(G *norm_groups(G)) void norm_backward_kernel(NormAr
     float *part = a.partials + (int64_t)blockIdx.x * K;
 #pragma unroll
     for (int v = 0; v < kSums; ++v)
-        if ((v * G + i) * N < K) {
-            const int j = (v * G + i) * N;
+        if (WHOLE ? p.mine(v) : (v * G + i) * N < K) {
+            const int j = WHOLE ? p.at(v) : (v * G + i) * N;
             put_sums(part + j, K - j, dw[v]);
             if (a.db) put_sums(part + (int64_t)gridDim.x * K + j, K - j, db[v]);
         }
@@ -371,7 +391,7 @@ __global__ __launch_bounds__(1024) void norm_params_kernel(NormArgs a, int64_t p
 template <typename T, int G> hipError_t launch(const NormArgs &a, const NormPlan &p, bool backward, hipStream_t stream) {
     constexpr int P = norm_groups(G);
     const dim3 grid((unsigned)(backward ? p.backward : p.forward));
-    const bool whole = a.K % kVec<T> == 0;
+    const bool whole = a.K >= kVec<T>;
     const size_t lds = P > 1 ? (size_t)a.K * 8 : 0;
 #define REQAT_NORM(V)                                                                                                          \
     case V:                                                                                                                    \
