@@ -1120,7 +1120,7 @@ class SemLoss(torch.autograd.Function):
 
 def _call(fn, device, *args):
     """The C call with the device current, on its current stream."""
-    current = torch.cuda.current_device()
+    current = torch._C._cuda_getDevice()
     if device.index is None or device.index == current:
         st = fn(*args, torch._C._cuda_getCurrentRawStream(current))
     else:
@@ -1336,7 +1336,7 @@ class AdamW:
     float32 master weights), or None.  The states of all tensors lie in one buffer each: ``m`` and ``v``, float32, or uint8
     codes with the float32 scales ``m_scale`` and ``v_scale`` of every 128 elements (the formats are stated in
     include/reqat.h); tensor i has the elements ``offsets[i]`` .. ``offsets[i]`` + its size.  All zeros at the start, they
-    may be written in place.  ``steps`` counts the steps taken; ``lr``, ``betas``, ``eps`` and ``weight_decay`` may be
+    may be written in place or assigned.  ``steps`` counts the steps taken; ``lr``, ``betas``, ``eps`` and ``weight_decay`` may be
     assigned between steps.
 
     captured=True is for steps in a HIP graph: the count is ``step_tensor`` (int32) and the rate ``lr_tensor`` (float32),
@@ -1372,13 +1372,7 @@ class AdamW:
         # an array of reqat_adamw_tensor; a step fills in the addresses of parameters, copies and gradients
         self._sizes = array.array("q", [p.numel() for p in self.params])
         self._tensors = array.array("q", bytes(64 * len(self.params)))
-        base = [t if t is None else t.data_ptr() for t in (self.m, self.v, self.m_scale, self.v_scale)]
-        for i, at in enumerate(self.offsets):
-            self._tensors[8 * i + 2] = base[0] + at * self.m.element_size()
-            self._tensors[8 * i + 3] = base[1] + at * self.v.element_size()
-            if state_bits == 8:
-                self._tensors[8 * i + 4] = base[2] + at // 32
-                self._tensors[8 * i + 5] = base[3] + at // 32
+        self._total, self._bases = size, None
         self.step_tensor = self.lr_tensor = self._coef = None
         if captured:
             self.step_tensor = torch.zeros(1, dtype=torch.int32, device=self.device)
@@ -1407,6 +1401,23 @@ class AdamW:
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("parameters and copies must not overlap")
         self._held, self._addresses = held, self._addresses_now()
+
+    def _place_states(self, bases):
+        """Checks the states' buffers and enters their addresses: at the first step, and when one was replaced."""
+        kind = torch.float32 if self.state_bits == 32 else torch.uint8
+        for name, n, dtype in (("m", self._total, kind), ("v", self._total, kind),
+                               ("m_scale", self._total // 128, torch.float32), ("v_scale", self._total // 128, torch.float32)):
+            if dtype is torch.float32 and self.state_bits == 32 and name.endswith("scale"):
+                continue
+            _index_arg(getattr(self, name), (n,), dtype, self.device, name)
+        for i, at in enumerate(self.offsets):
+            self._tensors[8 * i + 2] = bases[0] + at * self.m.element_size()
+            self._tensors[8 * i + 3] = bases[1] + at * self.v.element_size()
+            if self.state_bits == 8:
+                self._tensors[8 * i + 4] = bases[2] + at // 32
+                self._tensors[8 * i + 5] = bases[3] + at // 32
+        self._bases = bases
+        self._held_states = [t if t is None else t.detach() for t in (self.m, self.v, self.m_scale, self.v_scale)]
 
     def _tensor_arg(self, t, shape, dtypes, name):
         if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
@@ -1441,6 +1452,9 @@ class AdamW:
             at.append(g.data_ptr())
         if self._addresses_now() != self._addresses:     # a tensor that was given other memory
             self._adopt()
+        bases = [0 if t is None else t.data_ptr() for t in (self.m, self.v, self.m_scale, self.v_scale)]
+        if bases != self._bases:
+            self._place_states(bases)
         tensors, count = self._tensors, len(at)
         tensors[0::8] = self._addresses[:count]
         tensors[1::8] = array.array("q", at)
@@ -1461,7 +1475,10 @@ class AdamW:
         if self.state_bits == 32:
             return self.m, self.v
         _require_cuda(self.m, "m")
-        n = self.m.numel()
+        n = self._total
+        for name, shape, dtype in (("m", (n,), torch.uint8), ("v", (n,), torch.uint8), ("m_scale", (n // 128,), torch.float32),
+                                   ("v_scale", (n // 128,), torch.float32)):
+            _index_arg(getattr(self, name), shape, dtype, self.device, name)
         m, v = (torch.empty(n, dtype=torch.float32, device=self.device) for _ in range(2))
         _call(reqat_adamw_moments, self.device, self.m.data_ptr(), self.m_scale.data_ptr(), self.v.data_ptr(),
               self.v_scale.data_ptr(), n, m.data_ptr(), v.data_ptr())

@@ -1,4 +1,5 @@
 """GPU: AdamW steps against their formulas: states and codes exactly, parameters within FP32's rounding."""
+import copy
 import math
 
 import pytest
@@ -236,12 +237,39 @@ def test_gradients_in_odd_places():
         for off in range(1, 8):
             wide = torch.randn(n + 8, generator=torch.Generator().manual_seed(off)).to(DEV)
             grad = torch.randn(n + 8, generator=torch.Generator().manual_seed(9 + off)).to(BF).to(DEV)
-            copy = torch.zeros(n + 8, dtype=BF, device=DEV)
+            low = torch.zeros(n + 8, dtype=BF, device=DEV)
             a, b = wide.clone(), wide[off:off + n].clone()
-            one = reqat.AdamW([a[off:off + n]], 1e-2, state_bits=bits, copies=[copy[off:off + n]])
+            one = reqat.AdamW([a[off:off + n]], 1e-2, state_bits=bits, copies=[low[off:off + n]])
             two = reqat.AdamW([b], 1e-2, state_bits=bits)
             one.step([grad[off:off + n]])
             two.step([grad[off:off + n].clone()])
             assert torch.equal(a[off:off + n], b) and torch.equal(a[:off], wide[:off]) and torch.equal(a[off + n:], wide[off + n:])
-            assert torch.equal(copy[off:off + n], b.to(BF)) and not copy[:off].any() and not copy[off + n:].any()
+            assert torch.equal(low[off:off + n], b.to(BF)) and not low[:off].any() and not low[off + n:].any()
             assert torch.equal(one.m, two.m) and torch.equal(one.v, two.v)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_copied_and_assigned_states(bits):
+    """A deep copy steps its own parameters and states; assigned buffers are the ones used, ones that do not fit are refused."""
+    p = _make([300, 77], F32)
+    grads = _make([300, 77], F32, seed=3)
+    a = reqat.AdamW(p, 1e-2, state_bits=bits)
+    a.step(grads)
+    b = copy.deepcopy(a)
+    kept = [t.clone() for t in (a.m, a.v, *p)]
+    b.step(grads)
+    assert all(torch.equal(x, y) for x, y in zip(kept, (a.m, a.v, *p)))
+    assert b.steps == 2 and not torch.equal(b.params[0], p[0])
+    a.step(grads)
+    assert torch.equal(a.m, b.m) and torch.equal(a.v, b.v) and all(torch.equal(x, y) for x, y in zip(p, b.params))
+    old = a.m
+    before = old.clone()
+    a.m = torch.zeros_like(old)
+    a.step(grads)
+    assert torch.equal(old, before) and a.m.any()
+    a.v = a.v[:-128].clone()
+    with pytest.raises(ValueError):
+        a.step(grads)
+    a.v = torch.zeros(a.m.numel(), dtype=torch.float64, device=DEV)
+    with pytest.raises(TypeError):
+        a.step(grads)
