@@ -1120,7 +1120,7 @@ class SemLoss(torch.autograd.Function):
 
 def _call(fn, device, *args):
     """The C call with the device current, on its current stream."""
-    current = torch._C._cuda_getDevice()
+    current = torch.cuda.current_device()
     if device.index is None or device.index == current:
         st = fn(*args, torch._C._cuda_getCurrentRawStream(current))
     else:
