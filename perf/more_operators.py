@@ -516,6 +516,7 @@ def run(state):
         return reqat.embedding_backward(state["dy"], state["ids"], case["V"], scale=case["scale"],
                                         out_dtype=DTYPES[case["gdtype"]])
     opt = state["opt"]
+    opt.steps = STEP - 1                        # every pass is that step, as in the plain form
     opt.step(state["grads"], grad_scale=state["scale"])
     m, v = (opt.m, opt.v) if case["bits"] == 32 else opt.moments()
     return state["p"], m, v, state["copies"]
