@@ -1351,8 +1351,6 @@ class AdamW:
             raise ValueError("state_bits must be 8 or 32")
         if not self.params:
             raise ValueError("no parameters")
-        if self.copies is not None and len(self.copies) != len(self.params):
-            raise ValueError("copies must have one tensor (or None) for each parameter")
         first = self.params[0]
         if not isinstance(first, torch.Tensor) or first.dtype not in _FLOATS:
             raise TypeError("parameters must be bfloat16 or float32 tensors")
@@ -1388,6 +1386,10 @@ class AdamW:
     def _adopt(self):
         """Checks parameters and copies and holds on to their memory, so that an address that stays is theirs."""
         spans, held = [], []
+        if len(self.params) != len(self._shapes):
+            raise ValueError("params must stay %d tensors" % len(self._shapes))
+        if self.copies is not None and len(self.copies) != len(self.params):
+            raise ValueError("copies must have one tensor (or None) for each parameter")
         for i, (p, shape) in enumerate(zip(self.params, self._shapes)):
             self._tensor_arg(p, shape, (self.dtype,), "params[%d]" % i)
             c = None if self.copies is None else self.copies[i]
@@ -1458,8 +1460,7 @@ class AdamW:
         tensors, count = self._tensors, len(at)
         tensors[0::8] = self._addresses[:count]
         tensors[1::8] = array.array("q", at)
-        if self.copies is not None:
-            tensors[6::8] = self._addresses[count:]
+        tensors[6::8] = array.array("q", bytes(8 * count)) if self.copies is None else self._addresses[count:]
         tensors[7::8] = sizes
         hyper = AdamwHyper(self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1)
         _require_cuda(self.params[0], "params[0]")
