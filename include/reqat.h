@@ -552,9 +552,11 @@ size_t reqat_embedding_workspace_bytes(int64_t T, int64_t V, int64_t D);
  *     s = RN(max u' / 1.9375), u' = RN(sqrt(v')), code of RN(u' / s) to nearest, ties to
  *     even, and never 0 for u' / s > 0.  All bytes zero is the state at the start.
  *     A block with a NaN or Inf has scale NaN and codes 0, a block of zeros scale 0.
- * Tensors of n == 0 are skipped.  No two tensors may overlap; the tensors and the struct
- * array are checked on the host, which reads the array during the call.  count tensors
- * take ceil(count / 56) launches.
+ * Tensors of n == 0 are skipped.  A call's tensors share hyper->step, the number of steps
+ * that their moments have taken, this one included; tensors of another number go in a call
+ * of their own.  No two tensors may overlap; the tensors and the struct array are checked
+ * on the host, which reads the array during the call.  count tensors take
+ * ceil(count / 56) launches.
  *   hyper: host memory; step counts from 1 (REQAT_E_UNSUPPORTED for less, for a beta outside
  *     [0, 1), a negative eps or values that are not finite).
  *   coef: NULL, or three device floats from reqat_adamw_coefficients, which take the

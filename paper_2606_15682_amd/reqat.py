@@ -1336,12 +1336,14 @@ class AdamW:
     float32 master weights), or None.  The states of all tensors lie in one buffer each: ``m`` and ``v``, float32, or uint8
     codes with the float32 scales ``m_scale`` and ``v_scale`` of every 128 elements (the formats are stated in
     include/reqat.h); tensor i has the elements ``offsets[i]`` .. ``offsets[i]`` + its size.  All zeros at the start, they
-    may be written in place or assigned.  ``steps`` counts the steps taken; ``lr``, ``betas``, ``eps`` and ``weight_decay`` may be
-    assigned between steps.
+    may be written in place or assigned.  ``steps`` counts the steps taken, ``missed[i]`` those of them that left parameter
+    i out: its moments have moved steps - missed[i] times, and that count corrects their bias.  Both, ``lr``, ``betas``,
+    ``eps`` and ``weight_decay`` may be assigned between steps.
 
     captured=True is for steps in a HIP graph: the count is ``step_tensor`` (int32) and the rate ``lr_tensor`` (float32),
-    on the device, the count rising with every replay.  Parameters, copies, states and gradients of a captured step stay
-    where they are."""
+    on the device, the count rising with every replay.  It is one count for
+    all: the first step says which parameters have gradients, and every later one has them for the same.  Parameters,
+    copies, states and gradients of a captured step stay where they are."""
 
     def __init__(self, params, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, copies=None,
                  captured=False):
@@ -1371,7 +1373,8 @@ class AdamW:
         self._sizes = array.array("q", [p.numel() for p in self.params])
         self._tensors = array.array("q", bytes(64 * len(self.params)))
         self._total, self._bases = size, None
-        self.step_tensor = self.lr_tensor = self._coef = None
+        self.missed = [0] * len(self.params)
+        self.step_tensor = self.lr_tensor = self._coef = self._stepped = None
         if captured:
             self.step_tensor = torch.zeros(1, dtype=torch.int32, device=self.device)
             self.lr_tensor = torch.full((1,), lr, dtype=torch.float32, device=self.device)
@@ -1432,8 +1435,8 @@ class AdamW:
 
     def step(self, grads, grad_scale=None):
         """One step with the gradients of all parameters (tensors of their shapes, all bfloat16 or all float32; None: the
-        parameter is left out of this step), each times grad_scale (a float32 tensor of one element, as of a clipped
-        norm) first."""
+        parameter is left out of this step, its count too), each times grad_scale (a float32 tensor of one element, as
+        of a clipped norm) first.  Parameters of different counts go in launches of their own."""
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError("grads must have one tensor (or None) for each parameter")
@@ -1461,14 +1464,39 @@ class AdamW:
         tensors[0::8] = self._addresses[:count]
         tensors[1::8] = array.array("q", at)
         tensors[6::8] = array.array("q", bytes(8 * count)) if self.copies is None else self._addresses[count:]
-        tensors[7::8] = sizes
-        hyper = AdamwHyper(self.lr, *self.betas, self.eps, self.weight_decay, self.steps + 1)
         _require_cuda(self.params[0], "params[0]")
         if self._coef is not None:
-            _call(reqat_adamw_coefficients, self.device, hyper, self.lr_tensor.data_ptr(), self.step_tensor.data_ptr(),
-                  self._coef.data_ptr())
-        _call(reqat_adamw_step, dev, tensors, count, _FLOATS[self.dtype], _FLOATS[kind], self.state_bits, hyper,
-              _ptr(grad_scale), _ptr(self._coef))
+            self._step_captured(grads, kind, sizes, grad_scale)
+            return
+        missed = self.missed
+        if not any(missed):
+            behind = (0,)
+        else:                                            # the lowest count first: it is the one that may be refused
+            behind = sorted({n for n, size in zip(missed, sizes) if size}, reverse=True)
+        for n in behind:
+            tensors[7::8] = sizes if len(behind) == 1 else array.array("q", [z if k == n else 0 for z, k in zip(sizes, missed)])
+            _call(reqat_adamw_step, dev, tensors, count, _FLOATS[self.dtype], _FLOATS[kind], self.state_bits,
+                  self._hyper(self.steps + 1 - n), _ptr(grad_scale), None)
+        if sizes is not self._sizes:
+            self.missed = [k + (g is None) for k, g in zip(missed, grads)]
+        self.steps += 1
+
+    def _hyper(self, step):
+        return AdamwHyper(self.lr, *self.betas, self.eps, self.weight_decay, step)
+
+    def _step_captured(self, grads, kind, sizes, grad_scale):
+        stepped = [g is not None for g in grads]
+        if self._stepped is None and not any(stepped):
+            return
+        if self._stepped not in (None, stepped):
+            raise ValueError("captured steps have gradients for the same parameters each time")
+        hyper = self._hyper(1)                           # the count is on the device
+        self._tensors[7::8] = sizes
+        _call(reqat_adamw_coefficients, self.device, hyper, self.lr_tensor.data_ptr(), self.step_tensor.data_ptr(),
+              self._coef.data_ptr())
+        _call(reqat_adamw_step, self.device, self._tensors, len(grads), _FLOATS[self.dtype], _FLOATS[kind], self.state_bits,
+              hyper, _ptr(grad_scale), _ptr(self._coef))
+        self._stepped = stepped
         self.steps += 1
 
     def moments(self):

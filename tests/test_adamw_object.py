@@ -63,3 +63,54 @@ def test_copies_taken_away_and_given(calls, bits):
     assert opt.steps == 5 and len(_steps(calls)) == 5
     for x, w in zip(p, _steps(calls)[-1][1]):
         assert w["p"] == x.data_ptr() and w["n"] == x.numel()
+
+
+def _counts(calls, params):
+    """Parameter -> its step, of the calls made for one step; no parameter is in two of them."""
+    out = {}
+    for args, words in _steps(calls):
+        for i, w in enumerate(words):
+            if w["n"]:
+                assert i not in out and w["n"] == params[i].numel() and w["g"]
+                out[i] = args[5].step
+    calls.clear()
+    return out
+
+
+def test_left_out_parameters_keep_their_count(calls):
+    """The bias correction of a parameter goes by the steps that its moments have taken."""
+    p, g = _params(), _grads()
+    opt = reqat.AdamW(p, 1e-3)
+    opt.step(g)
+    assert _counts(calls, p) == {0: 1, 1: 1, 2: 1}
+    for k in range(2, 6):
+        opt.step([g[0], None, g[2]])
+        assert _counts(calls, p) == {0: k, 2: k}
+    opt.step(g)
+    assert _counts(calls, p) == {0: 6, 1: 2, 2: 6}
+    opt.step([None, None, None])
+    assert _counts(calls, p) == {}
+    opt.step([None, g[1], g[2]])
+    assert _counts(calls, p) == {1: 3, 2: 7}
+    opt.step(g)
+    assert _counts(calls, p) == {0: 7, 1: 4, 2: 8} and opt.steps == 9 and opt.missed == [2, 5, 1]
+    other = copy.deepcopy(opt)
+    other.step(g)
+    assert _counts(calls, other.params) == {0: 8, 1: 5, 2: 9} and opt.steps == 9
+    opt.steps, opt.missed = 100, [0, 0, 40]
+    opt.step(g)
+    assert _counts(calls, p) == {0: 101, 1: 101, 2: 61}
+
+
+def test_captured_steps_have_one_count(calls):
+    """On the device one count serves all parameters, so all steps have gradients for the same."""
+    p, g = _params(), _grads()
+    opt = reqat.AdamW(p, 1e-3, captured=True)
+    opt.step([None] * 3)                                  # moves nothing and counts nothing
+    assert not calls and opt.steps == 0
+    opt.step([g[0], None, g[2]])
+    assert [c[0] for c in calls] == ["reqat_adamw_coefficients", "reqat_adamw_step"]
+    assert [w["n"] for w in calls[1][2]] == [10, 0, 7]
+    for wrong in (g, [g[0], g[1], None], [None] * 3):
+        with pytest.raises(ValueError):
+            opt.step(wrong)
