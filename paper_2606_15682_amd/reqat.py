@@ -1341,7 +1341,7 @@ class AdamW:
     ``eps`` and ``weight_decay`` may be assigned between steps.
 
     captured=True is for steps in a HIP graph: the count is ``step_tensor`` (int32) and the rate ``lr_tensor`` (float32),
-    on the device, the count rising with every replay.  It is one count for
+    on the device, the count rising with every replay (``steps`` counts the steps outside of graphs).  It is one count for
     all: the first step says which parameters have gradients, and every later one has them for the same.  Parameters,
     copies, states and gradients of a captured step stay where they are."""
 
@@ -1497,7 +1497,9 @@ class AdamW:
         _call(reqat_adamw_step, self.device, self._tensors, len(grads), _FLOATS[self.dtype], _FLOATS[kind], self.state_bits,
               hyper, _ptr(grad_scale), _ptr(self._coef))
         self._stepped = stepped
-        self.steps += 1
+        with torch.cuda.device(self.device):
+            if not torch.cuda.is_current_stream_capturing():
+                self.steps += 1
 
     def moments(self):
         """The values of m and v as float32 buffers laid out like them (the states themselves when they have 32 bits)."""

@@ -1,4 +1,5 @@
 """AdamW's host side on CPU tensors, with the C calls recorded instead of made: what a step hands over."""
+import contextlib
 import copy
 
 import pytest
@@ -102,8 +103,12 @@ def test_left_out_parameters_keep_their_count(calls):
     assert _counts(calls, p) == {0: 101, 1: 101, 2: 61}
 
 
-def test_captured_steps_have_one_count(calls):
-    """On the device one count serves all parameters, so all steps have gradients for the same."""
+def test_captured_steps_have_one_count(calls, monkeypatch):
+    """On the device one count serves all parameters, so all steps have gradients for the same; what a capture records has
+    not run and is not counted."""
+    capturing = [False]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
     p, g = _params(), _grads()
     opt = reqat.AdamW(p, 1e-3, captured=True)
     opt.step([None] * 3)                                  # moves nothing and counts nothing
@@ -114,3 +119,6 @@ def test_captured_steps_have_one_count(calls):
     for wrong in (g, [g[0], g[1], None], [None] * 3):
         with pytest.raises(ValueError):
             opt.step(wrong)
+    capturing[0] = True
+    opt.step([g[0], None, g[2]])
+    assert len(calls) == 4 and opt.steps == 1

@@ -66,7 +66,7 @@ def test_captured_steps_count_replays():
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         opt.step(g)
-    assert int(opt.step_tensor) == 1
+    assert opt.steps == 1 and int(opt.step_tensor) == 1
     for k in range(2, 5):
         graph.replay()
         assert int(opt.step_tensor) == k and not p[1].any()
