@@ -16,6 +16,7 @@ from __future__ import annotations
 import array
 import ctypes
 import functools
+import operator
 import os
 
 import torch
@@ -1328,6 +1329,10 @@ def embedding_backward(dy, ids, rows, scale=1.0, out=None, accumulate=False, out
     return out
 
 
+def _same_objects(a, b):
+    return len(a) == len(b) and all(map(operator.is_, a, b))
+
+
 class AdamW:
     """AdamW over many tensors in few launches, with states in 32 or 8 bits.
 
@@ -1386,6 +1391,9 @@ class AdamW:
             at += [0 if c is None else c.data_ptr() for c in self.copies]
         return array.array("q", at)
 
+    def _tensors_now(self):
+        return [*self.params, *(self.copies or ())]
+
     def _adopt(self):
         """Checks parameters and copies and holds on to their memory, so that an address that stays is theirs."""
         spans, held = [], []
@@ -1405,7 +1413,7 @@ class AdamW:
         spans.sort()
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("parameters and copies must not overlap")
-        self._held, self._addresses = held, self._addresses_now()
+        self._held, self._addresses, self._seen = held, self._addresses_now(), self._tensors_now()
 
     def _place_states(self, bases):
         """Checks the states' buffers and enters their addresses: at the first step, and when one was replaced."""
@@ -1421,7 +1429,11 @@ class AdamW:
             if self.state_bits == 8:
                 self._tensors[8 * i + 4] = bases[2] + at // 32
                 self._tensors[8 * i + 5] = bases[3] + at // 32
-        self._bases = bases
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                       for t in (self.m, self.v, self.m_scale, self.v_scale) if t is not None and t.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("the states' buffers must not overlap")
+        self._bases, self._seen_states = bases, [self.m, self.v, self.m_scale, self.v_scale]
         self._held_states = [t if t is None else t.detach() for t in (self.m, self.v, self.m_scale, self.v_scale)]
 
     def _tensor_arg(self, t, shape, dtypes, name):
@@ -1455,10 +1467,12 @@ class AdamW:
                     and g.device == dev and g.is_contiguous()):
                 self._tensor_arg(g, shape, (kind,) if kind in _FLOATS else tuple(_FLOATS), "grads[%d]" % i)
             at.append(g.data_ptr())
-        if self._addresses_now() != self._addresses:     # a tensor that was given other memory
+        # another tensor, perhaps in the same memory, or one that was given other memory
+        if not _same_objects(self._tensors_now(), self._seen) or self._addresses_now() != self._addresses:
             self._adopt()
-        bases = [0 if t is None else t.data_ptr() for t in (self.m, self.v, self.m_scale, self.v_scale)]
-        if bases != self._bases:
+        states = [self.m, self.v, self.m_scale, self.v_scale]
+        bases = [0 if t is None else t.data_ptr() for t in states]
+        if bases != self._bases or not _same_objects(states, self._seen_states):
             self._place_states(bases)
         tensors, count = self._tensors, len(at)
         tensors[0::8] = self._addresses[:count]

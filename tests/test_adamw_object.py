@@ -122,3 +122,34 @@ def test_captured_steps_have_one_count(calls, monkeypatch):
     capturing[0] = True
     opt.step([g[0], None, g[2]])
     assert len(calls) == 4 and opt.steps == 1
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_other_tensors_in_the_same_memory_are_checked(calls, bits):
+    """A replaced tensor is checked also where it begins at the address of the one before it."""
+    p, g = _params(), _grads()
+    opt = reqat.AdamW(p, 1e-3, state_bits=bits, copies=[torch.empty(10, dtype=torch.bfloat16), None, None])
+    opt.step(g)
+    for name, wrong in (("params", p[0][:5]), ("params", p[0].view(2, 5)), ("params", p[0].view(torch.int32)),
+                        ("copies", opt.copies[0][:9]), ("copies", opt.copies[0].view(torch.float16))):
+        held = getattr(opt, name)
+        kept, held[0] = held[0], wrong
+        with pytest.raises((TypeError, ValueError)):
+            opt.step(g)
+        held[0] = kept
+    for name in ("m", "v", "m_scale", "v_scale")[:2 if bits == 32 else 4]:
+        kept = getattr(opt, name)
+        for wrong in (kept[:1], kept.view(torch.int32 if bits == 32 or "scale" in name else torch.int8), None):
+            setattr(opt, name, wrong)
+            with pytest.raises((TypeError, ValueError)):
+                opt.step(g)
+        setattr(opt, name, kept)
+    kept, opt.v = opt.v, opt.m                            # one buffer for both
+    with pytest.raises(ValueError):
+        opt.step(g)
+    opt.v, opt.copies = kept, None
+    opt.step(g)
+    opt.params[0] = p[0][:5]
+    with pytest.raises(ValueError):
+        opt.step(g)
+    assert opt.steps == 2 and len(_steps(calls)) == 2
