@@ -1154,6 +1154,11 @@ def _float_out(t, rows, cols, dtype, device, name):
     return t, ld
 
 
+def _written(*given):
+    """Tells autograd that a caller's tensors hold something else now: a graph that keeps one refuses its backward pass."""
+    torch.autograd.graph.increment_version(given)
+
+
 def _vector(t, n, device, name, dtypes=(torch.float32,)):
     """A contiguous vector of n numbers (the whole check first: small calls are short)."""
     if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == (n,) and t.device == device and t.is_contiguous():
@@ -1194,7 +1199,7 @@ def _policy_loss(logits, targets, old_logp, advantages, ref_logp, weights, clip_
         raise ValueError("kl_coef without ref_logp")
     if weights is not None:
         _vector(weights, T, dev, "weights")
-    ldg = 0
+    ldg, given = 0, out
     if grad:
         out, ldg = _float_out(out, T, V, logits.dtype, dev, "out")
     _require_cuda(logits, "logits")
@@ -1205,6 +1210,8 @@ def _policy_loss(logits, targets, old_logp, advantages, ref_logp, weights, clip_
     _call(reqat_policy_loss, dev, logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), old_logp.data_ptr(),
           advantages.data_ptr(), _ptr(ref_logp), _ptr(weights), clip_low, clip_high, kl_coef, temperature, stats.data_ptr(),
           loss.data_ptr(), _ptr(out) if grad else None, ldg, _ptr(ws))
+    if given is not None:
+        _written(given)
     return loss, stats, out
 
 
@@ -1239,10 +1246,13 @@ def policy_loss_backward(logits, targets, stats, temperature=1.0, grad_loss=None
     _index_arg(stats, (T, 4), torch.float32, dev, "stats")
     if grad_loss is not None:
         _scale_arg(grad_loss, NVFP4, dev, "grad_loss")
+    given = out
     out, ldg = _float_out(out, T, V, logits.dtype, dev, "out")
     _require_cuda(logits, "logits")
     _call(reqat_policy_loss_backward, dev, logits.data_ptr(), dt, T, V, ld, targets.data_ptr(), stats.data_ptr(),
           temperature, _ptr(grad_loss), out.data_ptr(), ldg)
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -1260,6 +1270,8 @@ def layer_norm(x, weight, bias=None, eps=1e-6, center=True, out=None):
     _require_cuda(x, "x")
     _call(reqat_layer_norm, dev, x.data_ptr(), dt, rows, cols, ldx, weight.data_ptr(), _ptr(bias), _dtype_arg(weight.dtype),
           eps, 1 if center else 0, y.data_ptr(), ldy, stats.data_ptr())
+    if out is not None:
+        _written(out)
     return y, stats
 
 
@@ -1287,6 +1299,8 @@ def layer_norm_backward(dy, x, weight, stats, center=True, bias=False, out=None,
     _call(reqat_layer_norm_backward, dev, dy.data_ptr(), lddy, x.data_ptr(), ldx, dt, rows, cols, weight.data_ptr(),
           _dtype_arg(weight.dtype), stats.data_ptr(), 1 if center else 0, dx.data_ptr(), lddx, dw.data_ptr(), _ptr(db),
           ws.data_ptr())
+    if out is not None:
+        _written(out)
     return dx, dw, db
 
 
@@ -1296,11 +1310,13 @@ def embedding(ids, table, scale=1.0, out=None):
     V, D, ld, dt = _float_rows(table, "table")
     if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
         raise TypeError("ids must be a 1-D int32 tensor")
-    T, dev = ids.shape[0], table.device
+    T, dev, given = ids.shape[0], table.device, out
     _vector(ids, T, dev, "ids", (torch.int32,))
     out, ldo = _float_out(out, T, D, table.dtype, dev, "out")
     _require_cuda(table, "table")
     _call(reqat_embedding, dev, ids.data_ptr(), T, table.data_ptr(), dt, V, D, ld, scale, out.data_ptr(), ldo)
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -1316,7 +1332,7 @@ def embedding_backward(dy, ids, rows, scale=1.0, out=None, accumulate=False, out
         raise ValueError("accumulate needs out")
     if out_dtype is None:
         out_dtype = dy.dtype if out is None else out.dtype
-    out_dt = _dtype_arg(out_dtype)
+    out_dt, given = _dtype_arg(out_dtype), out
     out, ld = _float_out(out, rows, D, out_dtype, dev, "out")
     need = _embedding_workspace(T, rows, D)
     if ws is not None:
@@ -1326,6 +1342,8 @@ def embedding_backward(dy, ids, rows, scale=1.0, out=None, accumulate=False, out
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
     _call(reqat_embedding_backward, dev, dy.data_ptr(), dt, lddy, ids.data_ptr(), T, rows, D, scale, out.data_ptr(), out_dt,
           ld, 1 if accumulate else 0, _ptr(ws))
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -1481,6 +1499,7 @@ class AdamW:
         _require_cuda(self.params[0], "params[0]")
         if self._coef is not None:
             self._step_captured(grads, kind, sizes, grad_scale)
+            self._step_written(grads)
             return
         missed = self.missed
         if not any(missed):
@@ -1494,6 +1513,13 @@ class AdamW:
         if sizes is not self._sizes:
             self.missed = [k + (g is None) for k, g in zip(missed, grads)]
         self.steps += 1
+        self._step_written(grads)
+
+    def _step_written(self, grads):
+        written = [p for p, g in zip(self.params, grads) if g is not None]
+        if self.copies is not None:
+            written += [c for c, g in zip(self.copies, grads) if c is not None and g is not None]
+        _written(*written)
 
     def _hyper(self, step):
         return AdamwHyper(self.lr, *self.betas, self.eps, self.weight_decay, step)
