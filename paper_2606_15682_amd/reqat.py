@@ -1100,6 +1100,29 @@ class FakeQuantSTE(torch.autograd.Function):
         return gy, None
 
 
+class _Once(torch.autograd.Function):
+    """Gradients of a kernel as functions of the tensors that they depend on, without a derivative of their own."""
+
+    @staticmethod
+    def forward(ctx, name, count, *tensors):
+        ctx.name = name
+        return tuple(t.view_as(t) for t in tensors[:count])
+
+    @staticmethod
+    def backward(ctx, *g):
+        raise RuntimeError("%s has no second derivative" % ctx.name)
+
+
+def _once(name, grads, *depends):
+    """The gradients that a backward pass returns.  Under create_graph they are tied to what they were computed from, so that
+    a derivative of them is refused; they would count as constants, and it would silently lack their part."""
+    if not torch.is_grad_enabled():
+        return grads
+    new = [t for t in grads if t is not None]
+    tied = iter(_Once.apply(name, len(new), *new, *depends))
+    return tuple(None if t is None else next(tied) for t in grads)
+
+
 class SemLoss(torch.autograd.Function):
     """The SEM loss as an autograd function over bfloat16 logits."""
 
@@ -1113,8 +1136,8 @@ class SemLoss(torch.autograd.Function):
     @staticmethod
     def backward(ctx, g):
         logits, targets, stats, weights = ctx.saved_tensors
-        grad = sem_loss_backward(logits, targets, stats, weights, ctx.lam, scale=float(g), out_dtype=logits.dtype)
-        return grad, None, None, None
+        grad = sem_loss_backward(logits, targets, stats, weights, ctx.lam, scale=float(g.detach()), out_dtype=logits.dtype)
+        return _once("SemLoss", (grad,), g, logits) + (None,) * 3
 
 
 # ------------------------------------------------------------------ the operators around the quantized layers
@@ -1572,7 +1595,7 @@ class PolicyLoss(torch.autograd.Function):
     def backward(ctx, g):
         logits, targets, stats = ctx.saved_tensors
         grad = policy_loss_backward(logits, targets, stats, ctx.temperature, g.reshape(1).to(torch.float32))
-        return (grad,) + (None,) * 9
+        return _once("PolicyLoss", (grad,), g, logits) + (None,) * 9
 
 
 class LayerNorm(torch.autograd.Function):
@@ -1589,7 +1612,7 @@ class LayerNorm(torch.autograd.Function):
     def backward(ctx, dy):
         x, weight, stats = ctx.saved_tensors
         dx, dw, db = layer_norm_backward(_dense_rows(dy), x, weight, stats, ctx.center, ctx.bias)
-        return dx, dw, db, None, None
+        return _once("LayerNorm", (dx, dw, db), dy, x, weight) + (None, None)
 
 
 class Embedding(torch.autograd.Function):
@@ -1604,7 +1627,8 @@ class Embedding(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         ids, = ctx.saved_tensors
-        return None, embedding_backward(_dense_rows(dy), ids, ctx.rows, ctx.scale), None
+        dtable = embedding_backward(_dense_rows(dy), ids, ctx.rows, ctx.scale)
+        return (None,) + _once("Embedding", (dtable,), dy) + (None,)
 
 
 def _dense_rows(g):
