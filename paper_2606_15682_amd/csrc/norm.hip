@@ -168,7 +168,8 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_forward_kernel(NormArg
             for (int e = 0; e < N; ++e) {
                 x[v][e] -= mu;
                 const bool in = WHOLE ? p.counts(v, e) : (v * G + i) * N + e < K;
-                s[0] = __builtin_fmaf(in ? x[v][e] : 0.0f, x[v][e], s[0]);
+                const float d = in ? x[v][e] : 0.0f;    // both factors: an element read once more may be infinite
+                s[0] = __builtin_fmaf(d, d, s[0]);
             }
         sum(s);
         const float rstd = 1.0f / sqrtf(s[0] * inv + a.eps);
