@@ -55,7 +55,7 @@ static reqat_status check_policy(const void *logits, reqat_dtype dtype, int64_t 
 
 static void set_temperature(PolicyArgs &a, float temperature) {
     a.c = (float)(1.4426950408889634074 / (double)temperature);
-    a.inv_temp = (float)(1.0 / (double)temperature);
+    a.temp = temperature;
 }
 
 size_t reqat_policy_loss_workspace_bytes(reqat_dtype dtype, int64_t T, int64_t V) {

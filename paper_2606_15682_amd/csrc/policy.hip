@@ -4,10 +4,9 @@
 //   dL/dlp = w_t (-A r [inside] - kl (exp(x) - 1)),  inside: neither A > 0, r > 1 + high nor A < 0, r < 1 - low,
 //   dL/dz_j = (dL/dlp) ([j = y] - p_j) / temperature.
 //
-// Softmax statistics relative to a reference: the largest logit, scaled.  bfloat16 rows: in base-2 units, c = log2(e) /
-// temperature, reference c max z, t = c z - reference in one fused multiply-add (8 half steps of c z at most, beside a
-// rounding to bfloat16).  FP32 rows: z / temperature is rounded, the reference taken off it, and the difference brought to
-// base 2, so that the likely tokens, whose 1 - p is small, keep FP32's digits.  S = sum 2^t in both.
+// Softmax statistics relative to the largest logit m: terms 2^t, t = (z - m) c, c = log2(e) / temperature, S their sum.  The
+// difference comes first: it is exact for the likely tokens, whose 1 - p is small, costs no digits where all logits are large,
+// and keeps its meaning up to the type's largest and lowest values, where c z is past FP32's range.
 #include "internal.h"
 #include "row_io.h"
 
@@ -18,17 +17,13 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kMaxHeld = 18;
 
-// The scaled logit that references are measured in, and the base-2 exponent of a logit.
-template <typename T> __device__ __forceinline__ float scaled(const PolicyArgs &a, float z) { return z * (sizeof(T) == 4 ? a.inv_temp : a.c); }
-template <typename T> __device__ __forceinline__ float base2(float d) { return sizeof(T) == 4 ? d * kLog2e : d; }
-template <typename T> __device__ __forceinline__ float exponent(const PolicyArgs &a, float z, float ref) {
-    return sizeof(T) == 4 ? (z * a.inv_temp - ref) * kLog2e : __builtin_fmaf(z, a.c, -ref);
-}
-
-// Running maximum and sum of a slice of a row; empty: m = -Inf, ref = 0, S = 0, and so for a slice of -Inf logits alone.
+// Running maximum and sum of a slice of a row; empty, and so for a slice of -Inf logits alone: m = -Inf, S = 0.
 struct Online {
-    float m, ref, S;
+    float m, S;
 };
+
+// What exponents are relative to: the maximum, or a number that leaves -Inf what it is.
+__device__ __forceinline__ float reference(float m) { return __builtin_fmaxf(m, -3.402823466e38f); }
 
 // A NaN logit makes S NaN, and so does +Inf (Inf - Inf): the row's statistics are NaN then.
 template <typename T> __device__ __forceinline__ void add(Online &o, const PolicyArgs &a, uint4 v) {
@@ -39,32 +34,30 @@ template <typename T> __device__ __forceinline__ void add(Online &o, const Polic
 #pragma unroll
     for (int i = 1; i < N; ++i) mx = __builtin_fmaxf(mx, z[i]);
     if (mx > o.m) {
-        const float ref = scaled<T>(a, mx);
-        if (o.S != 0.0f) o.S *= __builtin_amdgcn_exp2f(base2<T>(o.ref - ref));
+        if (o.S != 0.0f) o.S *= __builtin_amdgcn_exp2f((o.m - mx) * a.c);
         o.m = mx;
-        o.ref = ref;
     }
+    const float ref = reference(o.m);
 #pragma unroll
-    for (int i = 0; i < N; ++i) o.S += __builtin_amdgcn_exp2f(exponent<T>(a, z[i], o.ref));
+    for (int i = 0; i < N; ++i) o.S += __builtin_amdgcn_exp2f((z[i] - ref) * a.c);
 }
 
-template <typename T> __device__ __forceinline__ Online merge(Online a, Online b) {
+__device__ __forceinline__ Online merge(const PolicyArgs &args, Online a, Online b) {
     if (b.m > a.m) { const Online t = a; a = b; b = t; }
     if (b.S == 0.0f) return a;
-    a.S += b.S * __builtin_amdgcn_exp2f(base2<T>(b.ref - a.ref));
+    a.S += b.S * __builtin_amdgcn_exp2f((b.m - a.m) * args.c);
     return a;
 }
 
 // The workgroup's TH slices in a fixed order: within the wave, then wave by wave.
-template <typename T, int TH> __device__ __forceinline__ Online join(Online o, Online (&red)[TH / 64]) {
+template <int TH> __device__ __forceinline__ Online join(const PolicyArgs &a, Online o, Online (&red)[TH / 64]) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
-        o = merge<T>(o, Online{__shfl_xor(o.m, off, 64), __shfl_xor(o.ref, off, 64), __shfl_xor(o.S, off, 64)});
+    for (int off = 32; off > 0; off >>= 1) o = merge(a, o, Online{__shfl_xor(o.m, off, 64), __shfl_xor(o.S, off, 64)});
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = o;
     __syncthreads();
     o = red[0];
 #pragma unroll
-    for (int k = 1; k < TH / 64; ++k) o = merge<T>(o, red[k]);
+    for (int k = 1; k < TH / 64; ++k) o = merge(a, o, red[k]);
     return o;
 }
 
@@ -138,30 +131,23 @@ template <typename T> __device__ __forceinline__ RowInputs row_inputs(const Poli
 }
 
 // lp, log-sum-exp, dL/dlp and r of a row.
-template <typename T> __device__ __forceinline__ float4 row_stats(const PolicyArgs &a, const RowInputs &in, Online o) {
-    const float log2S = __builtin_amdgcn_logf(o.S);
-    float lp, lse;
-    if (sizeof(T) == 4) {
-        lp = (in.zy * a.inv_temp - o.ref) - log2S * kLn2;
-        lse = o.ref + log2S * kLn2;
-    } else {
-        lp = (__builtin_fmaf(in.zy, a.c, -o.ref) - log2S) * kLn2;
-        lse = (o.ref + log2S) * kLn2;
-    }
+__device__ __forceinline__ float4 row_stats(const PolicyArgs &a, const RowInputs &in, Online o) {
+    const float ref = reference(o.m), lnS = __builtin_amdgcn_logf(o.S) * kLn2;
+    const float lp = (in.zy - ref) / a.temp - lnS, lse = ref / a.temp + lnS;
     const float r = expf(lp - in.old);
     float slope = outside(a, r, in.adv) ? 0.0f : -in.adv * r;
     if (a.ref && a.kl != 0.0f) slope -= a.kl * expm1f(in.ref - lp);      // not 0 times Inf
     return make_float4(lp, lse, in.w * slope, r);
 }
 
-// dL/dz of a vector whose first element is j: f [j = y] - fs 2^t.
+// dL/dz of a vector whose first element is j: f [j = y] - fs 2^t, t = (z - ref) c.
 template <typename T>
 __device__ __forceinline__ uint4 grad_vec(const PolicyArgs &a, uint4 v, float ref, float fs, float f, int32_t j, int32_t y) {
     constexpr int N = kVec<T>;
     float z[N];
     unpack<T>(v, z);
 #pragma unroll
-    for (int i = 0; i < N; ++i) z[i] = -fs * __builtin_amdgcn_exp2f(exponent<T>(a, z[i], ref));
+    for (int i = 0; i < N; ++i) z[i] = -fs * __builtin_amdgcn_exp2f((z[i] - ref) * a.c);
     if ((uint32_t)(y - j) < (uint32_t)N) {
 #pragma unroll
         for (int i = 0; i < N; ++i) z[i] += j + i == y ? f : 0.0f;
@@ -207,7 +193,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_rows_ke
     }
     const T *row = reinterpret_cast<const T *>(a.logits) + t * a.ld;
     const RowInputs in = row_inputs(a, t, row);
-    Online o{-__builtin_inff(), 0.0f, 0.0f};
+    Online o{-__builtin_inff(), 0.0f};
     const int64_t V = a.V;
     int64_t j = (int64_t)threadIdx.x * N;
     for (; j + 3 * kStep + N <= V; j += 4 * kStep) {
@@ -219,8 +205,8 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_rows_ke
     }
     for (; j < V; j += kStep) add<T>(o, a, load_at(row, (int32_t)V, (int32_t)j));
     __shared__ Online red[kThreads / 64];
-    o = join<T, kThreads>(o, red);
-    if (threadIdx.x == 0) reinterpret_cast<float4 *>(a.stats)[t] = row_stats<T>(a, in, o);
+    o = join<kThreads>(a, o, red);
+    if (threadIdx.x == 0) reinterpret_cast<float4 *>(a.stats)[t] = row_stats(a, in, o);
 }
 
 // Vector v as it came, after x is known: without this the compiler unpacks all vectors of a row first, or keeps the unpacked
@@ -266,19 +252,19 @@ template <typename T, int TH, int NV> __global__ __launch_bounds__(TH) void poli
         if (v < NV - 1 || last) buf[v] = load_vec(reinterpret_cast<const char *>(row) + v * kBytes + lane);
     while (true) {
         const int32_t y = in.y;
-        Online o{-__builtin_inff(), 0.0f, 0.0f};
+        Online o{-__builtin_inff(), 0.0f};
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             pin(buf[v], o.S);
             if (v < NV - 1 || last) add<T>(o, a, buf[v]);
         }
         for (int32_t j = j0 + rest; j < V; j += kStep) add<T>(o, a, load_at(row, V, j));
-        o = join<T, TH>(o, red[half]);
+        o = join<TH>(a, o, red[half]);
         half ^= 1;                                      // the other half is written before this one is again
-        o.ref = uniform(o.ref);
-        const float4 s = row_stats<T>(a, in, o);
+        const float ref = uniform(reference(o.m));
+        const float4 s = row_stats(a, in, o);
         if (threadIdx.x == 0) reinterpret_cast<float4 *>(a.stats)[t] = s;
-        const float f = uniform(s.z * a.inv_temp), fs = uniform(f / o.S);
+        const float f = uniform(s.z / a.temp), fs = uniform(f / o.S);
         T *out = grad + t * a.ldg;
         const int64_t next = seek(t + gridDim.x);
         const bool more = next < a.T;
@@ -288,37 +274,70 @@ template <typename T, int TH, int NV> __global__ __launch_bounds__(TH) void poli
         in = row_inputs(a, more ? next : t, ahead);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            pin(buf[v], o.ref);
+            pin(buf[v], ref);
             if (v < NV - 1 || last) {
-                store_vec_once(reinterpret_cast<char *>(out) + v * kBytes + lane, grad_vec<T>(a, buf[v], o.ref, fs, f, j0 + v * kStep, y));
+                store_vec_once(reinterpret_cast<char *>(out) + v * kBytes + lane, grad_vec<T>(a, buf[v], ref, fs, f, j0 + v * kStep, y));
                 buf[v] = load_vec(reinterpret_cast<const char *>(ahead) + v * hop + lane);
             }
         }
-        write_grad<T, TH>(a, row, out, rest, V, o.ref, fs, f, y);
+        write_grad<T, TH>(a, row, out, rest, V, ref, fs, f, y);
         if (!more) return;
         t = next;
         row = ahead;
     }
 }
 
-// The gradient from the statistics: a workgroup per row and slice of it.
-template <typename T> __global__ __launch_bounds__(kThreads) void policy_backward_kernel(PolicyArgs a, int64_t slice) {
-    const int64_t t = blockIdx.x, begin = (int64_t)blockIdx.y * slice, end = begin + slice < a.V ? begin + slice : a.V;
+// The gradient from the statistics: a workgroup per row and slice of it.  p_j = 2^((z_j - z_y) c + lp log2(e)) or 2^(z_j c -
+// lse log2(e)), by the smaller of |lp| and |lse|, whose rounding is the exponent's error; dL/dz_y = -f (exp(lp) - 1).
+// hold: z_y has to stay for the row's other workgroups, where grad takes the logits' place; a launch of its own follows.
+template <typename T> __global__ __launch_bounds__(kThreads) void policy_backward_kernel(PolicyArgs a, int64_t slice, bool hold) {
+    constexpr int N = kVec<T>;
+    const int64_t t = blockIdx.x;
+    const int32_t begin = (int32_t)(blockIdx.y * slice), end = (int32_t)(begin + slice < a.V ? begin + slice : a.V);
     const T *row = reinterpret_cast<const T *>(a.logits) + t * a.ld;
     T *out = reinterpret_cast<T *>(a.grad) + t * a.ldg;
-    const float lse = a.stats[4 * t + 1], slope = a.stats[4 * t + 2];
-    if (slope == 0.0f) {                                   // no weight, or clipped without a KL term: nothing to read
-        write_zeros<T, kThreads>(out, (int32_t)begin, (int32_t)end);
+    const float4 s = reinterpret_cast<const float4 *>(a.stats)[t];
+    if (s.z == 0.0f) {                                     // no weight, or clipped without a KL term: nothing to read
+        write_zeros<T, kThreads>(out, begin, end);
         return;
     }
-    const float f = slope * a.inv_temp * (a.grad_loss ? a.grad_loss[0] : 1.0f);
-    float ref = lse, fs = f;
-    if (sizeof(T) == 2) {
-        // lse log2(e) as a rounded number and what it leaves, which joins the factor
-        ref = lse * kLog2e;
-        fs *= __builtin_amdgcn_exp2f(-(__builtin_fmaf(lse, kLog2e, -ref) + lse * 1.925963033500e-8f));
+    const int32_t y = a.targets[t];
+    const float f = s.z / a.temp * (a.grad_loss ? a.grad_loss[0] : 1.0f), fy = -f * expm1f(s.x);
+    const bool by_target = __builtin_fabsf(s.x) < __builtin_fabsf(s.y) && y >= 0 && y < a.V;
+    const float base = by_target ? to_f32(row[y]) : 0.0f, shift = (by_target ? s.x : -s.y) * kLog2e;
+    if (!hold) __syncthreads();                            // all have read z_y
+    for (int32_t j = begin + (int32_t)threadIdx.x * N; j < end; j += kThreads * N) {
+        float z[N];
+        unpack<T>(load_at(row, end, j), z);
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = -f * __builtin_amdgcn_exp2f(__builtin_fmaf(z[i] - base, a.c, shift));
+        const bool here = (uint32_t)(y - j) < (uint32_t)N;
+        if (here) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] = j + i == y ? fy : z[i];
+        }
+        if (here && hold) {
+            T e[N];
+            const uint4 v = pack<T>(z);
+            __builtin_memcpy(e, &v, 16);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (j + i < end && j + i != y) out[j + i] = e[i];
+        } else {
+            store_at(out, end, j, pack<T>(z));
+        }
     }
-    write_grad<T, kThreads>(a, row, out, (int32_t)begin, (int32_t)end, ref, fs, f, a.targets[t]);
+}
+
+// The targets' elements, a thread each, where the rows were held.
+template <typename T> __global__ __launch_bounds__(kThreads) void policy_backward_targets_kernel(PolicyArgs a) {
+    const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (t >= a.T) return;
+    const float4 s = reinterpret_cast<const float4 *>(a.stats)[t];
+    const int32_t y = a.targets[t];
+    if (s.z == 0.0f || y < 0 || y >= a.V) return;
+    const float f = s.z / a.temp * (a.grad_loss ? a.grad_loss[0] : 1.0f);
+    reinterpret_cast<T *>(a.grad)[t * a.ldg + y] = from_f32<T>(-f * expm1f(s.x));
 }
 
 constexpr int kSumThreads = 1024;
@@ -374,25 +393,24 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_part_ke
     if (weight_of(a, t) == 0.0f) return;
     const int32_t V = (int32_t)a.V, begin = (int32_t)blockIdx.y * slice, end = V - begin < slice ? V : begin + slice;
     const T *row = reinterpret_cast<const T *>(a.logits) + t * a.ld;
-    Online o{-__builtin_inff(), 0.0f, 0.0f};
+    Online o{-__builtin_inff(), 0.0f};
 #pragma unroll 4
     for (int32_t j = begin + (int32_t)threadIdx.x * kVec<T>; j < end; j += kThreads * kVec<T>) add<T>(o, a, load_at(row, end, j));
     __shared__ Online red[kThreads / 64];
-    o = join<T, kThreads>(o, red);
+    o = join<kThreads>(a, o, red);
     if (threadIdx.x == 0) {
         const int32_t y = a.targets[t];
-        a.parts[t * gridDim.y + blockIdx.y] = make_float4(o.m, o.ref, o.S, y >= begin && y < end ? to_f32(row[y]) : __builtin_nanf(""));
+        a.parts[t * gridDim.y + blockIdx.y] = make_float4(o.m, o.S, y >= begin && y < end ? to_f32(row[y]) : __builtin_nanf(""), 0.0f);
     }
 }
 
 // A row's slices in their order, and its target's logit.
-template <typename T>
 __device__ __forceinline__ Online merge_parts(const PolicyArgs &a, int64_t t, int32_t slice, int slices, RowInputs &in) {
-    Online o{-__builtin_inff(), 0.0f, 0.0f};
+    Online o{-__builtin_inff(), 0.0f};
     for (int k = 0; k < slices; ++k) {
         const float4 p = a.parts[t * slices + k];
-        o = merge<T>(o, Online{p.x, p.y, p.z});
-        if (in.y >= 0 && in.y / slice == k) in.zy = p.w;      // NaN for a target behind the row's end
+        o = merge(a, o, Online{p.x, p.y});
+        if (in.y >= 0 && in.y / slice == k) in.zy = p.z;      // NaN for a target behind the row's end
     }
     return o;
 }
@@ -407,8 +425,8 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_finish_
             float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (w != 0.0f) {
                 RowInputs in = {w, a.old_logp[t], a.adv[t], a.ref ? a.ref[t] : 0.0f, __builtin_nanf(""), a.targets[t]};
-                const Online o = merge_parts<T>(a, t, slice, slices, in);
-                st = row_stats<T>(a, in, o);
+                const Online o = merge_parts(a, t, slice, slices, in);
+                st = row_stats(a, in, o);
                 add_terms(a, w, in.adv, in.ref, st.x, st.w, s);
             }
             reinterpret_cast<float4 *>(a.stats)[t] = st;
@@ -425,9 +443,9 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_finish_
         return;
     }
     RowInputs in = row_inputs(a, t);
-    const Online o = merge_parts<T>(a, t, slice, slices, in);
-    const float f = row_stats<T>(a, in, o).z * a.inv_temp;
-    write_grad<T, kThreads>(a, row, out, begin, end, o.ref, f / o.S, f, in.y);
+    const Online o = merge_parts(a, t, slice, slices, in);
+    const float f = row_stats(a, in, o).z / a.temp;
+    write_grad<T, kThreads>(a, row, out, begin, end, reference(o.m), f / o.S, f, in.y);
 }
 
 }  // namespace
@@ -487,9 +505,15 @@ hipError_t launch_policy_backward(const PolicyArgs &a, bool bf16, hipStream_t st
     int64_t slices = (2048 + a.T - 1) / a.T;
     slices = slices < units ? slices : units;
     const int64_t slice = (units + slices - 1) / slices * unit;
-    const dim3 grid((unsigned)a.T, (unsigned)((a.V + slice - 1) / slice)), block(kThreads);
-    if (bf16) hipLaunchKernelGGL(policy_backward_kernel<uint16_t>, grid, block, 0, stream, a, slice);
-    else hipLaunchKernelGGL(policy_backward_kernel<float>, grid, block, 0, stream, a, slice);
+    const int64_t cuts = (a.V + slice - 1) / slice;
+    const bool hold = cuts > 1 && a.grad == a.logits;
+    const dim3 grid((unsigned)a.T, (unsigned)cuts), block(kThreads), targets((unsigned)((a.T + kThreads - 1) / kThreads));
+    if (bf16) hipLaunchKernelGGL(policy_backward_kernel<uint16_t>, grid, block, 0, stream, a, slice, hold);
+    else hipLaunchKernelGGL(policy_backward_kernel<float>, grid, block, 0, stream, a, slice, hold);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !hold) return e;
+    if (bf16) hipLaunchKernelGGL(policy_backward_targets_kernel<uint16_t>, targets, block, 0, stream, a);
+    else hipLaunchKernelGGL(policy_backward_targets_kernel<float>, targets, block, 0, stream, a);
     return hipGetLastError();
 }
 
