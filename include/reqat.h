@@ -463,7 +463,7 @@ reqat_status reqat_sem_loss_backward(const void *logits, int64_t T, int64_t V, i
  *   workspace: reqat_policy_loss_workspace_bytes(dtype, T, V) bytes, 16-byte aligned
  *     (may be NULL when that is 0): statistics of the slices that few rows are cut into.
  * A logit of -Inf has probability 0; NaN or +Inf gives NaN for its row.
- * 0 <= clip_low <= 1, clip_high >= 0, temperature > 0 and finite
+ * 0 <= clip_low <= 1, clip_high >= 0, temperature at least 2^-126 and finite
  * (REQAT_E_UNSUPPORTED); T at most 2^22, V at most 2^30.  T == 0 writes a loss of zeros.
  */
 reqat_status reqat_policy_loss(const void *logits, reqat_dtype dtype, int64_t T, int64_t V, int64_t ld, const int32_t *targets,

@@ -41,7 +41,7 @@ static reqat_status check_policy(const void *logits, reqat_dtype dtype, int64_t 
     if (!dtype_ok(dtype)) return REQAT_E_ENUM;
     if (T < 0 || T > kMaxTokens || V <= 0 || V > (1 << 30) || ld < V || !span_ok(T, ld)) return REQAT_E_SHAPE;
     if (need_grad && (ldg < V || !span_ok(T, ldg))) return REQAT_E_SHAPE;
-    if (!(temperature > 0.0f) || isinf(temperature)) return REQAT_E_UNSUPPORTED;
+    if (!(temperature >= 1.17549435e-38f) || isinf(temperature)) return REQAT_E_UNSUPPORTED;   // 2^-126: log2(e) / temperature is finite
     if (T == 0) return REQAT_OK;
     if (!logits || !targets || !stats || (need_grad && !grad)) return REQAT_E_NULL;
     if (!aligned(logits, size_of(dtype)) || !aligned(targets, 4) || !aligned(stats, 16) || !aligned(grad, size_of(dtype)))
