@@ -389,34 +389,25 @@ __global__ __launch_bounds__(1024) void norm_params_kernel(NormArgs a, int64_t p
     }
 }
 
-template <typename T, int G> hipError_t launch(const NormArgs &a, const NormPlan &p, bool backward, hipStream_t stream) {
+// The kernel of G threads and V vectors each, or of fewer, down to the fewest that norm_plan gives G threads.
+template <typename T, int G, int V = norm_most_vectors(G)>
+hipError_t launch(const NormArgs &a, const NormPlan &p, bool backward, hipStream_t stream) {
+    if constexpr (V > norm_least_vectors(G)) {
+        if (p.vpt < V) return launch<T, G, V - 1>(a, p, backward, stream);
+    }
+    if (p.vpt != V) return hipErrorInvalidValue;
     constexpr int P = norm_groups(G);
-    const dim3 grid((unsigned)(backward ? p.backward : p.forward));
-    const bool whole = a.K >= kVec<T>;
+    const dim3 grid((unsigned)(backward ? p.backward : p.forward)), forward(G == 64 ? 256 : G);
     const size_t lds = P > 1 ? (size_t)a.K * 8 : 0;
-#define REQAT_NORM(V)                                                                                                          \
-    case V:                                                                                                                    \
-        if (backward && whole) hipLaunchKernelGGL((norm_backward_kernel<T, G, V, true>), grid, dim3(G * P), lds, stream, a);   \
-        else if (backward) hipLaunchKernelGGL((norm_backward_kernel<T, G, V, false>), grid, dim3(G * P), lds, stream, a);      \
-        else if (whole) hipLaunchKernelGGL((norm_forward_kernel<T, G, V, true>), grid, dim3(G == 64 ? 256 : G), 0, stream, a); \
-        else hipLaunchKernelGGL((norm_forward_kernel<T, G, V, false>), grid, dim3(G == 64 ? 256 : G), 0, stream, a);           \
-        break;
-    switch (p.vpt) {
-        REQAT_NORM(1)
-        REQAT_NORM(2)
-        REQAT_NORM(3)
-        REQAT_NORM(4)
-    default:
-        if constexpr (G == 512 || (G == 1024 && sizeof(T) == 4)) {
-            switch (p.vpt) {
-                REQAT_NORM(5)
-                REQAT_NORM(6)
-                REQAT_NORM(7)
-                REQAT_NORM(8)
-            }
+    if constexpr (G == 64 && V == 1) {                   // the one form for rows of less than a vector
+        if (a.K < kVec<T>) {
+            if (backward) hipLaunchKernelGGL((norm_backward_kernel<T, G, V, false>), grid, dim3(G * P), lds, stream, a);
+            else hipLaunchKernelGGL((norm_forward_kernel<T, G, V, false>), grid, forward, 0, stream, a);
+            return hipGetLastError();
         }
     }
-#undef REQAT_NORM
+    if (backward) hipLaunchKernelGGL((norm_backward_kernel<T, G, V, true>), grid, dim3(G * P), lds, stream, a);
+    else hipLaunchKernelGGL((norm_forward_kernel<T, G, V, true>), grid, forward, 0, stream, a);
     return hipGetLastError();
 }
 

@@ -9,9 +9,13 @@ constexpr int64_t kNormMaxCols = 32768;    // 512 threads of eight vectors of bf
 // Groups of G threads, a row each, that a workgroup of the backward pass has.
 constexpr int norm_groups(int G) { return G == 64 ? 4 : 1; }
 
+// Vectors of a row that a thread of such a group holds: the kernels that there are.
+constexpr int norm_least_vectors(int G) { return G == 64 ? 1 : (G == 256 ? 2 : (G == 512 ? 3 : 5)); }
+constexpr int norm_most_vectors(int G) { return G <= 256 ? 4 : 8; }
+
 struct NormPlan {
     int threads;                           // of a row's group: 64 (four groups a workgroup), 256, 512 or 1024
-    int vpt;                               // 16-byte vectors of a row a thread holds: 1 to 4, of 512 and 1024 threads to 8
+    int vpt;                               // 16-byte vectors of a row a thread holds
     int64_t forward, backward;             // workgroups
     bool columns;                          // dw and db by columns, in a launch of their own
     int64_t sums;                          // rows of partial sums of dw, and of db

@@ -458,7 +458,7 @@ template <typename T, int TH, int NV> void launch_grad_of(const PolicyArgs &a, i
     if (steps == NV) {
         const int64_t most = TH == 256 ? 4 * 256 : 256;
         hipLaunchKernelGGL((policy_grad_kernel<T, TH, NV>), dim3((unsigned)(a.T < most ? a.T : most)), dim3(TH), 0, stream, a);
-    } else if constexpr (NV > 0) {
+    } else if constexpr (NV > (TH == 256 ? 0 : 2)) {       // more than 1024 vectors are at least two of 1024 threads
         launch_grad_of<T, TH, NV - 1>(a, steps, stream);
     }
 }

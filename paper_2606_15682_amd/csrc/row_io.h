@@ -34,9 +34,6 @@ template <typename T> __device__ __forceinline__ void store_vec(T *p, uint4 v) {
 
 // The same for data that a call touches once: it is not kept in the caches.
 typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
-template <typename T> __device__ __forceinline__ uint4 load_vec_once(const T *p) {
-    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const Words *>(p)));
-}
 template <typename T> __device__ __forceinline__ void store_vec_once(T *p, uint4 v) {
     __builtin_nontemporal_store(__builtin_bit_cast(Words, v), reinterpret_cast<Words *>(p));
 }
