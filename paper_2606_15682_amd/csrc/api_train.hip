@@ -25,6 +25,7 @@ struct Rows {
     int64_t rows, cols, ld, size;
 };
 bool overlap(const Rows &a, const Rows &b) {
+    if (a.rows == 0 || b.rows == 0) return false;     // the strides of no rows may be anything
     return rows_overlap(a.p, a.rows, a.cols * a.size / 2, a.ld * a.size / 2, b.p, b.rows, b.cols * b.size / 2, b.ld * b.size / 2);
 }
 bool in_place(const Rows &a, const Rows &b) { return a.p == b.p && (a.ld == b.ld || a.rows == 1) && a.size == b.size; }
