@@ -54,9 +54,14 @@ static reqat_status check_policy(const void *logits, reqat_dtype dtype, int64_t 
     return REQAT_OK;
 }
 
-static void set_temperature(PolicyArgs &a, float temperature) {
-    a.c = (float)(1.4426950408889634074 / (double)temperature);
+static void set_temperature(PolicyArgs &a, float temperature, bool bf16) {
+    const double c = 1.4426950408889634074 / (double)temperature;
     a.temp = temperature;
+    a.c = (float)c;
+    if (bf16) return;
+    if ((double)a.c >= c) a.c = nextafterf(a.c, 0.0f);
+    const float rest = (float)(c - (double)a.c);
+    a.c_rest = rest > 0.0f ? rest : 1e-45f;              // never 0, which -Inf times would be NaN
 }
 
 size_t reqat_policy_loss_workspace_bytes(reqat_dtype dtype, int64_t T, int64_t V) {
@@ -85,7 +90,7 @@ reqat_status reqat_policy_loss(const void *logits, reqat_dtype dtype, int64_t T,
     a.low = (float)(1.0 - (double)clip_low);
     a.high = (float)(1.0 + (double)clip_high);
     a.kl = kl_coef;
-    set_temperature(a, temperature);
+    set_temperature(a, temperature, dtype == REQAT_DT_BF16);
     return launch_policy_loss(a, dtype == REQAT_DT_BF16, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? REQAT_OK : REQAT_E_HIP;
 }
 
@@ -98,7 +103,7 @@ reqat_status reqat_policy_loss_backward(const void *logits, reqat_dtype dtype, i
     PolicyArgs a = {};
     a.logits = logits; a.targets = targets; a.stats = const_cast<float *>(stats); a.grad_loss = grad_loss; a.grad = grad;
     a.T = T; a.V = V; a.ld = ld; a.ldg = ldg;
-    set_temperature(a, temperature);
+    set_temperature(a, temperature, dtype == REQAT_DT_BF16);
     return launch_policy_backward(a, dtype == REQAT_DT_BF16, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? REQAT_OK : REQAT_E_HIP;
 }
 

@@ -117,7 +117,8 @@ struct PolicyArgs {
     float4 *parts;                         // workspace: the statistics of policy_plan's slices
     int64_t T, V, ld, ldg;
     float default_weight, low, high;       // low, high: bounds of the ratio
-    float kl, temp, c;                     // c: log2(e) / temperature
+    float kl, temp;
+    float c, c_rest;                       // log2(e) / temperature: rounded; FP32: rounded down, and what that leaves, > 0
 };
 // The statistics and the loss, and the gradient where a.grad is not null.
 hipError_t launch_policy_loss(const PolicyArgs &a, bool bf16, hipStream_t stream);

@@ -17,6 +17,12 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kMaxHeld = 18;
 
+// The base-2 exponent of a difference d <= 0, which may be -Inf.  FP32 rows take what the factor's rounding leaves too: that
+// error is the same in every term, c_rest / c of the distance to the maximum, where the other roundings average out.
+template <typename T> __device__ __forceinline__ float exponent(const PolicyArgs &a, float d) {
+    return sizeof(T) == 4 ? __builtin_fmaf(d, a.c, d * a.c_rest) : d * a.c;
+}
+
 // Running maximum and sum of a slice of a row; empty, and so for a slice of -Inf logits alone: m = -Inf, S = 0.
 struct Online {
     float m, S;
@@ -34,30 +40,30 @@ template <typename T> __device__ __forceinline__ void add(Online &o, const Polic
 #pragma unroll
     for (int i = 1; i < N; ++i) mx = __builtin_fmaxf(mx, z[i]);
     if (mx > o.m) {
-        if (o.S != 0.0f) o.S *= __builtin_amdgcn_exp2f((o.m - mx) * a.c);
+        if (o.S != 0.0f) o.S *= __builtin_amdgcn_exp2f(exponent<T>(a, o.m - mx));
         o.m = mx;
     }
     const float ref = reference(o.m);
 #pragma unroll
-    for (int i = 0; i < N; ++i) o.S += __builtin_amdgcn_exp2f((z[i] - ref) * a.c);
+    for (int i = 0; i < N; ++i) o.S += __builtin_amdgcn_exp2f(exponent<T>(a, z[i] - ref));
 }
 
-__device__ __forceinline__ Online merge(const PolicyArgs &args, Online a, Online b) {
+template <typename T> __device__ __forceinline__ Online merge(const PolicyArgs &args, Online a, Online b) {
     if (b.m > a.m) { const Online t = a; a = b; b = t; }
     if (b.S == 0.0f) return a;
-    a.S += b.S * __builtin_amdgcn_exp2f((b.m - a.m) * args.c);
+    a.S += b.S * __builtin_amdgcn_exp2f(exponent<T>(args, b.m - a.m));
     return a;
 }
 
 // The workgroup's TH slices in a fixed order: within the wave, then wave by wave.
-template <int TH> __device__ __forceinline__ Online join(const PolicyArgs &a, Online o, Online (&red)[TH / 64]) {
+template <typename T, int TH> __device__ __forceinline__ Online join(const PolicyArgs &a, Online o, Online (&red)[TH / 64]) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) o = merge(a, o, Online{__shfl_xor(o.m, off, 64), __shfl_xor(o.S, off, 64)});
+    for (int off = 32; off > 0; off >>= 1) o = merge<T>(a, o, Online{__shfl_xor(o.m, off, 64), __shfl_xor(o.S, off, 64)});
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = o;
     __syncthreads();
     o = red[0];
 #pragma unroll
-    for (int k = 1; k < TH / 64; ++k) o = merge(a, o, red[k]);
+    for (int k = 1; k < TH / 64; ++k) o = merge<T>(a, o, red[k]);
     return o;
 }
 
@@ -140,14 +146,14 @@ __device__ __forceinline__ float4 row_stats(const PolicyArgs &a, const RowInputs
     return make_float4(lp, lse, in.w * slope, r);
 }
 
-// dL/dz of a vector whose first element is j: f [j = y] - fs 2^t, t = (z - ref) c.
+// dL/dz of a vector whose first element is j: f [j = y] - fs 2^t.
 template <typename T>
 __device__ __forceinline__ uint4 grad_vec(const PolicyArgs &a, uint4 v, float ref, float fs, float f, int32_t j, int32_t y) {
     constexpr int N = kVec<T>;
     float z[N];
     unpack<T>(v, z);
 #pragma unroll
-    for (int i = 0; i < N; ++i) z[i] = -fs * __builtin_amdgcn_exp2f((z[i] - ref) * a.c);
+    for (int i = 0; i < N; ++i) z[i] = -fs * __builtin_amdgcn_exp2f(exponent<T>(a, z[i] - ref));
     if ((uint32_t)(y - j) < (uint32_t)N) {
 #pragma unroll
         for (int i = 0; i < N; ++i) z[i] += j + i == y ? f : 0.0f;
@@ -205,7 +211,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_rows_ke
     }
     for (; j < V; j += kStep) add<T>(o, a, load_at(row, (int32_t)V, (int32_t)j));
     __shared__ Online red[kThreads / 64];
-    o = join<kThreads>(a, o, red);
+    o = join<T, kThreads>(a, o, red);
     if (threadIdx.x == 0) reinterpret_cast<float4 *>(a.stats)[t] = row_stats(a, in, o);
 }
 
@@ -259,7 +265,7 @@ template <typename T, int TH, int NV> __global__ __launch_bounds__(TH) void poli
             if (v < NV - 1 || last) add<T>(o, a, buf[v]);
         }
         for (int32_t j = j0 + rest; j < V; j += kStep) add<T>(o, a, load_at(row, V, j));
-        o = join<TH>(a, o, red[half]);
+        o = join<T, TH>(a, o, red[half]);
         half ^= 1;                                      // the other half is written before this one is again
         const float ref = uniform(reference(o.m));
         const float4 s = row_stats(a, in, o);
@@ -310,7 +316,10 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_backwar
         float z[N];
         unpack<T>(load_at(row, end, j), z);
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = -f * __builtin_amdgcn_exp2f(__builtin_fmaf(z[i] - base, a.c, shift));
+        for (int i = 0; i < N; ++i) {
+            const float d = z[i] - base;
+            z[i] = -f * __builtin_amdgcn_exp2f(__builtin_fmaf(d, a.c, sizeof(T) == 4 ? __builtin_fmaf(d, a.c_rest, shift) : shift));
+        }
         const bool here = (uint32_t)(y - j) < (uint32_t)N;
         if (here) {
 #pragma unroll
@@ -397,7 +406,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_part_ke
 #pragma unroll 4
     for (int32_t j = begin + (int32_t)threadIdx.x * kVec<T>; j < end; j += kThreads * kVec<T>) add<T>(o, a, load_at(row, end, j));
     __shared__ Online red[kThreads / 64];
-    o = join<kThreads>(a, o, red);
+    o = join<T, kThreads>(a, o, red);
     if (threadIdx.x == 0) {
         const int32_t y = a.targets[t];
         a.parts[t * gridDim.y + blockIdx.y] = make_float4(o.m, o.S, y >= begin && y < end ? to_f32(row[y]) : __builtin_nanf(""), 0.0f);
@@ -405,11 +414,12 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_part_ke
 }
 
 // A row's slices in their order, and its target's logit.
+template <typename T>
 __device__ __forceinline__ Online merge_parts(const PolicyArgs &a, int64_t t, int32_t slice, int slices, RowInputs &in) {
     Online o{-__builtin_inff(), 0.0f};
     for (int k = 0; k < slices; ++k) {
         const float4 p = a.parts[t * slices + k];
-        o = merge(a, o, Online{p.x, p.y});
+        o = merge<T>(a, o, Online{p.x, p.y});
         if (in.y >= 0 && in.y / slice == k) in.zy = p.z;      // NaN for a target behind the row's end
     }
     return o;
@@ -425,7 +435,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_finish_
             float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (w != 0.0f) {
                 RowInputs in = {w, a.old_logp[t], a.adv[t], a.ref ? a.ref[t] : 0.0f, __builtin_nanf(""), a.targets[t]};
-                const Online o = merge_parts(a, t, slice, slices, in);
+                const Online o = merge_parts<T>(a, t, slice, slices, in);
                 st = row_stats(a, in, o);
                 add_terms(a, w, in.adv, in.ref, st.x, st.w, s);
             }
@@ -443,7 +453,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_finish_
         return;
     }
     RowInputs in = row_inputs(a, t);
-    const Online o = merge_parts(a, t, slice, slices, in);
+    const Online o = merge_parts<T>(a, t, slice, slices, in);
     const float f = row_stats(a, in, o).z / a.temp;
     write_grad<T, kThreads>(a, row, out, begin, end, reference(o.m), f / o.S, f, in.y);
 }

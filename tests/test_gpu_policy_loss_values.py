@@ -90,3 +90,29 @@ def test_masked_and_missing_targets_from_statistics(T, V, dtype):
     for out in (None, c["logits"].clone()):
         got = reqat.policy_loss_backward(c["logits"] if out is None else out, c["targets"], stats, out=out)
         assert torch.isnan(got[1]).all() and torch.isfinite(got[0]).all()
+
+
+def _worst_temperature():
+    """The temperature whose scale log2(e) / temperature is rounded most."""
+    def off(t):
+        c = math.log2(math.e) / pr.f32(t)
+        return abs(pr.f32(c) - c) / c
+    return max((0.4 + 0.01 * k for k in range(200)), key=off)
+
+
+@pytest.mark.parametrize("T,V", [(1040, 4000), (3, 40000), (300, 9001)])
+def test_probabilities_of_far_tokens(T, V):
+    """FP32: tokens 60 below the first one.  Each exponent's own roundings (2^-24 of 60) average out over thousands of tokens;
+    what the scale's rounding adds is the same in all, 54 half steps here, and does not."""
+    temp = _worst_temperature()
+    c = pr.case(T, V, F32, DEV, temp=temp, edit=lambda z, y: (z.uniform_(-64 * temp, -56 * temp), z[:, 0].zero_(), y.zero_()))
+    e = pr.exact(c, temp)
+    loss, stats, grad = _run(c, temp, 0.0)
+    back = reqat.policy_loss_backward(c["logits"], c["targets"], stats, temperature=temp)
+    live = stats[:, 2] != 0
+    assert live.any()
+    want = -(stats[:, 2:3].double() / e.temp) * e.p
+    for got in (grad, back):
+        rel = (got.double() / want - 1)[live, 1:].mean()
+        # the factor and its two divisions 3, the exponential 2; log p (0 here) and the averages 1
+        assert float(rel.abs()) <= 6 * pr.E, float(rel) / pr.E
