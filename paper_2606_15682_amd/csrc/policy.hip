@@ -44,8 +44,10 @@ template <typename T> __device__ __forceinline__ void add(Online &o, const Polic
         o.m = mx;
     }
     const float ref = reference(o.m);
+    float sum = 0.0f;                       // of the vector first: single small terms would be lost beside a large S
 #pragma unroll
-    for (int i = 0; i < N; ++i) o.S += __builtin_amdgcn_exp2f(exponent<T>(a, z[i] - ref));
+    for (int i = 0; i < N; ++i) sum += __builtin_amdgcn_exp2f(exponent<T>(a, z[i] - ref));
+    o.S += sum;
 }
 
 template <typename T> __device__ __forceinline__ Online merge(const PolicyArgs &args, Online a, Online b) {

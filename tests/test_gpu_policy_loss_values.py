@@ -116,3 +116,18 @@ def test_probabilities_of_far_tokens(T, V):
         rel = (got.double() / want - 1)[live, 1:].mean()
         # the factor and its two divisions 3, the exponential 2; log p (0 here) and the averages 1
         assert float(rel.abs()) <= 6 * pr.E, float(rel) / pr.E
+
+
+@pytest.mark.parametrize("dtype,vector", [(F32, 4), (BF, 8)])
+def test_many_small_terms_beside_a_large_one(dtype, vector):
+    """The thread that has a row's first token adds up some 297 terms of 2^-25 beside its 1.  One after the other they are lost, half
+    of 2^-24 each; by vectors every addition rounds once, and so does each join."""
+    T, V = 130, 152064
+    z = torch.full((T, V), -25 * math.log(2.0), dtype=dtype, device=DEV)
+    z[:, 0] = 0.0
+    zeros = torch.zeros(T, device=DEV)
+    stats = reqat.policy_loss(z, torch.zeros(T, dtype=torch.int32, device=DEV), zeros, zeros)[1]
+    want = -math.log1p((V - 1) * math.exp(float(z[0, 1])))
+    # additions of a thread, 14 joins, exponentials and the logarithm (of 0.0045)
+    room = pr.E * (-(-V // (512 * vector)) + 14 + 4)
+    assert torch.all((stats[:, 0].double() - want).abs() <= room)
