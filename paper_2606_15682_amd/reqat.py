@@ -1464,16 +1464,16 @@ class AdamW:
             if dtype is torch.float32 and self.state_bits == 32 and name.endswith("scale"):
                 continue
             _index_arg(getattr(self, name), (n,), dtype, self.device, name)
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                       for t in (self.m, self.v, self.m_scale, self.v_scale) if t is not None and t.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("the states' buffers must not overlap")
         for i, at in enumerate(self.offsets):
             self._tensors[8 * i + 2] = bases[0] + at * self.m.element_size()
             self._tensors[8 * i + 3] = bases[1] + at * self.v.element_size()
             if self.state_bits == 8:
                 self._tensors[8 * i + 4] = bases[2] + at // 32
                 self._tensors[8 * i + 5] = bases[3] + at // 32
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
-                       for t in (self.m, self.v, self.m_scale, self.v_scale) if t is not None and t.numel())
-        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
-            raise ValueError("the states' buffers must not overlap")
         self._bases, self._seen_states = bases, [self.m, self.v, self.m_scale, self.v_scale]
         self._held_states = [t if t is None else t.detach() for t in (self.m, self.v, self.m_scale, self.v_scale)]
 

@@ -149,6 +149,11 @@ def test_other_tensors_in_the_same_memory_are_checked(calls, bits):
         opt.step(g)
     opt.v, opt.copies = kept, None
     opt.step(g)
+    for i, w in enumerate(_steps(calls)[-1][1]):          # nothing of what was refused stays
+        at = opt.offsets[i]
+        assert w["m"] == opt.m[at:].data_ptr() and w["v"] == opt.v[at:].data_ptr()
+        if bits == 8:
+            assert w["m_scale"] == opt.m_scale[at // 128:].data_ptr() and w["v_scale"] == opt.v_scale[at // 128:].data_ptr()
     opt.params[0] = p[0][:5]
     with pytest.raises(ValueError):
         opt.step(g)
