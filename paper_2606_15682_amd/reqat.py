@@ -1370,6 +1370,10 @@ def embedding_backward(dy, ids, rows, scale=1.0, out=None, accumulate=False, out
     return out
 
 
+_TENSORS = {torch.Tensor, torch.nn.Parameter}
+_SHAPE, _DTYPE, _DEVICE = map(operator.attrgetter, ("shape", "dtype", "device"))
+
+
 def _same_objects(a, b):
     return len(a) == len(b) and all(map(operator.is_, a, b))
 
@@ -1404,6 +1408,8 @@ class AdamW:
             raise TypeError("parameters must be bfloat16 or float32 tensors")
         self.device, self.dtype, self.state_bits = first.device, first.dtype, state_bits
         self._shapes = [p.shape if isinstance(p, torch.Tensor) else None for p in self.params]
+        # an array of reqat_adamw_tensor; a step fills in the addresses of gradients, and what has changed
+        self._tensors = array.array("q", bytes(64 * len(self.params)))
         self._adopt()
         self.lr, self.betas, self.eps, self.weight_decay, self.steps = lr, betas, eps, weight_decay, 0
         self.offsets, size = [], 0
@@ -1415,9 +1421,7 @@ class AdamW:
         self.m_scale = self.v_scale = None
         if state_bits == 8:
             self.m_scale, self.v_scale = (torch.zeros(size // 128, dtype=torch.float32, device=self.device) for _ in range(2))
-        # an array of reqat_adamw_tensor; a step fills in the addresses of parameters, copies and gradients
         self._sizes = array.array("q", [p.numel() for p in self.params])
-        self._tensors = array.array("q", bytes(64 * len(self.params)))
         self._total, self._bases = size, None
         self.missed = [0] * len(self.params)
         self.step_tensor = self.lr_tensor = self._coef = self._stepped = None
@@ -1426,17 +1430,12 @@ class AdamW:
             self.lr_tensor = torch.full((1,), lr, dtype=torch.float32, device=self.device)
             self._coef = torch.zeros(3, dtype=torch.float32, device=self.device)
 
-    def _addresses_now(self):
-        at = [p.data_ptr() for p in self.params]
-        if self.copies is not None:
-            at += [0 if c is None else c.data_ptr() for c in self.copies]
-        return array.array("q", at)
-
     def _tensors_now(self):
         return [*self.params, *(self.copies or ())]
 
     def _adopt(self):
-        """Checks parameters and copies and holds on to their memory, so that an address that stays is theirs."""
+        """Checks parameters and copies, enters their addresses and holds on to their memory, so that an address that stays
+        is theirs."""
         spans, held = [], []
         if len(self.params) != len(self._shapes):
             raise ValueError("params must stay %d tensors" % len(self._shapes))
@@ -1454,7 +1453,12 @@ class AdamW:
         spans.sort()
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("parameters and copies must not overlap")
-        self._held, self._addresses, self._seen = held, self._addresses_now(), self._tensors_now()
+        self._held, self._seen = held, self._tensors_now()
+        self._live = [t for t in self._seen if t is not None]
+        self._addresses = list(map(torch.Tensor.data_ptr, self._live))
+        copies = self.copies if self.copies is not None else [None] * len(self.params)
+        self._tensors[0::8] = array.array("q", [p.data_ptr() for p in self.params])
+        self._tensors[6::8] = array.array("q", [0 if c is None else c.data_ptr() for c in copies])
 
     def _place_states(self, bases):
         """Checks the states' buffers and enters their addresses: at the first step, and when one was replaced."""
@@ -1486,6 +1490,13 @@ class AdamW:
             raise ValueError("%s must be contiguous" % name)
         _same_device(t, self.device, name)
 
+    def _all_as_expected(self, grads, kind):
+        """Whether every gradient is a tensor of its parameter's shape: the checks of many small tensors, one attribute at a
+        time."""
+        return (kind in _FLOATS and set(map(type, grads)) <= _TENSORS and list(map(_SHAPE, grads)) == self._shapes
+                and set(map(_DTYPE, grads)) == {kind} and set(map(_DEVICE, grads)) == {self.device}
+                and all(map(torch.Tensor.is_contiguous, grads)))
+
     def step(self, grads, grad_scale=None):
         """One step with the gradients of all parameters (tensors of their shapes, all bfloat16 or all float32; None: the
         parameter is left out of this step, its count too), each times grad_scale (a float32 tensor of one element, as
@@ -1496,29 +1507,26 @@ class AdamW:
         if grad_scale is not None:
             _scale_arg(grad_scale, NVFP4, self.device, "grad_scale")
         kind = next((g.dtype for g in grads if isinstance(g, torch.Tensor)), torch.float32)
-        at, sizes, dev = [], self._sizes, self.device
-        for i, (g, shape) in enumerate(zip(grads, self._shapes)):
-            if g is None:
-                if sizes is self._sizes:
-                    sizes = self._sizes[:]
-                sizes[i] = 0                             # left out
-                at.append(0)
-                continue
-            if not (isinstance(g, torch.Tensor) and g.dtype is kind and kind in _FLOATS and g.shape == shape
-                    and g.device == dev and g.is_contiguous()):
-                self._tensor_arg(g, shape, (kind,) if kind in _FLOATS else tuple(_FLOATS), "grads[%d]" % i)
-            at.append(g.data_ptr())
+        sizes, dev = self._sizes, self.device
+        if self._all_as_expected(grads, kind):
+            at = list(map(torch.Tensor.data_ptr, grads))
+        else:
+            at, sizes = [], sizes[:]
+            for i, (g, shape) in enumerate(zip(grads, self._shapes)):
+                if g is None:
+                    sizes[i] = 0                         # left out
+                else:
+                    self._tensor_arg(g, shape, (kind,) if kind in _FLOATS else tuple(_FLOATS), "grads[%d]" % i)
+                at.append(0 if g is None else g.data_ptr())
         # another tensor, perhaps in the same memory, or one that was given other memory
-        if not _same_objects(self._tensors_now(), self._seen) or self._addresses_now() != self._addresses:
+        if not _same_objects(self._tensors_now(), self._seen) or list(map(torch.Tensor.data_ptr, self._live)) != self._addresses:
             self._adopt()
         states = [self.m, self.v, self.m_scale, self.v_scale]
         bases = [0 if t is None else t.data_ptr() for t in states]
         if bases != self._bases or not _same_objects(states, self._seen_states):
             self._place_states(bases)
         tensors, count = self._tensors, len(at)
-        tensors[0::8] = self._addresses[:count]
         tensors[1::8] = array.array("q", at)
-        tensors[6::8] = array.array("q", bytes(8 * count)) if self.copies is None else self._addresses[count:]
         _require_cuda(self.params[0], "params[0]")
         if self._coef is not None:
             self._step_captured(grads, kind, sizes, grad_scale)
@@ -1539,9 +1547,9 @@ class AdamW:
         self._step_written(grads)
 
     def _step_written(self, grads):
-        written = [p for p, g in zip(self.params, grads) if g is not None]
-        if self.copies is not None:
-            written += [c for c, g in zip(self.copies, grads) if c is not None and g is not None]
+        written = self._live
+        if any(g is None for g in grads):
+            written = [t for t, g in zip(self._seen, [*grads, *grads]) if t is not None and g is not None]
         _written(*written)
 
     def _hyper(self, step):
