@@ -476,7 +476,10 @@ size_t reqat_policy_loss_workspace_bytes(reqat_dtype dtype, int64_t T, int64_t V
 
 /*
  * The gradient of the policy loss from logits and stats, times *grad_loss (a device
- * float; NULL: 1).  Rows whose dL/dlp is 0 are not read.  grad as above.
+ * float; NULL: 1).  Rows whose dL/dlp is 0 are not read.  grad as above.  p comes from
+ * the target's logit and lp, or from the log-sum-exp where that is smaller, so a row whose
+ * log-sum-exp FP32 does not hold (+-Inf: all logits near the type's ends, temperature
+ * below 1) has its gradient too.
  */
 reqat_status reqat_policy_loss_backward(const void *logits, reqat_dtype dtype, int64_t T, int64_t V, int64_t ld,
                                         const int32_t *targets, const float *stats, float temperature, const float *grad_loss,
@@ -490,6 +493,7 @@ reqat_status reqat_policy_loss_backward(const void *logits, reqat_dtype dtype, i
  *   weight, bias [cols] of w_dtype, bias may be NULL;  y [rows][ldy] of dtype (y == x
  *   with the same stride is allowed, any other overlap is not: REQAT_E_UNSUPPORTED);
  *   stats [rows][2] FP32 out: mu, rstd.  eps >= 0.  rows == 0 is a no-op.
+ * The squares are FP32: rstd is 0 for rows whose sum of squares is past FP32's range.
  */
 reqat_status reqat_layer_norm(const void *x, reqat_dtype dtype, int64_t rows, int64_t cols, int64_t ldx, const void *weight,
                               const void *bias, reqat_dtype w_dtype, float eps, int center, void *y, int64_t ldy, float *stats,
@@ -511,8 +515,8 @@ reqat_status reqat_layer_norm_backward(const void *dy, int64_t lddy, const void 
 size_t reqat_layer_norm_workspace_bytes(reqat_dtype dtype, int64_t rows, int64_t cols, int bias);
 
 /*
- * Embedding lookup: out[t] = scale * table[ids[t]], rounded once (exact for scale 1);
- * an id outside [0, V) is padding and gives a row of zeros.
+ * Embedding lookup: out[t] = scale * table[ids[t]], the FP32 product rounded to dtype
+ * (exact for scale 1); an id outside [0, V) is padding and gives a row of zeros.
  *   ids [T] int32, T at most 2^22; table [V][ld_table], V at most 2^23; out [T][ldo] of
  *   dtype, D columns, at most 2^20 and T D at most 2^37; out must not overlap table
  *   (REQAT_E_UNSUPPORTED).
@@ -587,7 +591,7 @@ reqat_status reqat_adamw_step(const reqat_adamw_tensor *tensors, int64_t count, 
  */
 reqat_status reqat_adamw_coefficients(const reqat_adamw_hyper *hyper, const float *lr, int32_t *step, float *coef, void *stream);
 
-/* The values of 8-bit states: m_out, v_out [n] FP32 from codes [n] and scales [ceil(n / 128)]. */
+/* The values of 8-bit states: m_out, v_out [n] FP32 from codes [n] and scales [ceil(n / 128)]; n at most 2^33. */
 reqat_status reqat_adamw_moments(const uint8_t *m, const float *m_scale, const uint8_t *v, const float *v_scale, int64_t n,
                                  float *m_out, float *v_out, void *stream);
 

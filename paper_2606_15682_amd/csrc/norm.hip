@@ -8,6 +8,10 @@
 // In the backward pass each adds up its own dw and db there and asks for its next row before it works on one; the groups
 // of a workgroup join theirs through LDS, and a second launch joins the workgroups' in their order.  Rows of more than four
 // vectors a thread leave no registers for dw and db: a launch of its own adds them up by columns.
+//
+// Forward at the rate of a large copy (9001 x 3584 bfloat16 24 us, 5.4 TB/s), backward too up to 12288 bfloat16 elements a row
+// (8192 x 5120 46 + 5 us, 5.0 TB/s).  Rows of 12289 to 16384 spill 25 registers backward (4096 x 13824: 102 us for the 66 of a copy),
+// FP32 rows of more than 20480 elements 5 to 22, and the columns' pass reads x and dy once more (2048 x 27648: 137 us for 66).
 #include "internal.h"
 #include "row_io.h"
 

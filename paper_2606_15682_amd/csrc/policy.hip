@@ -69,7 +69,7 @@ template <typename T, int TH> __device__ __forceinline__ Online join(const Polic
     return o;
 }
 
-// exp(x) - x - 1 >= 0.  Near zero the difference of close numbers is summed as its series (to x^8 / 8!: 2e-8 of it at 1/2).
+// exp(x) - x - 1 >= 0.  Near zero the difference of close numbers is summed as its series (to x^8 / 8!: 5e-8 of it at 1/2).
 __device__ __forceinline__ float kl_term(float x) {
     if (__builtin_fabsf(x) < 0.5f) {
         float s = 1.0f / 40320.0f;
@@ -229,9 +229,10 @@ __device__ __forceinline__ void pin(uint4 &v, float x) { asm volatile("" : "+v"(
 // The row has more than (NV - 1) TH whole vectors (or NV is 0), so that all but the last step's accesses are without a
 // condition: behind a branch the compiler cannot count the accesses in flight, and waits for all of them.
 //
-// 4096 rows of 152064 bfloat16 logits, a quarter without weight, take 467 us, 4.7 TB/s of one read and one write (a large
-// copy: 5.2).  The row read twice, the second time from the caches, 615 us; 18 of its 19 vectors a thread held and the
-// last read again 481 us, all 19 with spilled registers 492 us, 15 511 us.
+// 4096 rows of 152064 bfloat16 logits, a quarter without weight, take 474 us, 4.6 TB/s of one read and one write (a large
+// copy: 5.2); with 17 of its 19 vectors a thread held and the others read again 9 us more, with 15 35 us more.  All 19 take
+// three registers more than there are (12 bytes of scratch) and 2 us less; rows of 18 vectors are 2 us slower then.  A form that
+// read every row twice, the second time from the caches, took 615 us.
 template <typename T, int TH, int NV> __global__ __launch_bounds__(TH) void policy_grad_kernel(PolicyArgs a) {
     constexpr int N = kVec<T>, kStep = TH * N, kHeld = kStep * NV, kBytes = TH * 16;
     const int32_t V = (int32_t)a.V, j0 = threadIdx.x * N, full = V / N * N, rest = full < kHeld ? full : kHeld;
@@ -297,6 +298,7 @@ template <typename T, int TH, int NV> __global__ __launch_bounds__(TH) void poli
 
 // The gradient from the statistics: a workgroup per row and slice of it.  p_j = 2^((z_j - z_y) c + lp log2(e)) or 2^(z_j c -
 // lse log2(e)), by the smaller of |lp| and |lse|, whose rounding is the exponent's error; dL/dz_y = -f (exp(lp) - 1).
+// 4096 x 152064 bfloat16 493 us, 5.05 TB/s, 64 rows 7.8 us; FP32 1024 rows 266 us, 4.7 TB/s.
 // hold: z_y has to stay for the row's other workgroups, where grad takes the logits' place; a launch of its own follows.
 template <typename T> __global__ __launch_bounds__(kThreads) void policy_backward_kernel(PolicyArgs a, int64_t slice, bool hold) {
     constexpr int N = kVec<T>;
@@ -465,7 +467,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void policy_finish_
 namespace {
 
 // Workgroups of 256 threads for rows of up to 4096 bytes a wave, else of 1024, with as many vectors as the row has and the
-// registers hold (128 a thread).  They are persistent: as many as the card's 256 compute units hold at once.
+// registers hold (128 a thread, with 18).  They are persistent: as many as the card's 256 compute units hold at once.
 template <typename T, int TH, int NV> void launch_grad_of(const PolicyArgs &a, int64_t steps, hipStream_t stream) {
     if (steps == NV) {
         const int64_t most = TH == 256 ? 4 * 256 : 256;
