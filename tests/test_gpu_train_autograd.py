@@ -19,7 +19,7 @@ def _cases():
             "embedding": ([rand(9, 40)], lambda t: reqat.Embedding.apply(y, t, 2.0))}
 
 
-@pytest.mark.parametrize("name", list(_cases()))
+@pytest.mark.parametrize("name", ["policy", "sem", "norm", "embedding"])
 def test_create_graph(name):
     values, f = _cases()[name]
     leaves = [v.to(DEV).requires_grad_() for v in values]
